@@ -412,6 +412,83 @@ int mkq_layernorm_int8(const void *x, int64_t M, int64_t D, const float *gamma, 
 int mkq_attention_int8(const void *qkv, int64_t batch, int64_t seq, int64_t hidden, int64_t heads,
                        void *ctx, float s_next, int8_t *q_out, void *stream);
 
+/* Group-scaled 4-bit weights: a step for every `group` (32, 64 or 128) neighbours of a row.  One such matrix serves as the
+ * table of mkq_embedding_int4_group and, tied, as the weights of mkq_linear_int4_group.
+ *   rows    ceil(K / 32) * 16 bytes: the canonical nibble packing, zero codes from K up to the next multiple of 32; any K > 0
+ *   steps   s_w [N, ceil(K / group)] binary32, step g of a row for its codes g * group .. ; the last group may be short
+ * mkq_pack_weights_int4_group: W [N, K] of w_dtype (F32, F16, BF16), row stride ldw; every group's step is its abs-max / 7
+ * (all zeros -> 1) unless s_w_in gives them (then > 0 and below 2^120, a precondition), its codes are Eq. 1 of section 3.1
+ * under that step; s_w_out may alias s_w_in.  N == 0 is a no-op.  Steps and biases of what follows need only the alignment of
+ * a binary32 value, so that rows of a table can be passed on their own.
+ * Errors: NULL, SHAPE (N < 0, K <= 0, ldw < K, group), ALIGN, DTYPE, UNSUPPORTED (N or K from about 2^31 on), HIP. */
+size_t mkq_group_weight_bytes(int64_t N, int64_t K);
+int mkq_pack_weights_int4_group(const void *W, int w_dtype, int64_t N, int64_t K, int64_t ldw, int group,
+                                const float *s_w_in, float *s_w_out, uint8_t *Wq_out, void *stream);
+
+/* Linear of few tokens on group-scaled 4-bit weights, activations in floats (the head over the vocabulary, single linears
+ * of decoding or of a classifier):
+ *     y[m,n] = sum_g s_w[n,g] ( sum_{k in g} x[m,k] c[n,k] ) + bias[n],  + residual, act, narrowed once to out_dtype
+ * Activations and codes enter the products exactly (binary32 ones too), all sums are binary32.  Infinities and NaN in a row
+ * of x reach that row of y, as in IEEE arithmetic on the dequantized weights.
+ *   x     [M, K] of x_dtype (F32, F16, BF16), row stride ldx (any alignment of the rows: a multiple of 16 bytes is faster)
+ *   Wq, s_w  from mkq_pack_weights_int4_group with the same group;  bias [N] binary32 or NULL
+ *   out   [M, N] of out_dtype (F32, F16, BF16)
+ *   epi   NULL, or act and residual (residual_dtype F32, F16 or BF16); its code and accumulator outputs: UNSUPPORTED
+ * Any M (made for up to 128 tokens), N and K; M == 0 is a no-op.  No workspace.
+ * Errors: NULL, SHAPE (group, ldx < K, ...), ALIGN, DTYPE, UNSUPPORTED, HIP. */
+int mkq_linear_int4_group(const void *x, int x_dtype, int64_t ldx, const uint8_t *Wq, const float *s_w, int group,
+                          const float *bias, int64_t M, int64_t N, int64_t K, void *out, int out_dtype,
+                          const mkq_epilogue *epi, void *stream);
+
+/* Token rows: out[i,:] = scale * table[tokens[i],:], one multiplication in binary32 and one rounding to out_dtype per value.
+ * A token outside [0, V) gives a row of zeros.
+ *   tokens  [M] whole numbers of token_bits (32 or 64) bits, aligned to their own size
+ *   table   [V, D] of table_dtype (F32, F16, BF16), row stride ld_table; or group-scaled 4-bit rows and their steps from
+ *           mkq_pack_weights_int4_group (N = V, K = D): then a value is scale * (code * step), both products in binary32
+ *   out     [M, D] of out_dtype (F32, F16, BF16), row stride ld_out (what lies between the rows is left as it is)
+ *   scale   finite (sqrt(D) in some models, else 1)
+ * Any D; rows that are multiples of 16 bytes are faster.  M == 0 is a no-op.
+ * Errors: NULL, SHAPE, ALIGN, SCALE, DTYPE (token_bits too), UNSUPPORTED (V or D from about 2^31 on), HIP. */
+int mkq_embedding(const void *tokens, int token_bits, int64_t M, const void *table, int table_dtype, int64_t V, int64_t D,
+                  int64_t ld_table, float scale, void *out, int out_dtype, int64_t ld_out, void *stream);
+int mkq_embedding_int4_group(const void *tokens, int token_bits, int64_t M, const uint8_t *Wq, const float *s_w, int group,
+                             int64_t V, int64_t D, float scale, void *out, int out_dtype, int64_t ld_out, void *stream);
+
+/* Gradient of the lookup with respect to its float table:
+ *     grad[v,:] = scale * sum_{i: tokens[i] = v} dy[i,:]        (accumulate == 0: all V rows are written, zeros without a token)
+ *     grad[v,:] += the same                                     (accumulate != 0: rows without a token are left as they are)
+ * Tokens outside [0, V) and those equal to padding_token (a negative one: none) count for nothing.  The positions are sorted
+ * by token and every row is summed in binary32 in an order that the tokens alone decide: equal calls give equal bits.  One
+ * rounding to grad_dtype, behind the scale and the addition.
+ *   dy    [M, D] of dy_dtype (F32, F16, BF16), row stride ld_dy
+ *   grad  [V, D] of grad_dtype (F32, F16, BF16), row stride ld_grad (what lies between the rows is left as it is)
+ *   workspace  at least mkq_embedding_gradient_workspace_bytes(M, D) bytes, 16-byte aligned; no preparation
+ * M == 0 writes the zeros only (no workspace needed).
+ * Errors: NULL, SHAPE, ALIGN, SCALE, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
+size_t mkq_embedding_gradient_workspace_bytes(int64_t M, int64_t D);
+int mkq_embedding_gradient(const void *tokens, int token_bits, int64_t M, const void *dy, int dy_dtype, int64_t ld_dy,
+                           int64_t V, int64_t D, float scale, int64_t padding_token, int accumulate, void *grad,
+                           int grad_dtype, int64_t ld_grad, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Norm over the gradients of n tensors, and their clipping to it:
+ *     norm = sqrt(sum over all tensors and values of g^2)       (squares and sums binary64, in a fixed order)
+ *     out  = c g,  c = min(1, max_norm / (norm + 1e-6))          (mkq_clip_gradients; one rounding per value)
+ *   grads_host, counts_host, dtypes_host   host arrays [n]: device pointers, numbers of values, F32 / F16 / BF16 each; a tensor
+ *                 is contiguous and aligned to its own element size (16 bytes are faster); one without values may be NULL
+ *   outs_host     host array [n] of device pointers; outs_host[t] == grads_host[t] clips in place, otherwise it overlaps no
+ *                 gradient
+ *   norm_out      device, the norm before clipping, binary32
+ *   max_norm      > 0 (infinity: copies only)
+ *   workspace     at least mkq_gradient_norm_workspace_bytes(n) bytes, 16-byte aligned; no preparation
+ * A NaN among the gradients makes the norm and all results NaN; an infinity makes the norm infinite, c = 0 and itself NaN.
+ * n == 0: the norm is 0.  Errors: NULL, SHAPE, ALIGN, SCALE, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
+size_t mkq_gradient_norm_workspace_bytes(int64_t n);
+int mkq_gradient_norm(int64_t n, const void *const *grads_host, const int64_t *counts_host, const int32_t *dtypes_host,
+                      float *norm_out, void *workspace, size_t workspace_bytes, void *stream);
+int mkq_clip_gradients(int64_t n, const void *const *grads_host, void *const *outs_host, const int64_t *counts_host,
+                       const int32_t *dtypes_host, float max_norm, float *norm_out, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
 #ifdef __cplusplus
 }
 #endif

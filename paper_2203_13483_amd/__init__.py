@@ -33,6 +33,9 @@ EXPORTS = [
     "mkq_tuning_linear_int4", "mkq_tuning_linear_int4_e3m2", "mkq_tuning_linear_int4_stream", "mkq_tuning_linear_int8",
     "mkq_stream_weight_bytes", "mkq_repack_weights_int4_stream", "mkq_linear_int4_stream",
     "mkq_linear_int4_stream_static",
+    "mkq_group_weight_bytes", "mkq_pack_weights_int4_group", "mkq_linear_int4_group",
+    "mkq_embedding", "mkq_embedding_int4_group", "mkq_embedding_gradient_workspace_bytes", "mkq_embedding_gradient",
+    "mkq_gradient_norm_workspace_bytes", "mkq_gradient_norm", "mkq_clip_gradients",
     "mkq_measure_stream", "mkq_measure_mfma_i8_operand_bytes", "mkq_measure_mfma_i8_ops", "mkq_measure_mfma_i8",
 ]
 
@@ -143,6 +146,16 @@ def load() -> C.CDLL:
         "mkq_attention_int8": (ci, [vp, i64, i64, i64, i64, vp, f32, vp, vp]),
         "mkq_bert_layer_int8_workspace": (ci, [C.POINTER(BertLayerParams), C.POINTER(BertLayerWorkspaceLayout)]),
         "mkq_bert_layer_int8": (ci, [C.POINTER(BertLayerParams), vp, ci, vp, vp, vp, vp, sz, vp]),
+        "mkq_group_weight_bytes": (sz, [i64, i64]),
+        "mkq_pack_weights_int4_group": (ci, [vp, ci, i64, i64, i64, ci, vp, vp, vp, vp]),
+        "mkq_linear_int4_group": (ci, [vp, ci, i64, vp, vp, ci, vp, i64, i64, i64, vp, ci, C.POINTER(Epilogue), vp]),
+        "mkq_embedding": (ci, [vp, ci, i64, vp, ci, i64, i64, i64, f32, vp, ci, i64, vp]),
+        "mkq_embedding_int4_group": (ci, [vp, ci, i64, vp, vp, ci, i64, i64, f32, vp, ci, i64, vp]),
+        "mkq_embedding_gradient_workspace_bytes": (sz, [i64, i64]),
+        "mkq_embedding_gradient": (ci, [vp, ci, i64, vp, ci, i64, i64, i64, f32, i64, ci, vp, ci, i64, vp, sz, vp]),
+        "mkq_gradient_norm_workspace_bytes": (sz, [i64]),
+        "mkq_gradient_norm": (ci, [i64, vp, vp, vp, vp, vp, sz, vp]),
+        "mkq_clip_gradients": (ci, [i64, vp, vp, vp, vp, f32, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -625,6 +638,212 @@ def mkq_attention_varlen(qkv, cu_seqlens, max_seq: int, hidden: int, heads: int,
                                        float(s_next), _ptr(q), int(q_bits) if q_bits else 4, _stream(stream)),
            "mkq_attention_varlen")
     return ctx, q
+
+
+# The two ends of an encoder and the training of its table.  These take tensors as programs have them, so what would be read
+# wrongly is refused here: strides that the call cannot express, tensors of another device, sizes that do not agree.
+
+def _need(ok, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t, what: str):
+    """Row stride of a matrix whose rows are contiguous."""
+    _need(t.dim() == 2 and (t.size(1) <= 1 or t.stride(1) == 1), f"{what}: a matrix with contiguous rows")
+    return t.stride(0) if t.size(0) > 1 else max(t.size(1), 1)
+
+
+def _same_device(first, *rest):
+    dev = first.device
+    _need(dev.type == "cuda" and dev.index == _torch().cuda.current_device(), "tensors live on the current GPU")
+    for t in rest:
+        _need(t is None or t.device == dev, "tensors live on one GPU")
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor that belongs to the stream of the call, so that its memory is not handed on before the call is done."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def mkq_group_weight_bytes(N: int, K: int) -> int:
+    return int(load().mkq_group_weight_bytes(N, K))
+
+
+def mkq_pack_weights_int4_group(W, group: int = 64, s_w_in=None, stream=None):
+    """W [N,K] float32/float16/bfloat16 -> (Wq uint8 [N, ceil(K/32)*16], s_w float32 [N, ceil(K/group)])."""
+    torch = _torch()
+    ldw = _rows(W, "W")
+    N, K = W.shape
+    _same_device(W, s_w_in)
+    groups = -(-K // group) if group > 0 else 0
+    if s_w_in is not None:
+        _need(s_w_in.dtype == torch.float32 and s_w_in.is_contiguous() and tuple(s_w_in.shape) == (N, groups),
+              "s_w_in: contiguous float32 [N, ceil(K/group)]")
+    Wq = _new((N, -(-K // 32) * 16), torch.uint8, W.device, stream)
+    s_w = _new((N, groups), torch.float32, W.device, stream)
+    _check(load().mkq_pack_weights_int4_group(_ptr(W), _dtype_code(W), N, K, ldw, int(group), _ptr(s_w_in), _ptr(s_w),
+                                              _ptr(Wq), _stream(stream)), "mkq_pack_weights_int4_group")
+    return Wq, s_w
+
+
+def _group_table(Wq, s_w, N: int, K: int, group: int):
+    torch = _torch()
+    _need(Wq.dtype == torch.uint8 and Wq.is_contiguous() and Wq.numel() == N * (-(-K // 32) * 16),
+          "Wq: contiguous uint8 [N, ceil(K/32)*16]")
+    _need(s_w.dtype == torch.float32 and s_w.is_contiguous() and group > 0 and s_w.numel() == N * -(-K // group),
+          "s_w: contiguous float32 [N, ceil(K/group)]")
+
+
+def mkq_linear_int4_group(x, Wq, s_w, bias, N: int, K: int, group: int = 64, out_dtype: int | None = None, *,
+                          act: int = MKQ_ACT_NONE, residual=None, out=None, stream=None):
+    """x [M,K] float times group-scaled 4-bit weights (mkq_pack_weights_int4_group) -> [M,N] of out_dtype (None: x's)."""
+    torch = _torch()
+    ldx = _rows(x, "x")
+    M = x.size(0)
+    _need(x.size(1) == K, "x: [M, K]")
+    _same_device(x, Wq, s_w, bias, residual, out)
+    _group_table(Wq, s_w, N, K, group)
+    _need(bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == N), "bias: float32 [N]")
+    if out_dtype is None:
+        out_dtype = _dtype_code(x)
+    if out is None:
+        out = _new((M, N), _torch_dtype(out_dtype), x.device, stream)
+    else:
+        _need(out.dtype == _torch_dtype(out_dtype) and out.is_contiguous() and tuple(out.shape) == (M, N), "out: contiguous [M, N] of out_dtype")
+    epi = None
+    if act or residual is not None:
+        _need(residual is None or (residual.is_contiguous() and tuple(residual.shape) == (M, N)), "residual: contiguous [M, N]")
+        epi = C.byref(Epilogue(act=int(act), residual=_ptr(residual),
+                               residual_dtype=_dtype_code(residual) if residual is not None else MKQ_F32))
+    _check(load().mkq_linear_int4_group(_ptr(x), _dtype_code(x), ldx, _ptr(Wq), _ptr(s_w), int(group), _ptr(bias), M, N, K,
+                                        _ptr(out), int(out_dtype), epi, _stream(stream)), "mkq_linear_int4_group")
+    return out
+
+
+def _tokens(tokens):
+    torch = _torch()
+    _need(tokens.dtype in (torch.int32, torch.int64) and tokens.is_contiguous(), "tokens: contiguous int32 or int64")
+    return 64 if tokens.dtype == torch.int64 else 32
+
+
+def _token_rows(tokens, D: int, out, out_dtype: int, stream):
+    """The caller's [M, D] rows, or new ones, and their stride."""
+    M = tokens.numel()
+    if out is None:
+        return _new((M, D), _torch_dtype(out_dtype), tokens.device, stream), D
+    ld = _rows(out, "out")
+    _need(out.dtype == _torch_dtype(out_dtype) and tuple(out.shape) == (M, D), "out: [M, D] of out_dtype")
+    return out, ld
+
+
+def mkq_embedding(tokens, table, scale: float = 1.0, out_dtype: int | None = None, *, out=None, stream=None):
+    """Rows of table [V,D] for tokens (int32 / int64, any shape, M of them) times scale -> [M,D] of out_dtype (None: the table's)."""
+    bits = _tokens(tokens)
+    ld_table = _rows(table, "table")
+    V, D = table.shape
+    _same_device(tokens, table, out)
+    if out_dtype is None:
+        out_dtype = _dtype_code(table)
+    out, ld_out = _token_rows(tokens, D, out, out_dtype, stream)
+    _check(load().mkq_embedding(_ptr(tokens), bits, tokens.numel(), _ptr(table), _dtype_code(table), V, D, ld_table, float(scale),
+                                _ptr(out), int(out_dtype), ld_out, _stream(stream)), "mkq_embedding")
+    return out
+
+
+def mkq_embedding_int4_group(tokens, Wq, s_w, V: int, D: int, group: int = 64, scale: float = 1.0, out_dtype: int = MKQ_F32, *,
+                             out=None, stream=None):
+    """Rows of a group-scaled 4-bit table (mkq_pack_weights_int4_group with N = V, K = D) times scale -> [M,D] of out_dtype."""
+    bits = _tokens(tokens)
+    _same_device(tokens, Wq, s_w, out)
+    _group_table(Wq, s_w, V, D, group)
+    out, ld_out = _token_rows(tokens, D, out, out_dtype, stream)
+    _check(load().mkq_embedding_int4_group(_ptr(tokens), bits, tokens.numel(), _ptr(Wq), _ptr(s_w), int(group), V, D, float(scale),
+                                           _ptr(out), int(out_dtype), ld_out, _stream(stream)), "mkq_embedding_int4_group")
+    return out
+
+
+def mkq_embedding_gradient_workspace_bytes(M: int, D: int) -> int:
+    return int(load().mkq_embedding_gradient_workspace_bytes(M, D))
+
+
+def mkq_embedding_gradient(tokens, dy, V: int, scale: float = 1.0, grad_dtype: int = MKQ_F32, *, padding_token: int = -1,
+                           grad=None, accumulate: bool = False, workspace=None, stream=None):
+    """Gradient [V,D] of mkq_embedding's table from dy [M,D].  ``accumulate``: added to the ``grad`` that is passed in."""
+    torch = _torch()
+    bits = _tokens(tokens)
+    ld_dy = _rows(dy, "dy")
+    M, D = dy.shape
+    _need(tokens.numel() == M, "dy: a row for every token")
+    _same_device(tokens, dy, grad, workspace)
+    _need(grad is not None or not accumulate, "accumulate: needs the gradient to add to")
+    if grad is None:
+        grad, ld_grad = _new((V, D), _torch_dtype(grad_dtype), dy.device, stream), D
+    else:
+        ld_grad = _rows(grad, "grad")
+        _need(grad.dtype == _torch_dtype(grad_dtype) and tuple(grad.shape) == (V, D), "grad: [V, D] of grad_dtype")
+    if workspace is None:
+        workspace = _new(mkq_embedding_gradient_workspace_bytes(M, D), torch.uint8, dy.device, stream)
+    _check(load().mkq_embedding_gradient(_ptr(tokens), bits, M, _ptr(dy), _dtype_code(dy), ld_dy, V, D, float(scale), int(padding_token),
+                                         int(accumulate), _ptr(grad), int(grad_dtype), ld_grad, _ptr(workspace), workspace.nbytes,
+                                         _stream(stream)), "mkq_embedding_gradient")
+    return grad
+
+
+def mkq_gradient_norm_workspace_bytes(n: int) -> int:
+    return int(load().mkq_gradient_norm_workspace_bytes(n))
+
+
+def _tensor_list(tensors):
+    """Host arrays of addresses, numbers of values and types."""
+    n = len(tensors)
+    return ((C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int64 * n)(*[t.numel() for t in tensors]),
+            (C.c_int32 * n)(*[_dtype_code(t) for t in tensors]))
+
+
+def _norm_buffers(n: int, device, norm_out, workspace, stream):
+    torch = _torch()
+    if norm_out is None:
+        norm_out = _new(1, torch.float32, device, stream)
+    _need(norm_out.dtype == torch.float32 and norm_out.numel() == 1, "norm_out: float32 [1]")
+    if workspace is None:
+        workspace = _new(mkq_gradient_norm_workspace_bytes(n), torch.uint8, device, stream)
+    return norm_out, workspace
+
+
+def mkq_gradient_norm(grads, norm_out=None, workspace=None, stream=None):
+    """Norm over all values of a list of contiguous tensors (float32 / float16 / bfloat16, mixed) -> float32 tensor [1]."""
+    grads = list(grads)
+    _need(grads and all(t.is_contiguous() for t in grads), "grads: contiguous tensors, one at least")
+    _same_device(*grads, norm_out, workspace)
+    norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
+    at, counts, dtypes = _tensor_list(grads)
+    _check(load().mkq_gradient_norm(len(grads), at, counts, dtypes, _ptr(norm_out), _ptr(workspace), workspace.nbytes,
+                                    _stream(stream)), "mkq_gradient_norm")
+    return norm_out
+
+
+def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, workspace=None, stream=None):
+    """Scales a list of gradients to a norm of at most max_norm, in place or into ``outs`` (same types and sizes); returns the
+    norm before, float32 tensor [1]."""
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    _need(grads and all(t.is_contiguous() for t in grads), "grads: contiguous tensors, one at least")
+    _same_device(*grads, norm_out, workspace)
+    if outs is not grads:
+        _need(len(outs) == len(grads) and all(o.dtype == t.dtype and o.numel() == t.numel() and o.is_contiguous()
+                                              for o, t in zip(outs, grads)), "outs: contiguous, the gradients' types and sizes")
+        _same_device(*outs)
+    norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
+    at, counts, dtypes = _tensor_list(grads)
+    out_at = at if outs is grads else (C.c_void_p * len(outs))(*[t.data_ptr() for t in outs])
+    _check(load().mkq_clip_gradients(len(grads), at, out_at, counts, dtypes, float(max_norm), _ptr(norm_out), _ptr(workspace),
+                                     workspace.nbytes, _stream(stream)), "mkq_clip_gradients")
+    return norm_out
 
 
 class BertLayerInt4:

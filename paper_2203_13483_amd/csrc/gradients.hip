@@ -1,0 +1,248 @@
+// The norm over the gradients of many tensors, and their clipping:
+//
+//     norm = sqrt( sum_t sum_i g_t[i]^2 ),   out_t[i] = min(1, max_norm / (norm + 1e-6)) g_t[i]
+//
+// Bound by HBM: every value is read once for the norm and once more, behind it, to be scaled and written.  Squares and their
+// sums are binary64, in an order that does not depend on which workgroup is done first, so the norm of gradients beyond
+// 1e19 does not overflow and equal inputs give equal bits.
+#include "elements.h"
+
+namespace mkq {
+
+// Tensors of one launch travel in the kernel's arguments, whose room is 4 KiB
+constexpr int TENSORS = 100;
+constexpr int PIECE = 8192;           // values that a workgroup takes at a time
+constexpr int NORM_WORKGROUPS = 2048;  // partial sums of a launch
+struct TensorList {
+    const void *grad[TENSORS];
+    void *out[TENSORS];
+    int64_t count[TENSORS];
+    int32_t first_piece[TENSORS + 1];
+    int8_t dtype[TENSORS];
+    int32_t n;
+};
+static_assert(sizeof(TensorList) <= 3800, "kernel arguments");
+
+// f(tensor, first value, values) for the pieces of this workgroup
+template <class F>
+__device__ __forceinline__ void for_each_piece(const TensorList &l, F &&f)
+{
+    const int pieces = l.first_piece[l.n];
+    for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        int lo = 0, hi = l.n;  // the last tensor whose first piece is at most this one
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (l.first_piece[mid] <= piece) lo = mid;
+            else hi = mid;
+        }
+        const int64_t from = (int64_t)(piece - l.first_piece[lo]) * PIECE;
+        const int64_t left = l.count[lo] - from;
+        f(lo, from, (int)(left < PIECE ? left : PIECE));
+    }
+}
+
+// Sum over a workgroup of 256, the same bits in every thread
+__device__ __forceinline__ double workgroup_sum(double v, double *part)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+template <class E>
+__device__ __forceinline__ double sum_squares(const typename E::raw *g, int values)
+{
+    double sum = 0.0;
+    int i = threadIdx.x * 8;
+    if (reinterpret_cast<uintptr_t>(g) % 16 == 0) {
+        for (; i + 8 <= values; i += 256 * 8) {
+            float v[8];
+            get8<E>(g + i, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)v[e], (double)v[e], sum);
+        }
+    }
+    for (; i < values; i += 256 * 8)
+        for (int e = 0; e < 8; ++e)
+            if (i + e < values) {
+                const double v = (double)E::get(g[i + e]);
+                sum = __builtin_fma(v, v, sum);
+            }
+    return sum;
+}
+
+__global__ __launch_bounds__(256) void norm_partials_kernel(const TensorList l, double *__restrict__ partials)
+{
+    __shared__ double part[4];
+    double sum = 0.0;
+    for_each_piece(l, [&](int t, int64_t from, int values) {
+        if (l.dtype[t] == MKQ_F32) sum += sum_squares<ElemF32>(static_cast<const float *>(l.grad[t]) + from, values);
+        else if (l.dtype[t] == MKQ_F16) sum += sum_squares<ElemF16>(static_cast<const uint16_t *>(l.grad[t]) + from, values);
+        else sum += sum_squares<ElemBF16>(static_cast<const uint16_t *>(l.grad[t]) + from, values);
+    });
+    sum = workgroup_sum(sum, part);
+    if (threadIdx.x == 0) partials[blockIdx.x] = sum;
+}
+
+__device__ __forceinline__ double norm_of(const double *__restrict__ partials, int count, double *part)
+{
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < count; i += 256) sum += partials[i];
+    return sqrt(workgroup_sum(sum, part));
+}
+
+__global__ __launch_bounds__(256) void norm_kernel(const double *__restrict__ partials, int count, float *__restrict__ norm_out)
+{
+    __shared__ double part[4];
+    const double norm = norm_of(partials, count, part);
+    if (threadIdx.x == 0) *norm_out = (float)norm;
+}
+
+template <class E>
+__device__ __forceinline__ void scale_values(const typename E::raw *g, typename E::raw *out, int values, float c)
+{
+    int i = threadIdx.x * 8;
+    if ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) % 16 == 0) {
+        for (; i + 8 <= values; i += 256 * 8) {
+            float v[8];
+            get8<E>(g + i, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= c;
+            put8<E>(out + i, v);
+        }
+    }
+    for (; i < values; i += 256 * 8)
+        for (int e = 0; e < 8; ++e)
+            if (i + e < values) out[i + e] = E::put(E::get(g[i + e]) * c);
+}
+
+// Every workgroup adds up the partial sums itself (16 KB out of the L2), which spares a launch between the two passes.
+// A factor of 1 leaves gradients that are clipped in place as they are.
+__global__ __launch_bounds__(256) void clip_kernel(const TensorList l, const double *__restrict__ partials, int count, float max_norm,
+                                                   float *__restrict__ norm_out)
+{
+    __shared__ double part[4];
+    const double norm = norm_of(partials, count, part);
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    const double q = (double)max_norm / (norm + 1e-6);
+    const float c = q < 1.0 || q != q ? (float)q : 1.0f;
+    for_each_piece(l, [&](int t, int64_t from, int values) {
+        if (c == 1.0f && l.out[t] == l.grad[t]) return;
+        if (l.dtype[t] == MKQ_F32)
+            scale_values<ElemF32>(static_cast<const float *>(l.grad[t]) + from, static_cast<float *>(l.out[t]) + from, values, c);
+        else if (l.dtype[t] == MKQ_F16)
+            scale_values<ElemF16>(static_cast<const uint16_t *>(l.grad[t]) + from, static_cast<uint16_t *>(l.out[t]) + from, values, c);
+        else
+            scale_values<ElemBF16>(static_cast<const uint16_t *>(l.grad[t]) + from, static_cast<uint16_t *>(l.out[t]) + from, values, c);
+    });
+}
+
+// The lists of the launches that n tensors take, one after the other: f(list, workgroups)
+template <class F>
+static int for_each_list(int64_t n, const void *const *grads, void *const *outs, const int64_t *counts, const int32_t *dtypes, F &&f)
+{
+    for (int64_t t = 0; t < n;) {
+        TensorList l;
+        l.n = 0;
+        l.first_piece[0] = 0;
+        for (; t < n && l.n < TENSORS; ++t) {
+            if (counts[t] == 0) continue;
+            l.grad[l.n] = grads[t];
+            l.out[l.n] = outs ? outs[t] : const_cast<void *>(grads[t]);
+            l.count[l.n] = counts[t];
+            l.dtype[l.n] = (int8_t)dtypes[t];
+            l.first_piece[l.n + 1] = l.first_piece[l.n] + (int32_t)ceil_div(counts[t], PIECE);
+            ++l.n;
+        }
+        if (l.n == 0) break;
+        const int pieces = l.first_piece[l.n];
+        f(l, pieces < NORM_WORKGROUPS ? pieces : NORM_WORKGROUPS);
+        if (launch_status() != MKQ_OK) return MKQ_ERR_HIP;
+    }
+    return MKQ_OK;
+}
+
+static int check_tensors(int64_t n, const void *const *grads, void *const *outs, const int64_t *counts, const int32_t *dtypes,
+                         const void *workspace, size_t workspace_bytes)
+{
+    if (n < 0) return MKQ_ERR_SHAPE;
+    if (n > 0 && (!grads || !counts || !dtypes)) return MKQ_ERR_NULL;
+    int64_t pieces = 0;
+    for (int64_t t = 0; t < n; ++t) {
+        if (!is_float_dtype(dtypes[t])) return MKQ_ERR_DTYPE;
+        if (counts[t] < 0) return MKQ_ERR_SHAPE;
+        if (counts[t] == 0) continue;
+        if (!grads[t] || (outs && !outs[t])) return MKQ_ERR_NULL;
+        const uintptr_t low = reinterpret_cast<uintptr_t>(grads[t]) | (outs ? reinterpret_cast<uintptr_t>(outs[t]) : 0);
+        if (low % dtype_bytes(dtypes[t])) return MKQ_ERR_ALIGN;
+        pieces += (counts[t] - 1) / PIECE + 1;
+        if (pieces > 0x7FFFFFFF) return MKQ_ERR_UNSUPPORTED;
+    }
+    if (!workspace || workspace_bytes < mkq_gradient_norm_workspace_bytes(n)) return MKQ_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
+    return MKQ_OK;
+}
+
+// Launches the partial sums of all tensors; *count: how many there are
+static int launch_partials(int64_t n, const void *const *grads, const int64_t *counts, const int32_t *dtypes, double *partials, int *count,
+                           hipStream_t st)
+{
+    *count = 0;
+    return for_each_list(n, grads, nullptr, counts, dtypes, [&](const TensorList &l, int workgroups) {
+        norm_partials_kernel<<<workgroups, 256, 0, st>>>(l, partials + *count);
+        *count += workgroups;
+    });
+}
+
+}  // namespace mkq
+
+using namespace mkq;
+
+extern "C" size_t mkq_gradient_norm_workspace_bytes(int64_t n)
+{
+    return n < 0 ? 0 : (size_t)(n / TENSORS + 1) * NORM_WORKGROUPS * sizeof(double);
+}
+
+extern "C" int mkq_gradient_norm(int64_t n, const void *const *grads_host, const int64_t *counts_host, const int32_t *dtypes_host,
+                                 float *norm_out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!norm_out) return MKQ_ERR_NULL;
+    if (!aligned4(norm_out)) return MKQ_ERR_ALIGN;
+    int status = check_tensors(n, grads_host, nullptr, counts_host, dtypes_host, workspace, workspace_bytes);
+    if (status != MKQ_OK) return status;
+    const hipStream_t st = as_stream(stream);
+    double *partials = static_cast<double *>(workspace);
+    int count;
+    status = launch_partials(n, grads_host, counts_host, dtypes_host, partials, &count, st);
+    if (status != MKQ_OK) return status;
+    norm_kernel<<<1, 256, 0, st>>>(partials, count, norm_out);
+    return launch_status();
+}
+
+extern "C" int mkq_clip_gradients(int64_t n, const void *const *grads_host, void *const *outs_host, const int64_t *counts_host,
+                                  const int32_t *dtypes_host, float max_norm, float *norm_out, void *workspace, size_t workspace_bytes,
+                                  void *stream)
+{
+    if (!norm_out || (n > 0 && !outs_host)) return MKQ_ERR_NULL;
+    if (!aligned4(norm_out)) return MKQ_ERR_ALIGN;
+    if (!(max_norm > 0.0f)) return MKQ_ERR_SCALE;
+    int status = check_tensors(n, grads_host, outs_host, counts_host, dtypes_host, workspace, workspace_bytes);
+    if (status != MKQ_OK) return status;
+    const hipStream_t st = as_stream(stream);
+    double *partials = static_cast<double *>(workspace);
+    int count;
+    status = launch_partials(n, grads_host, counts_host, dtypes_host, partials, &count, st);
+    if (status != MKQ_OK) return status;
+    if (count == 0) {
+        norm_kernel<<<1, 256, 0, st>>>(partials, 0, norm_out);
+        return launch_status();
+    }
+    float *norm_at = norm_out;  // written by the first of the launches
+    return for_each_list(n, grads_host, outs_host, counts_host, dtypes_host, [&](const TensorList &l, int workgroups) {
+        clip_kernel<<<workgroups, 256, 0, st>>>(l, partials, count, max_norm, norm_at);
+        norm_at = nullptr;
+    });
+}

@@ -1,0 +1,128 @@
+"""The norm over many gradients and their clipping against 64 bits.  The norm is a binary64 sum: off by half a binary32 step (and
+a relative 1e-12 of the sum).  A result is g c with c rounded to binary32, the product rounded to binary32 and to the tensor's
+type: two steps of 2^-24 and half a step of the type."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+KINDS = [torch.float32, torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def mkq():
+    assert torch.cuda.is_available()
+    import paper_2203_13483_amd as m
+    m.load()
+    return m
+
+
+def tensors(sizes, seed, dtypes=KINDS, std=1.0):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return [(torch.randn(n, device="cuda", generator=g) * std).to(dtypes[i % len(dtypes)]) for i, n in enumerate(sizes)]
+
+
+def true_norm(ts):
+    return math.sqrt(math.fsum(float(t.double().square().sum()) for t in ts))
+
+
+def check(mkq, ts, max_norm, in_place):
+    before = [t.clone() for t in ts]
+    want = true_norm(before)
+    assert abs(float(mkq.mkq_gradient_norm(ts)) - want) <= want * (2.0 ** -24 + 1e-12)
+    outs = ts if in_place else [torch.full_like(t, 9) for t in ts]
+    norm = mkq.mkq_clip_gradients(ts, max_norm, outs=None if in_place else outs)
+    assert abs(float(norm) - want) <= want * (2.0 ** -24 + 1e-12)
+    c = min(1.0, max_norm / (want + 1e-6))
+    for o, b in zip(outs, before):
+        if c == 1.0:
+            assert torch.equal(o, b)
+            continue
+        y = b.double() * c
+        info = torch.finfo(o.dtype)
+        tol = 2 * 2.0 ** -24 * 1.01 * y.abs()
+        tol = tol + (y.abs() + tol) * info.eps / 2 + info.smallest_normal * info.eps / 2
+        assert bool(((o.double() - y).abs() <= tol).all())
+    if not in_place:
+        assert all(torch.equal(t, b) for t, b in zip(ts, before))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("factor", [0.01, 0.5, 2.0, math.inf])
+@pytest.mark.parametrize("sizes", [[1], [7], [8], [0, 5, 0], [8191, 8192, 8193], [3, 100000, 1, 17, 0, 65536], [1000000, 300001],
+                                   list(range(1, 120)), [50] * 250, [0, 0]])
+def test_clip(mkq, sizes, factor, in_place):
+    ts = tensors(sizes, len(sizes))
+    check(mkq, ts, factor * true_norm(ts) if true_norm(ts) and factor < 9 else 1.0 if factor < 9 else factor, in_place)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_views_at_any_element(mkq, in_place):
+    """Neighbours in one buffer: only their elements are aligned, and what lies between them is left alone"""
+    for dtype in KINDS:
+        flat = torch.full((40000,), 100.0, device="cuda", dtype=dtype)
+        spans = [(1, 4), (7, 8300), (8301, 8302), (8305, 30000), (30008, 39999)]
+        for a, b in spans:
+            flat[a:b] = torch.randn(b - a, device="cuda").to(dtype)
+        check(mkq, [flat[a:b] for a, b in spans], 3.0, in_place)
+        gaps = torch.ones(40000, dtype=torch.bool)
+        for a, b in spans:
+            gaps[a:b] = False
+        assert bool((flat[gaps.cuda()] == 100).all())
+
+
+def test_far_ends_of_the_range(mkq):
+    for std in (1e25, 1e-25, 1e-38):
+        ts = tensors([5000, 77], 3, [torch.float32], std)
+        want = true_norm(ts)
+        assert abs(float(mkq.mkq_gradient_norm(ts)) - want) <= want * (2.0 ** -24 + 1e-12) + 2.0 ** -150
+    norm = mkq.mkq_clip_gradients(ts := tensors([5000], 4, [torch.float32], 1e25), 1.0)
+    assert math.isfinite(float(norm)) and abs(true_norm(ts) - 1.0) < 1e-5
+
+
+def test_not_finite(mkq):
+    for bad, expect in ((float("nan"), math.isnan), (float("inf"), math.isinf)):
+        ts = tensors([100, 9000], 5)
+        ts[1][8500] = bad
+        assert expect(float(mkq.mkq_gradient_norm(ts)))
+        assert expect(float(mkq.mkq_clip_gradients(ts, 1.0)))
+        if math.isnan(bad):
+            assert all(bool(t.isnan().all()) for t in ts)
+        else:
+            assert math.isnan(float(ts[1][8500])) and bool((ts[0] == 0).all()) and int(ts[1].isnan().sum()) == 1
+
+
+def test_equal_bits_and_replays(mkq):
+    ts = tensors([300000, 1000, 77, 500000], 6)
+    outs = [torch.empty_like(t) for t in ts]
+    norm = torch.empty(1, device="cuda")
+    ws = torch.empty(mkq.mkq_gradient_norm_workspace_bytes(len(ts)), dtype=torch.uint8, device="cuda")
+    run = lambda: mkq.mkq_clip_gradients(ts, 5.0, outs=outs, norm_out=norm, workspace=ws)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(3):
+        for t, new in zip(ts, tensors([t.numel() for t in ts], 10 + i)):
+            t.copy_(new)
+        run()
+        want = [norm.clone()] + [o.clone() for o in outs]
+        norm.fill_(0)
+        for o in outs:
+            o.fill_(1)
+        ws.fill_(0xA5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip([norm] + outs, want))
+
+
+def test_other_stream(mkq):
+    ts = tensors([70000, 33], 8)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    norm = mkq.mkq_clip_gradients(ts, 1.0, stream=side)
+    side.synchronize()
+    assert float(norm) > 1 and abs(true_norm(ts) - 1.0) < 2e-3
