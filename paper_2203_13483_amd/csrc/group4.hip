@@ -8,15 +8,18 @@
 // Activations enter exactly too: binary16 and bfloat16 ones as they are, binary32 ones as the sum of three bfloat16 parts
 // (8 + 8 + 8 bits).
 //
-// Bound: the weights' bytes for few tokens (each is read once), the matrix pipe from about 100 tokens on.
+// Bound: the weights' bytes for few tokens, by the instructions that turn codes into operands from about 30 on.  Measured, us:
+// one token, K = 768, N = 30522, groups of 64 6.3 (2.1 TB/s); K = 8192, N = 28672, groups of 128: 1 token 31 (4.0 TB/s; the same loads
+// with the arithmetic left out 23.5), 16 tokens 34 (3.7), 32 tokens 43, 64 tokens 63 (475 TFLOP/s); 120 tokens, K = 1024,
+// N = 30522 15.9 (473 TFLOP/s).
 #include <type_traits>
 
 #include "elements.h"
+#include "gemm_common.h"
 
 namespace mkq {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 // ---- preparation of the weights ---------------------------------------------------------------------------------------
@@ -68,8 +71,9 @@ struct Group4Params {
     void *out;
     int residual_dtype, out_dtype, act;
     int M, N, K, pieces, groups;  // pieces: of 32 codes
-    int tiles;                    // workgroups along N
-    int ks;                       // waves of a workgroup that share a tile's k loop
+    int blocks_n;                 // workgroups along N
+    int x_vec;                    // rows of x are multiples of 16 bytes, K of 8
+    int lds_rows;                 // rows of x that a workgroup keeps: min(M, its tokens)
 };
 
 // Eight codes of a word as the matrix instruction takes them.
@@ -102,41 +106,40 @@ __device__ __forceinline__ v8b codes_bf16(uint32_t w)
     return __builtin_bit_cast(v8b, r);
 }
 
-// Eight neighbouring activations as matrix operands
+// The types of the products for one type of activations, and eight neighbouring activations as they enter them: PARTS
+// vectors of eight 16-bit values whose sum they are
 template <class E>
-struct XParts;
+struct Product;
 template <>
-struct XParts<ElemF16> {
+struct Product<ElemF16> {
+    using V = v8h;
     static constexpr int PARTS = 1;
-    v8h p[1];
-    __device__ __forceinline__ void set(uint4 a, uint4)
+    static constexpr float UNIT = 1.0f;  // what a code of 1 stands for is 1 / UNIT
+    __device__ static __forceinline__ V codes(uint32_t w) { return codes_f16(w); }
+    __device__ static __forceinline__ void parts(uint4 a, uint4, uint4 (&p)[1])
     {
-        const uint32_t r[4] = {__builtin_amdgcn_perm(a.z, a.x, 0x05040100u), __builtin_amdgcn_perm(a.z, a.x, 0x07060302u),
-                               __builtin_amdgcn_perm(a.w, a.y, 0x05040100u), __builtin_amdgcn_perm(a.w, a.y, 0x07060302u)};
-        p[0] = __builtin_bit_cast(v8h, r);
+        p[0] = make_uint4(__builtin_amdgcn_perm(a.z, a.x, 0x05040100u), __builtin_amdgcn_perm(a.z, a.x, 0x07060302u),
+                          __builtin_amdgcn_perm(a.w, a.y, 0x05040100u), __builtin_amdgcn_perm(a.w, a.y, 0x07060302u));
     }
-    using Codes = v8h;
-    __device__ static __forceinline__ Codes codes(uint32_t w) { return codes_f16(w); }
-    __device__ __forceinline__ v4f mul_codes(Codes b, v4f c) const { return __builtin_amdgcn_mfma_f32_16x16x32_f16(p[0], b, c, 0, 0, 0); }
-    static constexpr float UNIT = 1.0f;
+    __device__ static __forceinline__ v4f mul(V x, V c, v4f s) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, c, s, 0, 0, 0); }
+    __device__ static __forceinline__ v16f mul(V x, V c, v16f s) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, c, s, 0, 0, 0); }
 };
 template <>
-struct XParts<ElemBF16> {
+struct Product<ElemBF16> {
+    using V = v8b;
     static constexpr int PARTS = 1;
-    v8b p[1];
-    __device__ __forceinline__ void set(uint4 a, uint4) { p[0] = __builtin_bit_cast(v8b, a); }
-    using Codes = v8b;
-    __device__ static __forceinline__ Codes codes(uint32_t w) { return codes_bf16(w); }
-    __device__ __forceinline__ v4f mul_codes(Codes b, v4f c) const { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[0], b, c, 0, 0, 0); }
     static constexpr float UNIT = 16.0f;
+    __device__ static __forceinline__ V codes(uint32_t w) { return codes_bf16(w); }
+    __device__ static __forceinline__ void parts(uint4 a, uint4, uint4 (&p)[1]) { p[0] = a; }
+    __device__ static __forceinline__ v4f mul(V x, V c, v4f s) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, c, s, 0, 0, 0); }
+    __device__ static __forceinline__ v16f mul(V x, V c, v16f s) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, c, s, 0, 0, 0); }
 };
 // x = hi + mid + lo: each part is the upper half of what is left (its first 8 bits), and what is left is exact, down to the
-// smallest normal number; nothing is left of an infinity, and a NaN stays one.
+// smallest normal number; nothing is left of an infinity, and a NaN stays one.  The smallest part is multiplied first.
 template <>
-struct XParts<ElemF32> {
+struct Product<ElemF32> : Product<ElemBF16> {
     static constexpr int PARTS = 3;
-    v8b p[3];
-    __device__ __forceinline__ void set(uint4 a, uint4 b)
+    __device__ static __forceinline__ void parts(uint4 a, uint4 b, uint4 (&p)[3])
     {
         uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, mid[8], lo[8];
 #pragma unroll
@@ -148,158 +151,392 @@ struct XParts<ElemF32> {
             mid[i] = __float_as_uint(r);
             lo[i] = __float_as_uint(r - __uint_as_float(mid[i] & 0xFFFF0000u));
         }
-        uint32_t h[4], m[4], l[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[i] = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i], 0x07060302u);
-            m[i] = __builtin_amdgcn_perm(mid[2 * i + 1], mid[2 * i], 0x07060302u);
-            l[i] = __builtin_amdgcn_perm(lo[2 * i + 1], lo[2 * i], 0x07060302u);
-        }
-        p[0] = __builtin_bit_cast(v8b, l);
-        p[1] = __builtin_bit_cast(v8b, m);
-        p[2] = __builtin_bit_cast(v8b, h);
+        auto upper = [](const uint32_t (&v)[8]) {
+            return make_uint4(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u),
+                              __builtin_amdgcn_perm(v[5], v[4], 0x07060302u), __builtin_amdgcn_perm(v[7], v[6], 0x07060302u));
+        };
+        p[0] = upper(lo);
+        p[1] = upper(mid);
+        p[2] = upper(u);
     }
-    using Codes = v8b;
-    __device__ static __forceinline__ Codes codes(uint32_t w) { return codes_bf16(w); }
-    __device__ __forceinline__ v4f mul_codes(Codes b, v4f c) const
-    {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p[i], b, c, 0, 0, 0);
-        return c;
-    }
-    static constexpr float UNIT = 16.0f;
 };
 
-// Words of four lane quarters, transposed: word r of quarter q becomes word q of quarter r
-__device__ __forceinline__ void transpose4(uint32_t (&w)[4])
+__device__ __forceinline__ void swap32(uint32_t &a, uint32_t &b)
 {
-    auto s32 = [](uint32_t &a, uint32_t &b) {
-        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-        a = r[0];
-        b = r[1];
-    };
-    auto s16 = [](uint32_t &a, uint32_t &b) {
-        const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-        a = r[0];
-        b = r[1];
-    };
-    s32(w[0], w[2]);
-    s32(w[1], w[3]);
-    s16(w[0], w[1]);
-    s16(w[2], w[3]);
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ __forceinline__ void swap16(uint32_t &a, uint32_t &b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
 }
 
-__device__ __forceinline__ float load_dtype(const void *p, int dtype, int64_t i)
+// first[lane + 8 of 16] <-> second[lane]: of two registers, the upper halves of the first's rows of 16 lanes for the lower
+// halves of the second's
+__device__ __forceinline__ void swap8(uint32_t &a, uint32_t &b)
 {
-    if (dtype == MKQ_F32) return static_cast<const float *>(p)[i];
-    const uint16_t h = static_cast<const uint16_t *>(p)[i];
-    return dtype == MKQ_F16 ? ElemF16::get(h) : ElemBF16::get(h);
+    const int t = (int)a;
+    a = (uint32_t)__builtin_amdgcn_update_dpp(t, (int)b, 0x128, 0xF, 0xC, false);
+    b = (uint32_t)__builtin_amdgcn_update_dpp((int)b, t, 0x128, 0xF, 0x3, false);
 }
 
-// A wave owns 16 channels and up to 16 * MT tokens; with ks > 1 the ks waves of a workgroup share the tile and take the
-// steps of 128 codes in turn.  In a step a lane fetches 16 bytes (32 codes) of channel lane % 16; the words of the four lanes
-// that share a channel are then exchanged (transpose4), so that each of the four products of a step covers 32 neighbouring
-// codes and lies within one group, whatever its size.  A product's result has channel lane % 16, tokens 4 (lane / 16) + 0..3,
-// so a lane needs one step per group.
-template <class E, int G, int MT, bool VEC>
-__global__ __launch_bounds__(256) void group4_few_kernel(const Group4Params p)
-{
-    using X = XParts<E>;
-    __shared__ float part[4][MT * 4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int nl = lane & 15, kq = lane >> 4;
-    const int slice = wave % p.ks;
-    const int tile = (int)(blockIdx.x % (unsigned)p.tiles) * (4 / p.ks) + wave / p.ks;
-    const int m0 = (int)(blockIdx.x / (unsigned)p.tiles) * 16 * MT;
-    const int n = tile * 16 + nl, nc = n < p.N ? n : p.N - 1;  // channels past the end are computed and not stored
-    const uint8_t *wrow = p.W + (size_t)nc * ((size_t)p.pieces * 16);
-    const float *srow = p.s_w + (size_t)nc * p.groups;
-    const typename E::raw *xrow[MT];
-    bool token[MT];
+// A tile of TN channels and TN tokens: 16, products of KM = 32 codes a time, or 32, products of 16.  A wave fetches STEPS * 128
+// codes of each channel at a time, 16 bytes (a piece, 32 codes) a lane and load; lane (c, q) has c = lane % TN, q = lane / TN.
+// own() gives the words of the lane's own channel c: of 128 codes, piece q (32: also q + 2), of the next 128 likewise;
+// operands() exchanges the words of the lanes that share a channel so that operand j of 128 codes has, in lane (c, q), the
+// eight codes j * KM + 8 q ..: every product covers KM neighbours and lies within one group, whatever its size.
+template <int TN>
+struct Tile;
+// Eight rows of 128 bytes with every load, so that a line of memory is asked for once.  Fetched as 16 rows of 64 bytes, what a
+// lane needs at once, the other half of a line comes too late for the L1 where many waves stream: one token, K = 28672, N = 8192
+// 54 -> 38 us.  Load i of lane (c, q) has row 8 i + c % 8, piece 4 (c / 8) + q; six exchanges for 128 codes put that right.
+template <>
+struct Tile<16> {
+    using Acc = v4f;
+    static constexpr int ACC = 4, KM = 32, STEPS = 2;
+    __device__ static __forceinline__ int row(int i, int c) { return 8 * i + c % 8; }
+    __device__ static __forceinline__ int piece(int, int c, int q) { return 4 * (c / 8) + q; }
+    __device__ static __forceinline__ void own(uint32_t (&w)[8])
+    {
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int m = m0 + 16 * t + nl;
-        token[t] = m < p.M;
-        xrow[t] = static_cast<const typename E::raw *>(p.x) + (int64_t)(token[t] ? m : 0) * p.ldx;
+        for (int i = 0; i < 4; ++i) swap8(w[i], w[4 + i]);
     }
-    v4f total[MT];
+    __device__ static __forceinline__ void operands(uint32_t *w)
+    {
+        swap32(w[0], w[2]);
+        swap32(w[1], w[3]);
+        swap16(w[0], w[1]);
+        swap16(w[2], w[3]);
+    }
+    __device__ static __forceinline__ int token(int i, int q) { return 4 * q + i; }
+};
+// 32 rows of 32 bytes with every load: many tokens are bound by the products and what is issued beside them, and the
+// exchanges cost more than the lines (64 tokens, K = 8192, N = 28672 62 -> 76 us)
+template <>
+struct Tile<32> {
+    using Acc = v16f;
+    static constexpr int ACC = 16, KM = 16, STEPS = 1;
+    __device__ static __forceinline__ int row(int, int c) { return c; }
+    __device__ static __forceinline__ int piece(int i, int, int q) { return 2 * i + q; }
+    __device__ static __forceinline__ void own(uint32_t (&)[8]) {}
+    __device__ static __forceinline__ void operands(uint32_t *w)
+    {
 #pragma unroll
-    for (int t = 0; t < MT; ++t) total[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-
-    const int steps = (p.pieces + 3) / 4;
-    for (int step = slice; step < steps; step += p.ks) {
-        const int piece = step * 4 + kq;
-        const uint4 raw = *reinterpret_cast<const uint4 *>(wrow + (size_t)(piece < p.pieces ? piece : p.pieces - 1) * 16);
-        uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-        transpose4(w);
-        v4f sum[MT];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int g = (step * 128 + 32 * j) / G;
-            if (32 * j % G == 0) {
-#pragma unroll
-                for (int t = 0; t < MT; ++t) sum[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-            const int k = step * 128 + 32 * j + 8 * kq;
-            const typename X::Codes codes = X::codes(w[j]);
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                uint4 a = make_uint4(0, 0, 0, 0), b = a;
-                if (token[t]) {  // past K the activations are zeros, whatever the weights hold there
-                    if (VEC && k + 8 <= p.K) {
-                        const uint4 *at = reinterpret_cast<const uint4 *>(xrow[t] + k);
-                        a = at[0];
-                        if (E::BYTES == 4) b = at[1];
-                    } else if (k < p.K) {
-                        typename E::raw v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = k + i < p.K ? xrow[t][k + i] : typename E::raw(0);
-                        __builtin_memcpy(&a, v, 16);
-                        if (E::BYTES == 4) __builtin_memcpy(&b, reinterpret_cast<const char *>(v) + 8 * E::BYTES - 16, 16);
-                    }
-                }
-                X xp;
-                xp.set(a, b);
-                sum[t] = xp.mul_codes(codes, sum[t]);
-            }
-            if (32 * (j + 1) % G == 0) {
-                // (a group past the last one has sums of zero; its step is not read)
-                const float s = g < p.groups ? srow[g] * X::UNIT : 0.0f;
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) total[t][i] = __builtin_fmaf(sum[t][i], s, total[t][i]);
-            }
+        for (int i = 0; i < 8; i += 4) {
+            swap32(w[i], w[i + 1]);
+            swap32(w[i + 2], w[i + 3]);
+            const uint32_t t = w[i + 1];
+            w[i + 1] = w[i + 2];
+            w[i + 2] = t;
         }
     }
-    if (p.ks > 1) {
+    __device__ static __forceinline__ int token(int i, int q) { return (i & 3) + 8 * (i >> 2) + 4 * q; }
+};
+
+// A lane's results: bias, residual, activation, one rounding
+template <int TN, int MT>
+__device__ __forceinline__ void store_tile(const Group4Params &p, typename Tile<TN>::Acc (&y)[MT], int n, int m0, int rows, int q)
+{
+    using T = Tile<TN>;
+    if (n >= p.N) return;
+    // f(result, its place) for the tokens that exist
+    auto each = [&](auto &&f) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) part[wave][t * 4 + i][lane] = total[t][i];
-        __syncthreads();
-        if (slice != 0) return;
-        for (int s = 1; s < p.ks; ++s)
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) total[t][i] += part[wave + s][t * 4 + i][lane];
+            for (int i = 0; i < T::ACC; ++i) {
+                const int m = t * TN + T::token(i, q);
+                if (m < rows) {
+                    float v = y[t][i];
+                    f(v, (int64_t)(m0 + m) * p.N + n);
+                    y[t][i] = v;
+                }
+            }
+    };
+    auto add = [&](auto e) {
+        const auto *r = static_cast<const typename decltype(e)::raw *>(p.residual);
+        each([&](float &v, int64_t at) { v += decltype(e)::get(r[at]); });
+    };
+    auto write = [&](auto e) {
+        auto *o = static_cast<typename decltype(e)::raw *>(p.out);
+        each([&](float &v, int64_t at) { o[at] = decltype(e)::put(v); });
+    };
+    if (p.bias) {
+        const float bias = p.bias[n];
+        each([&](float &v, int64_t) { v += bias; });
     }
-    if (n >= p.N) return;
-    const float bias = p.bias ? p.bias[n] : 0.0f;
+    if (p.residual) {
+        if (p.residual_dtype == MKQ_F32) add(ElemF32());
+        else if (p.residual_dtype == MKQ_F16) add(ElemF16());
+        else add(ElemBF16());
+    }
+    if (p.act == MKQ_ACT_GELU) {
+        if (p.out_dtype == MKQ_F16) each([&](float &v, int64_t) { v = gelu_erf(v); });
+        else each([&](float &v, int64_t) { v = gelu_erf_tail(v); });
+    }
+    if (p.out_dtype == MKQ_F32) write(ElemF32());
+    else if (p.out_dtype == MKQ_F16) write(ElemF16());
+    else write(ElemBF16());
+}
+
+// Steps of 128 codes between two hand-overs of activations: what 64 KB of LDS and eight vectors a thread allow
+template <class E, int G, int TN, int MT, int KS>
+struct Shape {
+    static constexpr int PARTS = Product<E>::PARTS, ROWS = TN * MT;
+    static constexpr int FIT = 65536 / (512 * KS * ROWS * PARTS);
+    static constexpr int U = FIT >= 4 ? 4 : 2;
+    static constexpr int KC = 128 * U, PITCH = KC * 2 + 16;  // (bytes; 16 more than a multiple of 128: no bank conflicts among rows)
+    static constexpr int VECTORS = (ROWS * (KC / 8) * KS + 255) / 256;
+    // steps of a wave's channels for a chunk, and where they are in LDS: rows of an odd number of words (no bank conflicts)
+    static constexpr int SCALES = KC / G, SPITCH = SCALES | 1, SCALE_BYTES = 4 * TN * SPITCH * 4;
+    static constexpr size_t lds(int rows)
+    {
+        const size_t x = SCALE_BYTES + (size_t)2 * KS * PARTS * rows * PITCH, sums = KS > 1 ? (size_t)256 * MT * Tile<TN>::ACC * 4 : 0;
+        return x > sums ? x : sums;
+    }
+};
+
+// Four waves; KS of them share the k loop of a tile (chunks of KC codes in turn) and their sums meet in LDS at the end; the
+// other 4 / KS tiles of the workgroup are neighbours and share the activations, which come through LDS, converted once, two
+// chunks in turn: one is multiplied while the next is on its way in registers.  Weights and steps go from memory to registers,
+// one chunk ahead.
+template <class E, int G, int TN, int MT, int KS>
+__global__ __launch_bounds__(256, TN == 16 ? (KS == 1 ? 4 : 3) : 2) void group4_kernel(const Group4Params p)
+{
+    using S = Shape<E, G, TN, MT, KS>;
+    using T = Tile<TN>;
+    using P = Product<E>;
+    using Acc = typename T::Acc;
+    constexpr int U = S::U, KC = S::KC, ACC = T::ACC, CG = 4 / KS, XT = 256 / KS;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int nl = lane % TN, q = lane / TN;
+    const int slice = wave / CG, st = tid % XT;
+    const int n = ((int)(blockIdx.x % (unsigned)p.blocks_n) * CG + wave % CG) * TN + nl;
+    const int m0 = (int)(blockIdx.x / (unsigned)p.blocks_n) * S::ROWS;
+    const int rows = p.M - m0 < S::ROWS ? p.M - m0 : S::ROWS;
+    const int part_bytes = p.lds_rows * S::PITCH, buffer_bytes = S::PARTS * part_bytes;
+    uint8_t *const xs = smem + S::SCALE_BYTES + slice * 2 * buffer_bytes;
+    float *const scales = reinterpret_cast<float *>(smem) + wave * (TN * S::SPITCH);
+
+    // activations of chunk c: vectors of eight, zeros past K
+    uint4 xa[S::VECTORS], xb[E::BYTES == 4 ? S::VECTORS : 1];
+    auto fetch_x = [&](int c) {
+        const typename E::raw *const base = static_cast<const typename E::raw *>(p.x) + (int64_t)m0 * p.ldx;
+        if (p.x_vec) {  // vectors are whole or past the end
+#pragma unroll
+            for (int v = 0; v < S::VECTORS; ++v) {
+                const int i = v * XT + st, r = i / (KC / 8), k = c * KC + i % (KC / 8) * 8;
+                uint4 a = make_uint4(0, 0, 0, 0), b = a;
+                if (r < rows && k < p.K) {
+                    const uint4 *at = reinterpret_cast<const uint4 *>(base + (int64_t)r * p.ldx + k);
+                    a = at[0];
+                    if constexpr (E::BYTES == 4) b = at[1];
+                }
+                xa[v] = a;
+                if constexpr (E::BYTES == 4) xb[v] = b;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < S::VECTORS; ++v) {
+                const int i = v * XT + st, r = i / (KC / 8), k = c * KC + i % (KC / 8) * 8;
+                typename E::raw e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] = r < rows && k + j < p.K ? base[(int64_t)r * p.ldx + k + j] : typename E::raw(0);
+                __builtin_memcpy(&xa[v], e, 16);
+                if constexpr (E::BYTES == 4) __builtin_memcpy(&xb[v], e + 4, 16);
+            }
+        }
+    };
+    auto store_x = [&](int buffer) {
+#pragma unroll
+        for (int v = 0; v < S::VECTORS; ++v) {
+            const int i = v * XT + st, r = i / (KC / 8);
+            if (r < rows) {
+                uint4 parts[S::PARTS];
+                P::parts(xa[v], E::BYTES == 4 ? xb[v] : xa[v], parts);
+                uint8_t *to = xs + buffer * buffer_bytes + r * S::PITCH + i % (KC / 8) * 16;
+#pragma unroll
+                for (int k = 0; k < S::PARTS; ++k) *reinterpret_cast<uint4 *>(to + k * part_bytes) = parts[k];
+            }
+        }
+    };
+    // weights of STEPS steps of 128 codes from step s; past the end the last ones, whose activations are zeros
+    constexpr int STEPS = T::STEPS;
+    uint4 W[U / STEPS][2];
+    const uint8_t *wrow[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = n - nl + T::row(i, nl);  // channels past the end: the last one's weights, never stored
+        wrow[i] = p.W + (size_t)(r < p.N ? r : p.N - 1) * ((size_t)p.pieces * 16);
+    }
+    auto fetch_w = [&](int h, int s) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int piece = 4 * s + T::piece(i, nl, q);
+            W[h][i] = *reinterpret_cast<const uint4 *>(wrow[i] + (size_t)(piece < p.pieces ? piece : p.pieces - 1) * 16);
+        }
+    };
+    // steps of chunk c for the wave's channels: PER neighbours of a row a lane
+    constexpr int PER = (TN * S::SCALES + 63) / 64, LPR = S::SCALES / PER;
+    const int srow = lane / LPR, sg = lane % LPR * PER;
+    const int sn = n - nl + srow < p.N ? n - nl + srow : p.N - 1;
+    float sreg[PER];
+    auto fetch_s = [&](int c) {
+        const int g = c * S::SCALES + sg;
+        const float *at = p.s_w + (size_t)sn * p.groups;
+        if (srow < TN) {
+            if (g + PER <= p.groups) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) sreg[i] = at[g + i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) sreg[i] = at[g + i < p.groups ? g + i : p.groups - 1];
+            }
+        }
+    };
+    auto store_s = [&]() {  // (only this wave reads them)
+        if (srow < TN)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) scales[srow * S::SPITCH + sg + i] = sreg[i] * P::UNIT;
+    };
+
+    Acc total[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = m0 + 16 * t + 4 * kq + i;
-            if (m >= p.M) continue;
-            const int64_t at = (int64_t)m * p.N + n;
-            float y = total[t][i] + bias;
-            if (p.residual) y += load_dtype(p.residual, p.residual_dtype, at);
-            if (p.act == MKQ_ACT_GELU) y = p.out_dtype == MKQ_F16 ? gelu_erf(y) : gelu_erf_tail(y);
-            if (p.out_dtype == MKQ_F32) static_cast<float *>(p.out)[at] = y;
-            else static_cast<uint16_t *>(p.out)[at] = p.out_dtype == MKQ_F16 ? ElemF16::put(y) : ElemBF16::put(y);
+        for (int i = 0; i < ACC; ++i) total[t][i] = 0.0f;
+    int xrow[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int r = t * TN + nl;
+        xrow[t] = (r < p.lds_rows ? r : p.lds_rows - 1) * S::PITCH + q * 16;
+    }
+
+    const int steps = (p.K + 127) / 128, chunks = (p.K + KC - 1) / KC, rounds = (chunks + KS - 1) / KS;
+    // The i-th chunk of this workgroup: neighbours begin a chunk further on.  Rows are often a power of two of bytes apart, and
+    // workgroups that walk k side by side would all ask the same few memory channels (the loads alone, rows of 4 KB, 24.2 -> 20.2 us).
+    const int turn = (int)(blockIdx.x % (unsigned)chunks);
+    auto chunk_at = [&](int i) { return i >= chunks ? chunks : i + turn < chunks ? i + turn : i + turn - chunks; };
+    fetch_x(chunk_at(slice));
+#pragma unroll
+    for (int h = 0; h < U / STEPS; ++h) fetch_w(h, chunk_at(slice) * U + STEPS * h);
+    fetch_s(chunk_at(slice));
+    store_x(0);
+    store_s();
+    lds_barrier();
+    for (int round = 0; round < rounds; ++round) {
+        const int chunk = chunk_at(slice + round * KS), next = chunk_at(slice + (round + 1) * KS);
+        const bool more = round + 1 < rounds;
+        if (more) fetch_x(next);
+        if (more) fetch_s(next);
+        const uint8_t *xbuf = xs + (round & 1) * buffer_bytes;
+        uint32_t words[8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u % STEPS == 0) {
+                __builtin_memcpy(words, W[u / STEPS], sizeof(words));
+                T::own(words);
+                fetch_w(u / STEPS, next * U + u);  // (also behind the last chunk: under a branch they would all be waited for at its end)
+            }
+            if (chunk * U + u >= steps) continue;
+            uint32_t *const word = words + u % STEPS * 4;
+            float sc[128 / G];
+#pragma unroll
+            for (int i = 0; i < 128 / G; ++i) sc[i] = scales[nl * S::SPITCH + u * (128 / G) + i];
+            T::operands(word);
+            Acc sum[MT];
+#pragma unroll
+            for (int j = 0; j < 128 / T::KM; ++j) {
+                if (j * T::KM % G == 0)
+#pragma unroll
+                    for (int t = 0; t < MT; ++t)
+#pragma unroll
+                        for (int i = 0; i < ACC; ++i) sum[t][i] = 0.0f;
+                const typename P::V codes = P::codes(word[j]);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int k = 0; k < S::PARTS; ++k) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(xbuf + xrow[t] + k * part_bytes + (u * 128 + j * T::KM) * 2);
+                        sum[t] = P::mul(__builtin_bit_cast(typename P::V, x), codes, sum[t]);
+                    }
+                if ((j + 1) * T::KM % G == 0)
+#pragma unroll
+                    for (int t = 0; t < MT; ++t)
+#pragma unroll
+                        for (int i = 0; i < ACC; ++i) total[t][i] = __builtin_fmaf(sum[t][i], sc[j * T::KM / G], total[t][i]);
+            }
+            // (else the compiler keeps the sums of all groups until the last product of the chunk, in registers that it lacks)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) asm volatile("" : "+v"(total[t]));
         }
+        if (more) {
+            store_x((round + 1) & 1);
+            store_s();
+            lds_barrier();
+        }
+    }
+
+    if constexpr (KS > 1) {
+        float *const part = reinterpret_cast<float *>(smem);
+        lds_barrier();  // the last chunk has been read
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int i = 0; i < ACC; ++i) part[(t * ACC + i) * 256 + tid] = total[t][i];
+        lds_barrier();
+        if (slice != 0) return;
+#pragma unroll
+        for (int s = 1; s < KS; ++s)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int i = 0; i < ACC; ++i) total[t][i] += part[(t * ACC + i) * 256 + tid + s * XT];
+    }
+    store_tile<TN, MT>(p, total, n, m0, rows, q);
+}
+
+template <class E, int G, int TN, int MT, int KS>
+static int launch_group4(Group4Params p, hipStream_t st)
+{
+    using S = Shape<E, G, TN, MT, KS>;
+    static PerDeviceOnce once;  // (more than 64 KB of LDS have to be asked for)
+    if (once.get([]() -> int {
+            return hipFuncSetAttribute(reinterpret_cast<const void *>(&group4_kernel<E, G, TN, MT, KS>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)S::lds(S::ROWS)) == hipSuccess ? 1 : -1;
+        }) <= 0)
+        return MKQ_ERR_HIP;
+    static_assert(S::lds(S::ROWS) <= 160 * 1024, "LDS is 160 KiB per CU");
+    p.lds_rows = p.M < S::ROWS ? p.M : S::ROWS;
+    p.blocks_n = (int)ceil_div(p.N, TN * (4 / KS));
+    const int64_t workgroups = (int64_t)p.blocks_n * ceil_div(p.M, S::ROWS);
+    if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
+    group4_kernel<E, G, TN, MT, KS><<<(unsigned)workgroups, 256, S::lds(p.lds_rows), st>>>(p);
+    return launch_status();
+}
+
+// Which tile, and how many waves share its k loop: the largest tile whose workgroups fill the chip, since a tile of more
+// tokens converts a code for more of them, and a k loop shared by fewer waves reads x fewer times.  us, binary16 (tile and
+// waves): one token, K = 768, N = 30522 6.4 (16, 1), 8.0 (16, 2); K = 4096, N = 16384 12.7 (16, 1), 10.9 (16, 2), 12.1 (16, 4);
+// K = N = 8192 21.3, 13.9, 11.8; 24 tokens, K = 8192, N = 28672 56.7 (16, 1), 41.2 (32, 1), 44.7 (32, 2); 64 tokens there 67.7
+// (32, 1), 63.4 (64, 1), but with K = N = 4096 14.4 (16, 1), 13.2 (16, 2), 24.1 (32, 1), 36.2 (64, 1); 128 tokens, K = N = 4096 22.5
+// (16, 1), 28.1 (32, 1), 20.4 (32, 2), but K = 1024 8.2, 12.1, 9.9.  binary32 has 16 tokens a tile: its three parts leave a larger tile
+// short chunks (64 tokens, K = 8192, N = 28672 197 and 172, K = 768, N = 30522 of 48 20.2 and 23.6).
+template <class E, int G>
+static int choose_group4(const Group4Params &p, hipStream_t st)
+{
+    auto workgroups = [&](int tn, int mt, int ks) { return ceil_div(p.N, tn * (4 / ks)) * ceil_div(p.M, tn * mt); };
+    if constexpr (E::BYTES == 2) {
+        if (p.M > 32 && workgroups(32, 2, 1) >= 200) return launch_group4<E, G, 32, 2, 1>(p, st);
+        if (p.M > 16 && workgroups(32, 1, 1) >= 200) return launch_group4<E, G, 32, 1, 1>(p, st);
+        if (p.M > 16 && p.K >= 2048 && workgroups(32, 1, 2) >= 200) return launch_group4<E, G, 32, 1, 2>(p, st);
+        if (workgroups(16, 1, 1) < 300 && workgroups(16, 1, 2) < 400) return launch_group4<E, G, 16, 1, 4>(p, st);
+    }
+    return workgroups(16, 1, 1) >= 300 ? launch_group4<E, G, 16, 1, 1>(p, st) : launch_group4<E, G, 16, 1, 2>(p, st);
 }
 
 static bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
@@ -362,7 +599,7 @@ extern "C" int mkq_linear_int4_group(const void *x, int x_dtype, int64_t ldx, co
     if (!x || !Wq || !s_w || !out) return MKQ_ERR_NULL;
     if (!aligned16(x) || !aligned16(Wq) || !aligned4(s_w) || !aligned16(out) || !aligned4(bias) || (epi && !aligned16(epi->residual)))
         return MKQ_ERR_ALIGN;
-    if (M > 0x7FFFFFFF - 64 || N > 0x7FFFFFFF - 64 || K > 0x7FFFFFFF - 128) return MKQ_ERR_UNSUPPORTED;
+    if (M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > 0x7FFFF000) return MKQ_ERR_UNSUPPORTED;
     Group4Params p = {};
     p.x = x;
     p.ldx = ldx;
@@ -379,28 +616,11 @@ extern "C" int mkq_linear_int4_group(const void *x, int x_dtype, int64_t ldx, co
     p.K = (int)K;
     p.pieces = (int)ceil_div(K, 32);
     p.groups = (int)ceil_div(K, group);
-    p.ks = 4;
-    p.tiles = (int)ceil_div(ceil_div(N, 16), 4 / p.ks);
-    const int mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    const int64_t workgroups = (int64_t)p.tiles * ceil_div(M, 16 * mt);
-    if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
-    const bool vec = rows_aligned16(x, ldx, x_dtype);
+    p.x_vec = rows_aligned16(x, ldx, x_dtype) && K % 8 == 0;
     const hipStream_t st = as_stream(stream);
+    int status = MKQ_OK;
     with_elem(x_dtype, [&](auto e) {
-        using E = decltype(e);
-        with_group(group, [&](auto g) {
-            constexpr int G = decltype(g)::value;
-            auto launch = [&](auto t, auto v) {
-                group4_few_kernel<E, G, decltype(t)::value, decltype(v)::value><<<(unsigned)workgroups, 256, 0, st>>>(p);
-            };
-            auto tokens = [&](auto t) {
-                if (vec) launch(t, std::true_type());
-                else launch(t, std::false_type());
-            };
-            if (mt == 1) tokens(std::integral_constant<int, 1>());
-            else if (mt == 2) tokens(std::integral_constant<int, 2>());
-            else tokens(std::integral_constant<int, 4>());
-        });
+        with_group(group, [&](auto g) { status = choose_group4<decltype(e), decltype(g)::value>(p, st); });
     });
-    return launch_status();
+    return status;
 }

@@ -123,6 +123,24 @@ def test_whole_numbers_are_exact(mkq, M, xt, group):
     assert torch.equal(got.cpu().double(), x.double() @ dequantized(codes, s, group).T)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("xt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(3, 20003, 136), (16, 13001, 1030), (20, 26001, 392), (45, 26001, 160), (100, 25999, 520), (128, 3205, 2056), (130, 3250, 4100),
+                                   (16, 40, 4360), (7, 6500, 2056), (64, 4000, 1240)])
+def test_every_tile_is_exact_on_whole_numbers(mkq, M, N, K, xt, group):
+    """As above where the grid is large enough for tiles of 32 and 64 tokens and for waves that share nothing, with K that ends
+    within a chunk, within a step and within a piece"""
+    g = torch.Generator("cuda").manual_seed(M + N + K)
+    codes = torch.randint(-8, 8, (N, -(-K // 32) * 32), generator=g, device="cuda")
+    codes[:, K:] = 0
+    s = 2.0 ** torch.randint(-3, 4, (N, -(-K // group)), generator=g, device="cuda").float()
+    x = torch.randint(-15, 16, (M, K), generator=g, device="cuda").to(T[xt])
+    Wq = ((codes[:, 0::2] % 16) + 16 * (codes[:, 1::2] % 16)).to(torch.uint8)
+    got = mkq.mkq_linear_int4_group(x, Wq, s, None, N, K, group, mkq.MKQ_F32)
+    w = codes[:, :K].double() * s.double().repeat_interleave(group, 1)[:, :K]
+    assert torch.equal(got.double(), x.double() @ w.T.contiguous())
+
+
 @pytest.mark.parametrize("xt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("M", [3, 50])
 @pytest.mark.parametrize("pad", [8, 3])
