@@ -3,7 +3,9 @@
 //     out[i,:] = scale * table[t_i,:]              dT[v,:] = scale * sum_{i: t_i = v} dy[i,:]
 //
 // All are bound by bytes: the rows read and written, and for the gradient the whole of dT, whose rows without a token are
-// zeros.  A lookup is one multiplication in binary32 and one rounding per value.
+// zeros.  A lookup is one multiplication in binary32 and one rounding per value.  Gradients, us: 4096 binary16 tokens of 768 into
+// binary32 [30522, 768] 28 (17 sorting beside the zeros, 5 sums, 6 joining), 65536 bfloat16 tokens of 1024 into [30522, 1024] 103 (44
+// sorting beside the zeros, 49 sums: 4.6 TB/s, 8 joining).
 #include "elements.h"
 
 namespace mkq {
@@ -91,11 +93,52 @@ __global__ __launch_bounds__(256) void lookup_kernel(const LookupParams p)
     }
 }
 
+// ---- gradient: zeros ------------------------------------------------------------------------------------------------------
+// The rows without a token take most of the bytes of a usual gradient, sorting the tokens is bound by latency: the launches
+// that sort fill the table with zeros as well, each a share of it in workgroups behind the sorting ones.
+struct ZeroParams {
+    void *grad;
+    int64_t ld, rows_from, rows_to;  // this launch's share
+    int D, bytes, vec;               // of a value; vec: rows are multiples of 16 bytes
+    unsigned first;                  // workgroup
+};
+
+__device__ __forceinline__ void zero_rows(const ZeroParams &z)
+{
+    const int64_t threads = (int64_t)(gridDim.x - z.first) * blockDim.x, t = (int64_t)(blockIdx.x - z.first) * blockDim.x + threadIdx.x;
+    uint8_t *const base = static_cast<uint8_t *>(z.grad) + z.rows_from * z.ld * z.bytes;
+    const int64_t rows = z.rows_to - z.rows_from;
+    if (z.ld == z.D && z.vec) {
+        const int64_t total = rows * z.D * z.bytes / 16;
+        for (int64_t i = t; i < total; i += threads) reinterpret_cast<uint4 *>(base)[i] = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const int per = z.vec ? 16 / z.bytes : 1, units = (z.D + per - 1) / per;
+    for (int64_t i = t; i < rows * units; i += threads) {
+        const int64_t row = i / units;
+        const int d = (int)(i - row * units) * per;
+        uint8_t *at = base + (row * z.ld + d) * z.bytes;
+        if (z.vec && d + per <= z.D) {
+            *reinterpret_cast<uint4 *>(at) = make_uint4(0, 0, 0, 0);
+        } else {
+            for (int e = 0; e < per && d + e < z.D; ++e) {
+                if (z.bytes == 4) reinterpret_cast<uint32_t *>(at)[e] = 0;
+                else reinterpret_cast<uint16_t *>(at)[e] = 0;
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void zero_rows_kernel(const ZeroParams z) { zero_rows(z); }
+
 // ---- gradient: sorting the tokens ---------------------------------------------------------------------------------------
-// Positions are put in the order of their tokens by a stable radix sort (least significant digit first, up to nine bits a
-// pass), so equal tokens keep the order of the batch and a row's sum does not depend on how the work fell.  Tokens that
-// count for nothing (the padding token, ids outside the table) get the key V, behind all others.
-constexpr int SORT_BINS = 512, SORT_TILE = 1024, SORT_BLOCKS = 256;
+// Positions are put in the order of their tokens, equal tokens in the order of the batch, so a row's sum does not depend on how
+// the work fell.  Tokens that count for nothing (the padding token, ids outside the table) get the key V, behind all others.
+// Short batches: a position's place is the number of positions before it, counted directly; longer ones: a stable radix sort
+// (least significant digit first, up to nine bits a pass).  A gradient of V = 30522, D = 768, us: 12000 tokens 39.6 counted directly, 16384
+// 56.8, sorted by digits 51.7.
+constexpr int SORT_BINS = 512, SORT_THREADS = 1024, SORT_WAVES = 16, SORT_ROUNDS = 2, SORT_TILE = SORT_THREADS * SORT_ROUNDS, SORT_BLOCKS = 256;
+constexpr int RANK_MAX = 12288, RANK_KEYS = 64, RANK_THREADS = 1024;
 
 struct SortParams {
     const void *tokens;
@@ -106,6 +149,7 @@ struct SortParams {
     const uint32_t *keys_in, *order_in;  // null in the first pass: keys come from the tokens
     uint32_t *keys_out, *order_out;
     uint32_t *counts;  // [blocks][SORT_BINS]
+    ZeroParams zero;
 };
 
 template <class I, bool FIRST>
@@ -116,67 +160,150 @@ __device__ __forceinline__ uint32_t sort_key(const SortParams &p, int i)
     return t >= 0 && t < (int64_t)p.V && t != p.padding ? (uint32_t)t : p.V;
 }
 
-template <class I, bool FIRST>
-__global__ __launch_bounds__(256) void sort_count_kernel(const SortParams p)
+// A lane per position, 64 of them a workgroup, whose 16 waves share all M keys: two operations for a pair.  Keys behind a
+// workgroup's own count if they are smaller, keys before it also if they are equal.
+template <class I>
+__global__ __launch_bounds__(RANK_THREADS) void rank_kernel(const SortParams p)
 {
-    __shared__ uint32_t bins[SORT_BINS];
-    for (int b = threadIdx.x; b < SORT_BINS; b += 256) bins[b] = 0;
+    if (blockIdx.x >= p.zero.first) {
+        zero_rows(p.zero);
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) uint32_t keys[RANK_MAX];
+    __shared__ uint32_t part[RANK_THREADS / 64][RANK_KEYS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int groups = (p.M + 63) / 64, own = blockIdx.x;
+    for (int i = tid; i < groups * 64; i += RANK_THREADS) keys[i] = i < p.M ? sort_key<I, true>(p, i) : 0xFFFFFFFFu;
     __syncthreads();
-    const uint32_t mask = (1u << p.bits) - 1;
-    const int64_t from = (int64_t)blockIdx.x * p.per_block;
-    const int to = (int)(from + p.per_block < p.M ? from + p.per_block : p.M);
-    for (int i = (int)from + threadIdx.x; i < to; i += 256) atomicAdd(&bins[(sort_key<I, FIRST>(p, i) >> p.shift) & mask], 1u);
-    __syncthreads();
-    for (int b = threadIdx.x; b < SORT_BINS; b += 256) p.counts[blockIdx.x * SORT_BINS + b] = bins[b];
-}
-
-// A workgroup finds where its share of every digit begins (all counts of smaller digits, and those of the digit in the
-// workgroups before), then places its positions tile by tile.  Within a tile every wave has 256 neighbours: a position's
-// place is the digit's start, plus the counts of the waves before, plus the lanes before it with the same digit (ballots).
-template <class I, bool FIRST>
-__global__ __launch_bounds__(256) void sort_place_kernel(const SortParams p)
-{
-    __shared__ uint32_t start[SORT_BINS], count[4][SORT_BINS], part[256];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t mask = (1u << p.bits) - 1;
-    uint32_t before[2] = {0, 0}, all[2] = {0, 0};  // of digits 2 tid, 2 tid + 1
-    for (int b = 0; b < p.blocks; ++b) {
-        const uint2 c = *reinterpret_cast<const uint2 *>(p.counts + b * SORT_BINS + 2 * tid);
-        all[0] += c.x;
-        all[1] += c.y;
-        if (b < (int)blockIdx.x) {
-            before[0] += c.x;
-            before[1] += c.y;
+    const uint32_t key = keys[own * 64 + lane];
+    uint32_t count = 0;
+    for (int g = wave; g < groups; g += RANK_THREADS / 64) {
+        const uint4 *at = reinterpret_cast<const uint4 *>(keys + g * 64);
+        if (g == own) {
+            for (int j = 0; j < 64; ++j) {
+                const uint32_t k = keys[g * 64 + j];
+                count += k < key || (k == key && j < lane);
+            }
+        } else {
+            const uint32_t limit = g < own ? key + 1 : key;  // (keys are at most V < 2^31, but for the places behind M, which nobody asks for)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const uint4 k = at[j];
+                count += k.x < limit;
+                count += k.y < limit;
+                count += k.z < limit;
+                count += k.w < limit;
+            }
         }
     }
-    part[tid] = all[0] + all[1];
+    part[wave][lane] = count;
     __syncthreads();
-    for (int off = 1; off < 256; off <<= 1) {  // inclusive sums over the threads
-        const uint32_t v = tid >= off ? part[tid - off] : 0;
-        __syncthreads();
-        part[tid] += v;
-        __syncthreads();
-    }
-    const uint32_t base = part[tid] - all[0] - all[1];
-    start[2 * tid] = base + before[0];
-    start[2 * tid + 1] = base + all[0] + before[1];
+    if (wave != 0 || own * 64 + lane >= p.M) return;
+#pragma unroll
+    for (int w = 1; w < RANK_THREADS / 64; ++w) count += part[w][lane];
+    p.keys_out[count] = key;
+    p.order_out[count] = (uint32_t)(own * 64 + lane);
+}
 
+template <class I, bool FIRST>
+__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(const SortParams p)
+{
+    if (blockIdx.x >= p.zero.first) {
+        zero_rows(p.zero);
+        return;
+    }
+    __shared__ uint32_t bins[SORT_BINS];
+    if (threadIdx.x < SORT_BINS) bins[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t mask = (1u << p.bits) - 1;
     const int64_t from = (int64_t)blockIdx.x * p.per_block;
     const int to = (int)(from + p.per_block < p.M ? from + p.per_block : p.M);
     for (int64_t tile = from; tile < to; tile += SORT_TILE) {
-        for (int b = tid; b < 4 * SORT_BINS; b += 256) count[b / SORT_BINS][b % SORT_BINS] = 0;
-        __syncthreads();
-        uint32_t key[4], ord[4], rank[4];
-        bool in[4];
+        uint32_t key[SORT_ROUNDS];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t i = tile + wave * 256 + r * 64 + lane;
-            in[r] = i < to;
-            key[r] = in[r] ? sort_key<I, FIRST>(p, (int)i) : 0;
-            ord[r] = FIRST ? (uint32_t)i : in[r] ? p.order_in[i] : 0;
+        for (int r = 0; r < SORT_ROUNDS; ++r) {
+            const int64_t i = tile + r * SORT_THREADS + threadIdx.x;
+            key[r] = i < to ? sort_key<I, FIRST>(p, (int)i) : 0;
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < SORT_ROUNDS; ++r)
+            if (tile + r * SORT_THREADS + threadIdx.x < to) atomicAdd(&bins[(key[r] >> p.shift) & mask], 1u);
+    }
+    __syncthreads();
+    if (threadIdx.x < SORT_BINS) p.counts[blockIdx.x * SORT_BINS + threadIdx.x] = bins[threadIdx.x];
+}
+
+// A workgroup finds where its share of every digit begins (all counts of smaller digits, and those of the digit in the
+// workgroups before), then places its positions tile by tile.  Within a tile a wave's positions are neighbours: a position's
+// place is the digit's start, plus the counts of the waves before, plus the lanes before it with the same digit (ballots).
+// Few large workgroups: each reads all workgroups' counts, and 64 of them with 1024 positions each took 22 us for 65536 positions.
+template <class I, bool FIRST>
+__global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(const SortParams p)
+{
+    if (blockIdx.x >= p.zero.first) {
+        zero_rows(p.zero);
+        return;
+    }
+    __shared__ uint32_t start[SORT_BINS], count[SORT_WAVES][SORT_BINS], part[2][SORT_BINS], sums[SORT_BINS / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t mask = (1u << p.bits) - 1;
+    const int64_t from = (int64_t)blockIdx.x * p.per_block;
+    const int to = (int)(from + p.per_block < p.M ? from + p.per_block : p.M);
+    uint32_t key[SORT_ROUNDS], ord[SORT_ROUNDS];
+    auto fetch = [&](int64_t tile) {
+#pragma unroll
+        for (int r = 0; r < SORT_ROUNDS; ++r) {
+            const int64_t i = tile + (wave * SORT_ROUNDS + r) * 64 + lane;
+            key[r] = i < to ? sort_key<I, FIRST>(p, (int)i) : 0;
+            ord[r] = FIRST ? (uint32_t)i : i < to ? p.order_in[i] : 0;
+        }
+    };
+    fetch(from);
+    {
+        const int digit = tid % SORT_BINS, half = tid / SORT_BINS;  // (a half of the threads has every other workgroup's counts)
+        uint32_t before = 0, all = 0;
+        for (int b = half; b < p.blocks; b += 32) {
+            uint32_t c[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) c[i] = p.counts[(b + 2 * i < p.blocks ? b + 2 * i : b) * SORT_BINS + digit];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (b + 2 * i >= p.blocks) break;
+                all += c[i];
+                if (b + 2 * i < (int)blockIdx.x) before += c[i];
+            }
+        }
+        if (half) {
+            part[0][digit] = before;
+            part[1][digit] = all;
+        }
+        __syncthreads();
+        uint32_t upto = 0;
+        if (!half) {  // sums over the digits: within a wave, then over the waves before
+            before += part[0][digit];
+            all += part[1][digit];
+            upto = all;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const uint32_t v = __shfl_up(upto, off, 64);
+                if (lane >= off) upto += v;
+            }
+            if (lane == 63) sums[wave] = upto;
+        }
+        __syncthreads();
+        if (!half) {
+            for (int w = 0; w < wave; ++w) upto += sums[w];
+            start[digit] = upto - all + before;
+        }
+    }
+    for (int64_t tile = from; tile < to; tile += SORT_TILE) {
+        for (int b = tid; b < SORT_WAVES * SORT_BINS; b += SORT_THREADS) count[b / SORT_BINS][b % SORT_BINS] = 0;
+        __syncthreads();
+        uint32_t rank[SORT_ROUNDS];
+        bool in[SORT_ROUNDS];
+#pragma unroll
+        for (int r = 0; r < SORT_ROUNDS; ++r) {
+            in[r] = tile + (wave * SORT_ROUNDS + r) * 64 + lane < to;
             const uint32_t digit = (key[r] >> p.shift) & mask;
             uint64_t same = __ballot(in[r]);
             for (int b = 0; b < p.bits; ++b) {
@@ -193,24 +320,25 @@ __global__ __launch_bounds__(256) void sort_place_kernel(const SortParams p)
             rank[r] = seen + (uint32_t)__popcll(below);
         }
         __syncthreads();
-        for (int b = tid; b < SORT_BINS; b += 256) {  // counts -> starts of the waves, and of the next tile
-            uint32_t at = start[b];
+        if (tid < SORT_BINS) {  // counts -> starts of the waves, and of the next tile
+            uint32_t at = start[tid];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t c = count[w][b];
-                count[w][b] = at;
+            for (int w = 0; w < SORT_WAVES; ++w) {
+                const uint32_t c = count[w][tid];
+                count[w][tid] = at;
                 at += c;
             }
-            start[b] = at;
+            start[tid] = at;
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < SORT_ROUNDS; ++r)
             if (in[r]) {
                 const uint32_t to_at = count[wave][(key[r] >> p.shift) & mask] + rank[r];
                 p.keys_out[to_at] = key[r];
                 p.order_out[to_at] = ord[r];
             }
+        if (tile + SORT_TILE < to) fetch(tile + SORT_TILE);
         __syncthreads();
     }
 }
@@ -228,137 +356,198 @@ struct GradParams {
     int accumulate;
 };
 
-template <class O, bool VEC>
+// Eight columns of a row of the gradient from d, of a row's sums
+template <class O, bool VEC, bool ADD>
 __device__ __forceinline__ void write_row8(const GradParams &p, uint32_t row, int d, const float (&sum)[8])
 {
     typename O::raw *at = static_cast<typename O::raw *>(p.grad) + (int64_t)row * p.ld_grad + d;
     float v[8];
-    if (VEC && d + 8 <= p.D) {
-        if (p.accumulate) get8<O>(at, v);
+    if constexpr (VEC) {
+        if (ADD) get8<O>(at, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p.accumulate ? __builtin_fmaf(sum[i], p.scale, v[i]) : sum[i] * p.scale;
+        for (int i = 0; i < 8; ++i) v[i] = ADD ? __builtin_fmaf(sum[i], p.scale, v[i]) : sum[i] * p.scale;
         put8<O>(at, v);
     } else {
-#pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (d + i < p.D) at[i] = O::put(p.accumulate ? __builtin_fmaf(sum[i], p.scale, O::get(at[i])) : sum[i] * p.scale);
+            if (d + i < p.D) at[i] = O::put(ADD ? __builtin_fmaf(sum[i], p.scale, O::get(at[i])) : sum[i] * p.scale);
     }
 }
 
-template <class O, bool VEC>
-__global__ __launch_bounds__(256) void zero_rows_kernel(const GradParams p, int units)
-{
-    const int64_t total = (int64_t)p.V * units;
-    for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < total; w += (int64_t)gridDim.x * 256) {
-        const int64_t row = w / units;
-        const int d = (int)(w - row * units) * 8;
-        typename O::raw *at = static_cast<typename O::raw *>(p.grad) + row * p.ld_grad + d;
-        const float zero[8] = {};
-        if (VEC && d + 8 <= p.D) {
-            put8<O>(at, zero);
-        } else {
-            for (int i = 0; i < 8; ++i)
-                if (d + i < p.D) at[i] = O::put(0.0f);
-        }
-    }
-}
-
-// A workgroup sums the rows of `chunk` sorted positions.  A run of one token that lies within the chunk goes straight to its
-// row; the parts of one that crosses chunks are kept and joined by the next kernel, so that a token as frequent as the padding
-// of a batch is spread over the chip like all others.
-template <class E, class O, bool VEC>
+// A workgroup sums the rows of `chunk` (at most 64) sorted positions.  The next rows are asked for before the sums at hand are written:
+// loads and stores come back in one order, and a wave that asks behind its stores waits for both.  A run of one token that
+// lies within the chunk goes straight to its row; the parts of one that crosses chunks are kept and joined by the next kernel, so
+// that a token as frequent as the padding of a batch is spread over the chip like all others.
+// VEC: D is a multiple of 8 and all rows of 16 bytes: a lane has eight neighbouring columns.  Otherwise a lane's eight columns are a
+// workgroup's width apart, so that neighbouring lanes still ask for neighbouring values.
+template <class E, class O, bool VEC, bool ADD>
 __global__ __launch_bounds__(256) void sum_runs_kernel(const GradParams p)
 {
-    const int c = blockIdx.x;
+    constexpr int AHEAD = !VEC ? 2 : E::BYTES == 4 ? 4 : 8;
+    constexpr uint32_t NONE = 0xFFFFFFFFu;
+    struct alignas(16) Eight {
+        typename E::raw v[8];
+    };
+    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 63, width = blockDim.x;
     const int64_t from = (int64_t)c * p.chunk;
     const int to = (int)(from + p.chunk < p.M ? from + p.chunk : p.M);
-    const uint32_t before = from > 0 ? p.keys[from - 1] : 0xFFFFFFFFu;
-    const uint32_t after = to < p.M ? p.keys[to] : 0xFFFFFFFFu;
-    for (int d = threadIdx.x * 8; d < p.D; d += 256 * 8) {
+    const bool in = from + lane < to;
+    const uint32_t my_key = in ? p.keys[from + lane] : NONE, my_row = in ? p.order[from + lane] : 0;
+    const uint32_t before = from > 0 ? p.keys[from - 1] : NONE, after = to < p.M ? p.keys[to] : NONE;
+    const int n = __popcll(__ballot(my_key < p.V));  // (keys of V are behind all others)
+    if (n == 0) return;
+    // (all lanes stay in this loop, whether they have columns or not: the keys and rows that they hold are read across lanes)
+    for (int base = 0; base < p.D; base += width * 8) {
+        const int d = VEC ? base + tid * 8 : base + tid, stride = VEC ? 1 : width;
         float sum[8];
-        uint32_t run = 0xFFFFFFFFu;
+        uint32_t run = NONE;
         bool first = true;
         auto flush = [&](bool last) {
-            if (first && run == before) {
-                float *at = p.head + (int64_t)c * p.pitch + d;
-                reinterpret_cast<float4 *>(at)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-                reinterpret_cast<float4 *>(at)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
-            } else if (last && run == after) {
-                float *at = p.tail + (int64_t)c * p.pitch + d;
-                reinterpret_cast<float4 *>(at)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-                reinterpret_cast<float4 *>(at)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
-            } else {
-                write_row8<O, VEC>(p, run, d, sum);
-            }
+            const bool head = first && run == before;
             first = false;
-        };
-        for (int i = (int)from; i < to; ++i) {
-            const uint32_t key = p.keys[i];
-            if (key >= p.V) break;
-            const typename E::raw *row = static_cast<const typename E::raw *>(p.dy) + (int64_t)p.order[i] * p.ld_dy + d;
-            float v[8];
-            if (VEC && d + 8 <= p.D) {
-                get8<E>(row, v);
+            if (d >= p.D) return;
+            if (head || (last && run == after)) {
+                float *at = (head ? p.head : p.tail) + (int64_t)c * p.pitch + d;
+                if constexpr (VEC) {
+                    put8<ElemF32>(at, sum);
+                } else {
+                    for (int e = 0; e < 8; ++e)
+                        if (d + e * stride < p.D) at[e * stride] = sum[e];
+                }
+            } else if constexpr (VEC) {
+                write_row8<O, true, ADD>(p, run, d, sum);
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = d + e < p.D ? E::get(row[e]) : 0.0f;
+                typename O::raw *at = static_cast<typename O::raw *>(p.grad) + (int64_t)run * p.ld_grad + d;
+                for (int e = 0; e < 8; ++e)
+                    if (d + e * stride < p.D)
+                        at[e * stride] = O::put(ADD ? __builtin_fmaf(sum[e], p.scale, O::get(at[e * stride])) : sum[e] * p.scale);
             }
-            if (key != run) {
-                if (run != 0xFFFFFFFFu) flush(false);
-                run = key;
+        };
+        Eight rows[2][AHEAD];
+        auto fetch = [&](int i, Eight(&to)[AHEAD]) {
+            const typename E::raw *at[AHEAD];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = v[e];
-            } else {
+            for (int a = 0; a < AHEAD; ++a) {
+                const uint32_t r = (uint32_t)__builtin_amdgcn_readlane((int)my_row, i + a < n ? i + a : n - 1);
+                at[a] = static_cast<const typename E::raw *>(p.dy) + (int64_t)r * p.ld_dy + d;
+            }
+            if (d < p.D) {
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) {
+                    if constexpr (VEC) {
+#pragma unroll
+                        for (int w = 0; w < (int)sizeof(Eight) / 16; ++w)
+                            reinterpret_cast<uint4 *>(&to[a])[w] = reinterpret_cast<const uint4 *>(at[a])[w];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) to[a].v[e] = d + e * stride < p.D ? at[a][e * stride] : typename E::raw(0);
+                    }
+                }
+            }
+        };
+        auto add = [&](int i, const Eight(&from)[AHEAD]) {
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                if (i + a >= n) break;
+                const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)my_key, i + a);
+                if (key != run) {
+                    if (run != NONE) flush(false);
+                    run = key;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] = E::get(from[a].v[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += E::get(from[a].v[e]);
+                }
+            }
+        };
+        fetch(0, rows[0]);
+        for (int i = 0; i < n; i += 2 * AHEAD) {
+            if (i + AHEAD < n) fetch(i + AHEAD, rows[1]);
+            add(i, rows[0]);
+            if (i + 2 * AHEAD < n) fetch(i + 2 * AHEAD, rows[0]);
+            add(i + AHEAD, rows[1]);
+        }
+        flush(true);
+    }
+}
+
+// Joins the parts of the runs that cross chunks.  Workgroup c of the first `chunks` - 1 has the run that begins in chunk c, if it goes
+// on, but over fewer than JOIN_SHORT chunks more.  A longer one covers a boundary whose number is a multiple of JOIN_SHORT: the
+// first such boundary's JOIN_SHARES workgroups have a share of its columns each.  (Workgroups for all shares of all chunks, of which
+// nearly all found nothing to do, took 17 us for 1024 chunks; a binary search for a run's end 11 us of latencies.)  Threads that share
+// columns take the chunks in turn, and their sums are added in a fixed order.
+constexpr int JOIN_SHARES = 8, JOIN_SHORT = 16;
+template <class O, bool VEC, bool ADD>
+__global__ __launch_bounds__(256) void join_runs_kernel(const GradParams p)
+{
+    __shared__ __attribute__((aligned(16))) float part[256][8];
+    __shared__ int ends;
+    const int tid = threadIdx.x;
+    // whether a run of this key crosses boundary k (the begin of chunk k, 0 < k < chunks)
+    auto crosses = [&](int k, uint32_t run) { return p.keys[(int64_t)k * p.chunk - 1] == run && p.keys[(int64_t)k * p.chunk] == run; };
+    int c, last, share = -1;
+    uint32_t run;
+    if ((int)blockIdx.x < p.chunks - 1) {
+        c = blockIdx.x;
+        run = p.keys[(int64_t)(c + 1) * p.chunk - 1];
+        const uint32_t next = p.keys[(int64_t)(c + 1) * p.chunk], begun = c > 0 ? p.keys[(int64_t)c * p.chunk - 1] : 0xFFFFFFFFu;
+        const int k = c + 2 + (tid & 63);  // (a wave has all it needs, and all waves find the same)
+        const bool goes_on = (tid & 63) < JOIN_SHORT && k < p.chunks && p.keys[(int64_t)k * p.chunk] == run;
+        if (run >= p.V || next != run || begun == run) return;  // (sorted: begun == run says that it began before)
+        last = c + 1 + __builtin_ctzll(~__ballot(goes_on));
+        if (last - c >= JOIN_SHORT) return;
+    } else {
+        const int job = blockIdx.x - (p.chunks - 1), m = (job / JOIN_SHARES + 1) * JOIN_SHORT;
+        share = job % JOIN_SHARES;
+        run = p.keys[(int64_t)m * p.chunk];
+        if (run >= p.V || !crosses(m, run) || (m > JOIN_SHORT && crosses(m - JOIN_SHORT, run))) return;
+        const int back = tid & 63;
+        const bool longer = back < JOIN_SHORT && m - back > 0 && crosses(m - back, run);
+        c = m - __builtin_ctzll(~__ballot(longer));  // (boundaries m, m - 1, .. are crossed: as many chunks back it begins)
+        last = m;
+        for (int base = m + 1; base < p.chunks; base += 256) {
+            if (tid == 0) ends = 256;
+            __syncthreads();
+            const int k = base + tid;
+            if (!(k < p.chunks && p.keys[(int64_t)k * p.chunk] == run)) atomicMin(&ends, tid);
+            __syncthreads();
+            const int e = ends;
+            last = base + e - 1;
+            __syncthreads();
+            if (e < 256) break;
+        }
+        if (last - c < JOIN_SHORT) return;
+    }
+    const int units = p.pitch / 8;
+    int u0 = 0, u1 = units;
+    if (share >= 0) {
+        const int per = (units + JOIN_SHARES - 1) / JOIN_SHARES;
+        u0 = share * per;
+        u1 = u0 + per < units ? u0 + per : units;
+    }
+    for (; u0 < u1; u0 += 256) {
+        const int tx = u1 - u0 < 256 ? u1 - u0 : 256, sharers = 256 / tx;
+        const int r = tid / tx, u = u0 + tid - r * tx;
+        float sum[8] = {};
+        if (r < sharers) {
+#pragma unroll 4
+            for (int k = c + r; k <= last; k += sharers) {
+                float v[8];
+                load8<float>((k == c ? p.tail : p.head) + (int64_t)k * p.pitch + u * 8, v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += v[e];
             }
         }
-        if (run != 0xFFFFFFFFu) flush(true);
-    }
-}
-
-// Joins the parts of the run that chunk blockIdx.x begins and does not end: 32 rows of 8 threads take the chunks it crosses in
-// turn, 64 columns at a time, and their sums are added in a fixed order.
-template <class O, bool VEC>
-__global__ __launch_bounds__(256) void join_runs_kernel(const GradParams p)
-{
-    __shared__ float part[32][65];
-    const int c = blockIdx.x;
-    const int64_t from = (int64_t)c * p.chunk, to = from + p.chunk;
-    if (to >= p.M) return;
-    const uint32_t run = p.keys[to - 1];
-    if (run >= p.V || p.keys[to] != run) return;
-    if (from > 0 && p.keys[from] == run && p.keys[from - 1] == run) return;  // it began before
-    int lo = (int)to, hi = p.M;  // the first position past the run
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (p.keys[mid] <= run) lo = mid + 1;
-        else hi = mid;
-    }
-    const int last = (lo - 1) / p.chunk;
-    const int r = threadIdx.x >> 3, t = threadIdx.x & 7;
-    const int d = blockIdx.y * 64 + t * 8;
-    float sum[8] = {};
-    if (d < p.D)
-        for (int k = c + r; k <= last; k += 32) {
-            const float *at = (k == c ? p.tail : p.head) + (int64_t)k * p.pitch + d;
-            float v[8];
-            load8<float>(at, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += v[e];
-        }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) part[r][t * 8 + e] = sum[e];
-    for (int half = 16; half > 0; half >>= 1) {
         __syncthreads();
-        if (r < half)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) part[r][t * 8 + e] += part[r + half][t * 8 + e];
-    }
-    if (r == 0 && d < p.D) {
+        for (int e = 0; e < 8; ++e) part[tid][e] = sum[e];
+        __syncthreads();
+        if (r == 0) {
+            for (int s = 1; s < sharers; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = part[0][t * 8 + e];
-        write_row8<O, VEC>(p, run, d, sum);
+                for (int e = 0; e < 8; ++e) sum[e] += part[s * tx + tid][e];
+            write_row8<O, VEC, ADD>(p, run, u * 8, sum);
+        }
     }
 }
 
@@ -511,52 +700,66 @@ extern "C" int mkq_embedding_gradient(const void *tokens, int token_bits, int64_
     g.scale = scale;
     g.accumulate = accumulate != 0;
     const bool vec_grad = (ld_grad * dtype_bytes(grad_dtype)) % 16 == 0;
-    const int units = (int)ceil_div(D, 8);
     GradWorkspace w = {};
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     if (M > 0) {
         w = grad_workspace(M, D);
         if (!workspace || workspace_bytes < w.total) return MKQ_ERR_WORKSPACE;
         if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
-        if (!grid_ok(w.chunks, 256) || ceil_div(D, 64) > 65535 || !grid_ok(w.chunks * ceil_div(D, 64), 256)) return MKQ_ERR_UNSUPPORTED;
+        if (!grid_ok((int64_t)w.chunks * 2, 256)) return MKQ_ERR_UNSUPPORTED;
     }
-    if (!g.accumulate) {
-        int64_t workgroups = ceil_div(V * units, 256);
-        if (workgroups > 8192) workgroups = 8192;
-        with_elem(grad_dtype, [&](auto o) {
-            with_bool(vec_grad, [&](auto v) {
-                zero_rows_kernel<decltype(o), decltype(v)::value><<<(unsigned)workgroups, 256, 0, st>>>(g, units);
-            });
-        });
-        if (launch_status() != MKQ_OK) return MKQ_ERR_HIP;
+    // share i of n of the rows to fill with zeros, behind `first` workgroups; *workgroups: how many more for it
+    auto zero_share = [&](int i, int n, unsigned first, int threads, unsigned *workgroups) {
+        ZeroParams z = {grad, ld_grad, V * i / n, V * (i + 1) / n, (int)D, (int)dtype_bytes(grad_dtype), vec_grad, first};
+        const int64_t vectors = (z.rows_to - z.rows_from) * ceil_div(D * z.bytes, 16), most = 262144 / threads;
+        const int64_t need = ceil_div(vectors, threads);
+        *workgroups = g.accumulate ? 0 : (unsigned)(need < most ? need : most);
+        return z;
+    };
+    if (M == 0) {
+        unsigned workgroups;
+        const ZeroParams z = zero_share(0, 1, 0, 256, &workgroups);
+        if (workgroups == 0) return MKQ_OK;
+        zero_rows_kernel<<<workgroups, 256, 0, st>>>(z);
+        return launch_status();
     }
-    if (M == 0) return MKQ_OK;
 
     SortParams s = {};
     s.tokens = tokens;
     s.padding = padding_token;
     s.M = (int)M;
     s.V = (uint32_t)V;
-    s.per_block = (int)(ceil_div(ceil_div(M, SORT_BLOCKS), SORT_TILE) * SORT_TILE);
-    s.blocks = (int)ceil_div(M, s.per_block);
     s.counts = reinterpret_cast<uint32_t *>(ws + w.counts);
-    int key_bits = 1;  // of 0 .. V
-    while (((int64_t)1 << key_bits) <= V) ++key_bits;
-    const int passes = (key_bits + 8) / 9;
-    s.bits = (key_bits + passes - 1) / passes;
-    for (int pass = 0; pass < passes; ++pass) {
-        s.shift = pass * s.bits;
-        s.keys_in = pass ? reinterpret_cast<uint32_t *>(ws + w.keys[(pass + 1) & 1]) : nullptr;
-        s.order_in = pass ? reinterpret_cast<uint32_t *>(ws + w.order[(pass + 1) & 1]) : nullptr;
-        s.keys_out = reinterpret_cast<uint32_t *>(ws + w.keys[pass & 1]);
-        s.order_out = reinterpret_cast<uint32_t *>(ws + w.order[pass & 1]);
-        with_index(token_bits, [&](auto i) {
-            with_bool(pass == 0, [&](auto first) {
-                sort_count_kernel<decltype(i), decltype(first)::value><<<s.blocks, 256, 0, st>>>(s);
-                sort_place_kernel<decltype(i), decltype(first)::value><<<s.blocks, 256, 0, st>>>(s);
+    unsigned zeros;
+    if (M <= RANK_MAX) {
+        const unsigned blocks = (unsigned)ceil_div(M, RANK_KEYS);
+        s.keys_out = reinterpret_cast<uint32_t *>(ws + w.keys[0]);
+        s.order_out = reinterpret_cast<uint32_t *>(ws + w.order[0]);
+        s.zero = zero_share(0, 1, blocks, RANK_THREADS, &zeros);
+        with_index(token_bits, [&](auto i) { rank_kernel<decltype(i)><<<blocks + zeros, RANK_THREADS, 0, st>>>(s); });
+    } else {
+        s.per_block = (int)(ceil_div(ceil_div(M, SORT_BLOCKS), SORT_TILE) * SORT_TILE);
+        s.blocks = (int)ceil_div(M, s.per_block);
+        int key_bits = 1;  // of 0 .. V
+        while (((int64_t)1 << key_bits) <= V) ++key_bits;
+        const int passes = (key_bits + 8) / 9;
+        s.bits = (key_bits + passes - 1) / passes;
+        for (int pass = 0; pass < passes; ++pass) {
+            s.shift = pass * s.bits;
+            s.keys_in = pass ? reinterpret_cast<uint32_t *>(ws + w.keys[(pass + 1) & 1]) : nullptr;
+            s.order_in = pass ? reinterpret_cast<uint32_t *>(ws + w.order[(pass + 1) & 1]) : nullptr;
+            s.keys_out = reinterpret_cast<uint32_t *>(ws + w.keys[pass & 1]);
+            s.order_out = reinterpret_cast<uint32_t *>(ws + w.order[pass & 1]);
+            with_index(token_bits, [&](auto i) {
+                with_bool(pass == 0, [&](auto first) {
+                    s.zero = zero_share(2 * pass, 2 * passes, s.blocks, SORT_THREADS, &zeros);
+                    sort_count_kernel<decltype(i), decltype(first)::value><<<s.blocks + zeros, SORT_THREADS, 0, st>>>(s);
+                    s.zero = zero_share(2 * pass + 1, 2 * passes, s.blocks, SORT_THREADS, &zeros);
+                    sort_place_kernel<decltype(i), decltype(first)::value><<<s.blocks + zeros, SORT_THREADS, 0, st>>>(s);
+                });
             });
-        });
-        if (launch_status() != MKQ_OK) return MKQ_ERR_HIP;
+            if (launch_status() != MKQ_OK) return MKQ_ERR_HIP;
+        }
     }
     g.keys = s.keys_out;
     g.order = s.order_out;
@@ -565,11 +768,16 @@ extern "C" int mkq_embedding_gradient(const void *tokens, int token_bits, int64_
     g.chunk = w.chunk;
     g.chunks = w.chunks;
     g.pitch = w.pitch;
+    const unsigned join_workgroups = (unsigned)(g.chunks - 1 + (g.chunks - 1) / JOIN_SHORT * JOIN_SHARES);
+    const int sum_threads = (int)(D > 1536 ? 256 : ceil_div(D, 512) * 64);  // eight columns each
     with_elem(dy_dtype, [&](auto e) {
         with_elem(grad_dtype, [&](auto o) {
-            with_bool(vec_grad && (ld_dy * decltype(e)::BYTES) % 16 == 0, [&](auto v) {
-                sum_runs_kernel<decltype(e), decltype(o), decltype(v)::value><<<g.chunks, 256, 0, st>>>(g);
-                join_runs_kernel<decltype(o), decltype(v)::value><<<dim3(g.chunks, (unsigned)ceil_div(D, 64)), 256, 0, st>>>(g);
+            with_bool(vec_grad && (ld_dy * decltype(e)::BYTES) % 16 == 0 && D % 8 == 0, [&](auto v) {
+                with_bool(g.accumulate, [&](auto add) {
+                    constexpr bool VEC = decltype(v)::value, ADD = decltype(add)::value;
+                    sum_runs_kernel<decltype(e), decltype(o), VEC, ADD><<<g.chunks, sum_threads, 0, st>>>(g);
+                    if (g.chunks > 1) join_runs_kernel<decltype(o), VEC, ADD><<<join_workgroups, 256, 0, st>>>(g);
+                });
             });
         });
     });

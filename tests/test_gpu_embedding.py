@@ -168,7 +168,7 @@ def test_gradient_of_extreme_batches(mkq, M, tokens):
     check_gradient(got, t, dy, V, 1.0, padding)
 
 
-@pytest.mark.parametrize("M,V,D", [(300000, 1000, 8), (300000, 200000, 4), (65536, 30522, 32)])
+@pytest.mark.parametrize("M,V,D", [(300000, 1000, 8), (300000, 200000, 4), (65536, 30522, 32), (12288, 5000, 24), (12289, 5000, 24), (1200000, 90, 8)])
 def test_gradient_of_long_batches(mkq, M, V, D):
     t = some_tokens(M, V, 1, torch.int32)
     dy = torch.randn(M, D, generator=torch.Generator().manual_seed(2))
