@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmkq.so")
@@ -212,9 +213,14 @@ def _dtype_code(t):
     return _dtype_codes[t.dtype]
 
 
+_torch_dtypes = {}
+
+
 def _torch_dtype(code):
-    torch = _torch()
-    return {MKQ_F32: torch.float32, MKQ_F16: torch.float16, MKQ_BF16: torch.bfloat16}[code]
+    if not _torch_dtypes:
+        torch = _torch()
+        _torch_dtypes.update({MKQ_F32: torch.float32, MKQ_F16: torch.float16, MKQ_BF16: torch.bfloat16})
+    return _torch_dtypes[code]
 
 
 # ----------------------------------------------------------------------------------
@@ -650,15 +656,23 @@ def _need(ok, what: str):
 
 def _rows(t, what: str):
     """Row stride of a matrix whose rows are contiguous."""
-    _need(t.dim() == 2 and (t.size(1) <= 1 or t.stride(1) == 1), f"{what}: a matrix with contiguous rows")
-    return t.stride(0) if t.size(0) > 1 else max(t.size(1), 1)
+    if t.dim() == 2:
+        rows, cols = t.shape
+        ld, step = t.stride()
+        if cols <= 1 or step == 1:
+            return ld if rows > 1 else max(cols, 1)
+    raise ValueError(f"{what}: a matrix with contiguous rows")
 
 
-def _same_device(first, *rest):
-    dev = first.device
-    _need(dev.type == "cuda" and dev.index == _torch().cuda.current_device(), "tensors live on the current GPU")
-    for t in rest:
-        _need(t is None or t.device == dev, "tensors live on one GPU")
+def _same_device(*tensors):
+    """All on the current GPU.  (get_device is a number, -1 on the host; comparing device objects took 2 us of a call.)"""
+    torch = _torch()
+    dev = tensors[0].get_device()
+    if dev < 0 or dev != (torch._C._cuda_getDevice() if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device()):
+        raise ValueError("tensors live on the current GPU")
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors live on one GPU")
 
 
 def _new(shape, dtype, device, stream):
@@ -798,11 +812,17 @@ def mkq_gradient_norm_workspace_bytes(n: int) -> int:
     return int(load().mkq_gradient_norm_workspace_bytes(n))
 
 
-def _tensor_list(tensors):
-    """Host arrays of addresses, numbers of values and types."""
-    n = len(tensors)
-    return ((C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int64 * n)(*[t.numel() for t in tensors]),
-            (C.c_int32 * n)(*[_dtype_code(t) for t in tensors]))
+def _tensor_list(tensors, what: str):
+    """Numbers of values, types and addresses of contiguous tensors of the current GPU.  (One pass a question, in C: a loop over fifty
+    tensors and their outputs took 50 us of a call.)"""
+    torch = _torch()
+    T = torch.Tensor
+    if not tensors or not all(map(T.is_contiguous, tensors)):
+        raise ValueError(f"{what}: contiguous tensors, one at least")
+    _same_device(tensors[0])
+    if len(set(map(T.get_device, tensors))) != 1:
+        raise ValueError("tensors live on one GPU")
+    return list(map(T.numel, tensors)), [t.dtype for t in tensors], array("Q", map(T.data_ptr, tensors))
 
 
 def _norm_buffers(n: int, device, norm_out, workspace, stream):
@@ -818,12 +838,12 @@ def _norm_buffers(n: int, device, norm_out, workspace, stream):
 def mkq_gradient_norm(grads, norm_out=None, workspace=None, stream=None):
     """Norm over all values of a list of contiguous tensors (float32 / float16 / bfloat16, mixed) -> float32 tensor [1]."""
     grads = list(grads)
-    _need(grads and all(t.is_contiguous() for t in grads), "grads: contiguous tensors, one at least")
-    _same_device(*grads, norm_out, workspace)
+    counts, dtypes, at = _tensor_list(grads, "grads")
+    _same_device(grads[0], norm_out, workspace)
     norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
-    at, counts, dtypes = _tensor_list(grads)
-    _check(load().mkq_gradient_norm(len(grads), at, counts, dtypes, _ptr(norm_out), _ptr(workspace), workspace.nbytes,
-                                    _stream(stream)), "mkq_gradient_norm")
+    counts, codes = array("q", counts), array("i", map(_dtype_codes.__getitem__, dtypes))
+    _check(load().mkq_gradient_norm(len(grads), at.buffer_info()[0], counts.buffer_info()[0], codes.buffer_info()[0], _ptr(norm_out),
+                                    _ptr(workspace), workspace.nbytes, _stream(stream)), "mkq_gradient_norm")
     return norm_out
 
 
@@ -831,18 +851,19 @@ def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, work
     """Scales a list of gradients to a norm of at most max_norm, in place or into ``outs`` (same types and sizes); returns the
     norm before, float32 tensor [1]."""
     grads = list(grads)
-    outs = grads if outs is None else list(outs)
-    _need(grads and all(t.is_contiguous() for t in grads), "grads: contiguous tensors, one at least")
-    _same_device(*grads, norm_out, workspace)
-    if outs is not grads:
-        _need(len(outs) == len(grads) and all(o.dtype == t.dtype and o.numel() == t.numel() and o.is_contiguous()
-                                              for o, t in zip(outs, grads)), "outs: contiguous, the gradients' types and sizes")
-        _same_device(*outs)
+    counts, dtypes, at = _tensor_list(grads, "grads")
+    _same_device(grads[0], norm_out, workspace)
+    out_at = at
+    if outs is not None:
+        outs = list(outs)
+        out_counts, out_dtypes, out_at = _tensor_list(outs, "outs")
+        _same_device(grads[0], outs[0])
+        _need(out_counts == counts and out_dtypes == dtypes, "outs: the gradients' types and sizes")
     norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
-    at, counts, dtypes = _tensor_list(grads)
-    out_at = at if outs is grads else (C.c_void_p * len(outs))(*[t.data_ptr() for t in outs])
-    _check(load().mkq_clip_gradients(len(grads), at, out_at, counts, dtypes, float(max_norm), _ptr(norm_out), _ptr(workspace),
-                                     workspace.nbytes, _stream(stream)), "mkq_clip_gradients")
+    counts, codes = array("q", counts), array("i", map(_dtype_codes.__getitem__, dtypes))
+    _check(load().mkq_clip_gradients(len(grads), at.buffer_info()[0], out_at.buffer_info()[0], counts.buffer_info()[0],
+                                     codes.buffer_info()[0], float(max_norm), _ptr(norm_out), _ptr(workspace), workspace.nbytes,
+                                     _stream(stream)), "mkq_clip_gradients")
     return norm_out
 
 

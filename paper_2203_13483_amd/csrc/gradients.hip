@@ -6,12 +6,13 @@
 // sums are binary64, in an order that does not depend on which workgroup is done first, so the norm of gradients beyond
 // 1e19 does not overflow and equal inputs give equal bits.
 #include "elements.h"
+#include "gemm_common.h"
 
 namespace mkq {
 
 // Tensors of one launch travel in the kernel's arguments, whose room is 4 KiB
 constexpr int TENSORS = 100;
-constexpr int PIECE = 8192;           // values that a workgroup takes at a time
+constexpr int PIECE = 8192;            // values that a workgroup takes at a time
 constexpr int NORM_WORKGROUPS = 2048;  // partial sums of a launch
 struct TensorList {
     const void *grad[TENSORS];
@@ -24,11 +25,12 @@ struct TensorList {
 static_assert(sizeof(TensorList) <= 3800, "kernel arguments");
 
 // f(tensor, first value, values) for the pieces of this workgroup
-template <class F>
+template <bool BACKWARDS, class F>
 __device__ __forceinline__ void for_each_piece(const TensorList &l, F &&f)
 {
     const int pieces = l.first_piece[l.n];
-    for (int piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+    for (int i = blockIdx.x; i < pieces; i += gridDim.x) {
+        const int piece = BACKWARDS ? pieces - 1 - i : i;
         int lo = 0, hi = l.n;  // the last tensor whose first piece is at most this one
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
@@ -52,25 +54,63 @@ __device__ __forceinline__ double workgroup_sum(double v, double *part)
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// The values of 16 bytes
 template <class E>
-__device__ __forceinline__ double sum_squares(const typename E::raw *g, int values)
-{
-    double sum = 0.0;
-    int i = threadIdx.x * 8;
-    if (reinterpret_cast<uintptr_t>(g) % 16 == 0) {
-        for (; i + 8 <= values; i += 256 * 8) {
-            float v[8];
-            get8<E>(g + i, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = __builtin_fma((double)v[e], (double)v[e], sum);
-        }
+struct Vector {
+    static constexpr int N = 16 / E::BYTES;
+    uint4 raw;
+    __device__ __forceinline__ float get(int i) const
+    {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        if constexpr (E::BYTES == 4) return __uint_as_float(w[i]);
+        else return E::get((uint16_t)(w[i / 2] >> (16 * (i % 2))));
     }
-    for (; i < values; i += 256 * 8)
-        for (int e = 0; e < 8; ++e)
-            if (i + e < values) {
-                const double v = (double)E::get(g[i + e]);
-                sum = __builtin_fma(v, v, sum);
-            }
+    __device__ __forceinline__ void scale(float c)
+    {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E::BYTES == 4) w[i] = __float_as_uint(get(i) * c);
+            else w[i] = std::is_same<E, ElemF16>::value ? pack2_f16(get(2 * i) * c, get(2 * i + 1) * c) : pack2_bf16(get(2 * i) * c, get(2 * i + 1) * c);
+        }
+        raw = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+// f(number of vectors, the first) and g(a value's place) for the values of a piece: whole pieces as neighbouring vectors of 16 bytes
+// a thread, all of them asked for before the first is used; what is left, or not aligned to vectors, value by value
+template <class E, class F, class G>
+__device__ __forceinline__ void each_vector(uintptr_t aligned, int values, F &&f, G &&g)
+{
+    constexpr int N = Vector<E>::N;
+    int from = 0;
+    if (aligned % 16 == 0) {
+        if (values == PIECE) return f(IntC<PIECE / 256 / N>(), threadIdx.x);
+        const int vectors = values / N;
+        for (int v = threadIdx.x; v < vectors; v += 256) f(IntC<1>(), v);
+        from = vectors * N;
+    }
+    for (int i = from + threadIdx.x; i < values; i += 256) g(i);
+}
+
+template <class E>
+__device__ __forceinline__ double sum_squares(const void *p, int64_t at, int values)
+{
+    const typename E::raw *g = static_cast<const typename E::raw *>(p) + at;
+    double sum = 0.0;
+    auto add = [&](float v) { sum = __builtin_fma((double)v, (double)v, sum); };
+    each_vector<E>(
+        reinterpret_cast<uintptr_t>(g), values,
+        [&](auto n, int v) {
+            Vector<E> x[decltype(n)::value];
+#pragma unroll
+            for (int k = 0; k < decltype(n)::value; ++k) x[k].raw = reinterpret_cast<const uint4 *>(g)[v + k * 256];
+#pragma unroll
+            for (int k = 0; k < decltype(n)::value; ++k)
+#pragma unroll
+                for (int i = 0; i < Vector<E>::N; ++i) add(x[k].get(i));
+        },
+        [&](int i) { add(E::get(g[i])); });
     return sum;
 }
 
@@ -78,10 +118,10 @@ __global__ __launch_bounds__(256) void norm_partials_kernel(const TensorList l, 
 {
     __shared__ double part[4];
     double sum = 0.0;
-    for_each_piece(l, [&](int t, int64_t from, int values) {
-        if (l.dtype[t] == MKQ_F32) sum += sum_squares<ElemF32>(static_cast<const float *>(l.grad[t]) + from, values);
-        else if (l.dtype[t] == MKQ_F16) sum += sum_squares<ElemF16>(static_cast<const uint16_t *>(l.grad[t]) + from, values);
-        else sum += sum_squares<ElemBF16>(static_cast<const uint16_t *>(l.grad[t]) + from, values);
+    for_each_piece<false>(l, [&](int t, int64_t from, int values) {
+        if (l.dtype[t] == MKQ_F32) sum += sum_squares<ElemF32>(l.grad[t], from, values);
+        else if (l.dtype[t] == MKQ_F16) sum += sum_squares<ElemF16>(l.grad[t], from, values);
+        else sum += sum_squares<ElemBF16>(l.grad[t], from, values);
     });
     sum = workgroup_sum(sum, part);
     if (threadIdx.x == 0) partials[blockIdx.x] = sum;
@@ -102,24 +142,27 @@ __global__ __launch_bounds__(256) void norm_kernel(const double *__restrict__ pa
 }
 
 template <class E>
-__device__ __forceinline__ void scale_values(const typename E::raw *g, typename E::raw *out, int values, float c)
+__device__ __forceinline__ void scale_values(const void *p, void *q, int64_t at, int values, float c)
 {
-    int i = threadIdx.x * 8;
-    if ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) % 16 == 0) {
-        for (; i + 8 <= values; i += 256 * 8) {
-            float v[8];
-            get8<E>(g + i, v);
+    const typename E::raw *g = static_cast<const typename E::raw *>(p) + at;
+    typename E::raw *out = static_cast<typename E::raw *>(q) + at;
+    each_vector<E>(
+        reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out), values,
+        [&](auto n, int v) {
+            Vector<E> x[decltype(n)::value];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= c;
-            put8<E>(out + i, v);
-        }
-    }
-    for (; i < values; i += 256 * 8)
-        for (int e = 0; e < 8; ++e)
-            if (i + e < values) out[i + e] = E::put(E::get(g[i + e]) * c);
+            for (int k = 0; k < decltype(n)::value; ++k) x[k].raw = reinterpret_cast<const uint4 *>(g)[v + k * 256];
+#pragma unroll
+            for (int k = 0; k < decltype(n)::value; ++k) {
+                x[k].scale(c);
+                reinterpret_cast<uint4 *>(out)[v + k * 256] = x[k].raw;
+            }
+        },
+        [&](int i) { out[i] = E::put(E::get(g[i]) * c); });
 }
 
 // Every workgroup adds up the partial sums itself (16 KB out of the L2), which spares a launch between the two passes.
+// Last pieces first: they were read last, and what the memory-side cache still holds of them need not come from HBM again.
 // A factor of 1 leaves gradients that are clipped in place as they are.
 __global__ __launch_bounds__(256) void clip_kernel(const TensorList l, const double *__restrict__ partials, int count, float max_norm,
                                                    float *__restrict__ norm_out)
@@ -129,14 +172,11 @@ __global__ __launch_bounds__(256) void clip_kernel(const TensorList l, const dou
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const double q = (double)max_norm / (norm + 1e-6);
     const float c = q < 1.0 || q != q ? (float)q : 1.0f;
-    for_each_piece(l, [&](int t, int64_t from, int values) {
+    for_each_piece<true>(l, [&](int t, int64_t from, int values) {
         if (c == 1.0f && l.out[t] == l.grad[t]) return;
-        if (l.dtype[t] == MKQ_F32)
-            scale_values<ElemF32>(static_cast<const float *>(l.grad[t]) + from, static_cast<float *>(l.out[t]) + from, values, c);
-        else if (l.dtype[t] == MKQ_F16)
-            scale_values<ElemF16>(static_cast<const uint16_t *>(l.grad[t]) + from, static_cast<uint16_t *>(l.out[t]) + from, values, c);
-        else
-            scale_values<ElemBF16>(static_cast<const uint16_t *>(l.grad[t]) + from, static_cast<uint16_t *>(l.out[t]) + from, values, c);
+        if (l.dtype[t] == MKQ_F32) scale_values<ElemF32>(l.grad[t], l.out[t], from, values, c);
+        else if (l.dtype[t] == MKQ_F16) scale_values<ElemF16>(l.grad[t], l.out[t], from, values, c);
+        else scale_values<ElemBF16>(l.grad[t], l.out[t], from, values, c);
     });
 }
 

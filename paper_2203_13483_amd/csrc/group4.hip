@@ -504,17 +504,17 @@ template <class E, int G, int TN, int MT, int KS>
 static int launch_group4(Group4Params p, hipStream_t st)
 {
     using S = Shape<E, G, TN, MT, KS>;
+    static_assert(S::lds(S::ROWS) <= 160 * 1024, "LDS is 160 KiB per CU");
+    p.lds_rows = p.M < S::ROWS ? p.M : S::ROWS;
+    p.blocks_n = (int)ceil_div(p.N, TN * (4 / KS));
+    const int64_t workgroups = (int64_t)p.blocks_n * ceil_div(p.M, S::ROWS);
+    if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
     static PerDeviceOnce once;  // (more than 64 KB of LDS have to be asked for)
     if (once.get([]() -> int {
             return hipFuncSetAttribute(reinterpret_cast<const void *>(&group4_kernel<E, G, TN, MT, KS>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)S::lds(S::ROWS)) == hipSuccess ? 1 : -1;
         }) <= 0)
         return MKQ_ERR_HIP;
-    static_assert(S::lds(S::ROWS) <= 160 * 1024, "LDS is 160 KiB per CU");
-    p.lds_rows = p.M < S::ROWS ? p.M : S::ROWS;
-    p.blocks_n = (int)ceil_div(p.N, TN * (4 / KS));
-    const int64_t workgroups = (int64_t)p.blocks_n * ceil_div(p.M, S::ROWS);
-    if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
     group4_kernel<E, G, TN, MT, KS><<<(unsigned)workgroups, 256, S::lds(p.lds_rows), st>>>(p);
     return launch_status();
 }
