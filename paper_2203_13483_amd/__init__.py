@@ -684,6 +684,12 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _new_matrix(rows: int, cols: int, dtype, device, stream):
+    if stream is None:  # (0.4 us less than empty)
+        return _torch().empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+    return _new((rows, cols), dtype, device, stream)
+
+
 def mkq_group_weight_bytes(N: int, K: int) -> int:
     return int(load().mkq_group_weight_bytes(N, K))
 
@@ -726,7 +732,7 @@ def mkq_linear_int4_group(x, Wq, s_w, bias, N: int, K: int, group: int = 64, out
     if out_dtype is None:
         out_dtype = _dtype_code(x)
     if out is None:
-        out = _new((M, N), _torch_dtype(out_dtype), x.device, stream)
+        out = _new_matrix(M, N, _torch_dtype(out_dtype), x.device, stream)
     else:
         _need(out.dtype == _torch_dtype(out_dtype) and out.is_contiguous() and tuple(out.shape) == (M, N), "out: contiguous [M, N] of out_dtype")
     epi = None
@@ -749,7 +755,7 @@ def _token_rows(tokens, D: int, out, out_dtype: int, stream):
     """The caller's [M, D] rows, or new ones, and their stride."""
     M = tokens.numel()
     if out is None:
-        return _new((M, D), _torch_dtype(out_dtype), tokens.device, stream), D
+        return _new_matrix(M, D, _torch_dtype(out_dtype), tokens.device, stream), D
     ld = _rows(out, "out")
     _need(out.dtype == _torch_dtype(out_dtype) and tuple(out.shape) == (M, D), "out: [M, D] of out_dtype")
     return out, ld
@@ -796,7 +802,7 @@ def mkq_embedding_gradient(tokens, dy, V: int, scale: float = 1.0, grad_dtype: i
     _same_device(tokens, dy, grad, workspace)
     _need(grad is not None or not accumulate, "accumulate: needs the gradient to add to")
     if grad is None:
-        grad, ld_grad = _new((V, D), _torch_dtype(grad_dtype), dy.device, stream), D
+        grad, ld_grad = _new_matrix(V, D, _torch_dtype(grad_dtype), dy.device, stream), D
     else:
         ld_grad = _rows(grad, "grad")
         _need(grad.dtype == _torch_dtype(grad_dtype) and tuple(grad.shape) == (V, D), "grad: [V, D] of grad_dtype")

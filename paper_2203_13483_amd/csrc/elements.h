@@ -27,6 +27,15 @@ struct ElemBF16 {
     __device__ static __forceinline__ raw put(float v) { return float_to_bf16_bits(v); }
 };
 
+// A product rounded to binary32, also where it is narrowed next: the compiler would fuse a single value's product with its rounding
+// to 16 bits, but not those of a vector, and the same value would come out differently by where it lies.
+__device__ __forceinline__ float product(float a, float b)
+{
+    float r = a * b;
+    asm("" : "+v"(r));
+    return r;
+}
+
 // Eight neighbours as binary32, from an address that is a multiple of 16
 template <class E>
 __device__ __forceinline__ void get8(const typename E::raw *p, float (&v)[8])

@@ -10,84 +10,116 @@
 
 namespace mkq {
 
-template <class I>
-__device__ __forceinline__ uint32_t token_row(const I *__restrict__ tokens, int64_t i, uint32_t V)
+constexpr uint32_t NO_ROW = 0xFFFFFFFFu;
+// The table row of position i's token, or NO_ROW
+__device__ __forceinline__ uint32_t token_row(const void *__restrict__ tokens, int bits, int64_t i, uint32_t V)
 {
-    const int64_t t = (int64_t)tokens[i];
-    return t >= 0 && t < (int64_t)V ? (uint32_t)t : 0xFFFFFFFFu;
+    const int64_t t = bits == 64 ? static_cast<const int64_t *>(tokens)[i] : (int64_t)static_cast<const int32_t *>(tokens)[i];
+    return t >= 0 && t < (int64_t)V ? (uint32_t)t : NO_ROW;
 }
 
 // ---- lookup -------------------------------------------------------------------------------------------------------------
 struct LookupParams {
     const void *tokens;
-    const void *table;  // float rows, or rows of nibbles
+    const void *table;  // float rows, or rows of nibbles (ld_table in words)
     const float *s_w;   // [V, groups] of the nibbles
     void *out;
     int64_t M, ld_table, ld_out;
     uint32_t V;
-    int D, groups, units, threads_per_row;
+    int D, groups, group_shift, token_bits, threads_per_row;
     float scale;
 };
 
-// Where a row's values come from: eight at position d (a multiple of 8), zeros from D on
-template <class E, bool VEC>
+// Where a row's values come from: eight neighbours from d (a multiple of 8), as fetched, or one
+template <class E>
 struct FloatRow {
+    struct alignas(16) Eight {
+        typename E::raw v[8];
+    };
     const typename E::raw *row;
-    __device__ __forceinline__ FloatRow(const LookupParams &p, uint32_t r) : row(static_cast<const typename E::raw *>(p.table) + (int64_t)r * p.ld_table) {}
-    __device__ __forceinline__ void get(const LookupParams &p, int d, float (&v)[8]) const
+    __device__ __forceinline__ void set(const LookupParams &p, uint32_t r) { row = static_cast<const typename E::raw *>(p.table) + (int64_t)r * p.ld_table; }
+    __device__ __forceinline__ void fetch(const LookupParams &, int d, Eight &to) const
     {
-        if (VEC && d + 8 <= p.D) {
-            get8<E>(row + d, v);
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = d + i < p.D ? E::get(row[d + i]) : 0.0f;
-        }
+        for (int w = 0; w < (int)sizeof(Eight) / 16; ++w) reinterpret_cast<uint4 *>(&to)[w] = reinterpret_cast<const uint4 *>(row + d)[w];
     }
+    __device__ static __forceinline__ float get(const Eight &x, int i) { return E::get(x.v[i]); }
+    __device__ __forceinline__ float one(const LookupParams &, int d) const { return E::get(row[d]); }
 };
-template <int G>
 struct NibbleRow {
+    struct Eight {
+        uint32_t word;
+        float step;
+    };
     const uint32_t *row;
     const float *s;
-    __device__ __forceinline__ NibbleRow(const LookupParams &p, uint32_t r)
-        : row(static_cast<const uint32_t *>(p.table) + (int64_t)r * p.ld_table), s(p.s_w + (int64_t)r * p.groups) {}
-    __device__ __forceinline__ void get(const LookupParams &, int d, float (&v)[8]) const
+    __device__ __forceinline__ void set(const LookupParams &p, uint32_t r)
     {
-        const uint32_t w = row[d / 8];
-        const float step = s[d / G];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)((int)(w << (28 - 4 * i)) >> 28) * step;
+        row = static_cast<const uint32_t *>(p.table) + (int64_t)r * p.ld_table;
+        s = p.s_w + (int64_t)r * p.groups;
+    }
+    __device__ __forceinline__ void fetch(const LookupParams &p, int d, Eight &to) const
+    {
+        to.word = row[d / 8];
+        to.step = s[d >> p.group_shift];
+    }
+    __device__ static __forceinline__ float get(const Eight &x, int i) { return (float)((int)(x.word << (28 - 4 * i)) >> 28) * x.step; }
+    __device__ __forceinline__ float one(const LookupParams &p, int d) const
+    {
+        return (float)((int)(row[d / 8] << (28 - 4 * (d % 8))) >> 28) * s[d >> p.group_shift];
     }
 };
 
-// threads_per_row neighbouring threads write a token's row, eight values each at a time.
-template <class Row, class O, class I, bool VEC_OUT>
+// threads_per_row neighbouring threads write a token's row, and ROWS of them at a time, so that as many tokens, then as many rows are
+// on their way together (65536 binary16 rows of 1024 one at a time 46 us).  VEC: D is a multiple of 8 and all rows of 16 bytes, a
+// thread has eight neighbouring values; otherwise eight that are threads_per_row apart.
+template <class Row, class O, bool VEC, int ROWS>
 __global__ __launch_bounds__(256) void lookup_kernel(const LookupParams p)
 {
-    const int rows = blockDim.x / p.threads_per_row;
-    const int r = threadIdx.x / p.threads_per_row, u0 = threadIdx.x - r * p.threads_per_row;
+    const int rows = 256 / p.threads_per_row;
+    const int r = threadIdx.x / p.threads_per_row, u = threadIdx.x - r * p.threads_per_row;
     if (r >= rows) return;
-    for (int64_t i = (int64_t)blockIdx.x * rows + r; i < p.M; i += (int64_t)gridDim.x * rows) {
-        const uint32_t t = token_row(static_cast<const I *>(p.tokens), i, p.V);
-        const bool known = t != 0xFFFFFFFFu;
-        const Row row(p, known ? t : 0);
-        typename O::raw *out = static_cast<typename O::raw *>(p.out) + i * p.ld_out;
-        for (int u = u0; u < p.units; u += p.threads_per_row) {
-            const int d = u * 8;
-            float v[8];
-            if (known) {
-                row.get(p, d, v);
+    for (int64_t i0 = (int64_t)blockIdx.x * rows * ROWS + r; i0 < p.M; i0 += (int64_t)gridDim.x * rows * ROWS) {
+        Row row[ROWS];
+        bool known[ROWS];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= p.scale;
-            } else {
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t i = i0 + k * rows;
+            const uint32_t t = i < p.M ? token_row(p.tokens, p.token_bits, i, p.V) : NO_ROW;
+            known[k] = t != NO_ROW;
+            row[k].set(p, known[k] ? t : 0);
+        }
+        if constexpr (VEC) {
+            for (int d = u * 8; d < p.D; d += p.threads_per_row * 8) {
+                typename Row::Eight x[ROWS];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+                for (int k = 0; k < ROWS; ++k) row[k].fetch(p, d, x[k]);  // (row 0 exists where there is none to look up)
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = known[k] ? product(Row::get(x[k], e), p.scale) : 0.0f;
+                    if (i0 + k * rows < p.M) put8<O>(static_cast<typename O::raw *>(p.out) + (i0 + k * rows) * p.ld_out + d, v);
+                }
             }
-            if (VEC_OUT && d + 8 <= p.D) {
-                put8<O>(out + d, v);
-            } else {
+        } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (d + e < p.D) out[d + e] = O::put(v[e]);
+            for (int k = 0; k < ROWS; ++k) {
+                if (i0 + k * rows >= p.M) break;
+                typename O::raw *out = static_cast<typename O::raw *>(p.out) + (i0 + k * rows) * p.ld_out;
+                for (int d0 = u; d0 < p.D; d0 += p.threads_per_row * 8) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int d = d0 + e * p.threads_per_row;
+                        v[e] = known[k] && d < p.D ? product(row[k].one(p, d), p.scale) : 0.0f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int d = d0 + e * p.threads_per_row;
+                        if (d < p.D) out[d] = O::put(v[e]);
+                    }
+                }
             }
         }
     }
@@ -365,11 +397,11 @@ __device__ __forceinline__ void write_row8(const GradParams &p, uint32_t row, in
     if constexpr (VEC) {
         if (ADD) get8<O>(at, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = ADD ? __builtin_fmaf(sum[i], p.scale, v[i]) : sum[i] * p.scale;
+        for (int i = 0; i < 8; ++i) v[i] = ADD ? __builtin_fmaf(sum[i], p.scale, v[i]) : product(sum[i], p.scale);
         put8<O>(at, v);
     } else {
         for (int i = 0; i < 8; ++i)
-            if (d + i < p.D) at[i] = O::put(ADD ? __builtin_fmaf(sum[i], p.scale, O::get(at[i])) : sum[i] * p.scale);
+            if (d + i < p.D) at[i] = O::put(ADD ? __builtin_fmaf(sum[i], p.scale, O::get(at[i])) : product(sum[i], p.scale));
     }
 }
 
@@ -419,7 +451,7 @@ __global__ __launch_bounds__(256) void sum_runs_kernel(const GradParams p)
                 typename O::raw *at = static_cast<typename O::raw *>(p.grad) + (int64_t)run * p.ld_grad + d;
                 for (int e = 0; e < 8; ++e)
                     if (d + e * stride < p.D)
-                        at[e * stride] = O::put(ADD ? __builtin_fmaf(sum[e], p.scale, O::get(at[e * stride])) : sum[e] * p.scale);
+                        at[e * stride] = O::put(ADD ? __builtin_fmaf(sum[e], p.scale, O::get(at[e * stride])) : product(sum[e], p.scale));
             }
         };
         Eight rows[2][AHEAD];
@@ -569,16 +601,22 @@ static void with_bool(bool b, F &&f)
     else f(std::false_type());
 }
 
-template <class Row, class O, class I>
-static int launch_lookup(LookupParams p, hipStream_t st)
+template <class Row>
+static int launch_lookup(LookupParams p, bool table_vec, int out_dtype, hipStream_t st)
 {
-    p.units = (int)ceil_div(p.D, 8);
-    p.threads_per_row = p.units < 256 ? p.units : 256;
+    const int64_t units = ceil_div(p.D, 8);
+    p.threads_per_row = (int)(units < 256 ? units : 256);
     const int rows = 256 / p.threads_per_row;
-    int64_t workgroups = ceil_div(p.M, rows);
-    if (workgroups > 8192) workgroups = 8192;
-    with_bool((p.ld_out * O::BYTES) % 16 == 0, [&](auto v) {
-        lookup_kernel<Row, O, I, decltype(v)::value><<<(unsigned)workgroups, 256, 0, st>>>(p);
+    // four rows a thread where that still leaves a workgroup for every place on the chip, eight a CU
+    const bool four = p.M >= (int64_t)rows * 4 * 2048;
+    int64_t workgroups = ceil_div(p.M, rows * (four ? 4 : 1));
+    if (workgroups > 1 << 20) workgroups = 1 << 20;
+    with_elem(out_dtype, [&](auto o) {
+        with_bool(table_vec && p.D % 8 == 0 && (p.ld_out * decltype(o)::BYTES) % 16 == 0, [&](auto v) {
+            with_bool(four, [&](auto f) {
+                lookup_kernel<Row, decltype(o), decltype(v)::value, decltype(f)::value ? 4 : 1><<<(unsigned)workgroups, 256, 0, st>>>(p);
+            });
+        });
     });
     return launch_status();
 }
@@ -632,18 +670,10 @@ extern "C" int mkq_embedding(const void *tokens, int token_bits, int64_t M, cons
     if (!tokens || !table || !out) return MKQ_ERR_NULL;
     if (!tokens_aligned(tokens, token_bits) || !aligned16(table) || !aligned16(out)) return MKQ_ERR_ALIGN;
     if (V > MAX_ROWS || D > MAX_ROWS) return MKQ_ERR_UNSUPPORTED;
-    LookupParams p = {tokens, table, nullptr, out, M, ld_table, ld_out, (uint32_t)V, (int)D, 0, 0, 0, scale};
+    const LookupParams p = {tokens, table, nullptr, out, M, ld_table, ld_out, (uint32_t)V, (int)D, 0, 0, token_bits, 0, scale};
     const hipStream_t st = as_stream(stream);
     int status = MKQ_OK;
-    with_elem(table_dtype, [&](auto e) {
-        with_elem(out_dtype, [&](auto o) {
-            with_index(token_bits, [&](auto i) {
-                with_bool((ld_table * decltype(e)::BYTES) % 16 == 0, [&](auto v) {
-                    status = launch_lookup<FloatRow<decltype(e), decltype(v)::value>, decltype(o), decltype(i)>(p, st);
-                });
-            });
-        });
-    });
+    with_elem(table_dtype, [&](auto e) { status = launch_lookup<FloatRow<decltype(e)>>(p, (ld_table * decltype(e)::BYTES) % 16 == 0, out_dtype, st); });
     return status;
 }
 
@@ -657,19 +687,9 @@ extern "C" int mkq_embedding_int4_group(const void *tokens, int token_bits, int6
     if (!tokens || !Wq || !s_w || !out) return MKQ_ERR_NULL;
     if (!tokens_aligned(tokens, token_bits) || !aligned16(Wq) || !aligned4(s_w) || !aligned16(out)) return MKQ_ERR_ALIGN;
     if (V > MAX_ROWS || D > MAX_ROWS) return MKQ_ERR_UNSUPPORTED;
-    LookupParams p = {tokens, Wq, s_w, out, M, ceil_div(D, 32) * 4, ld_out, (uint32_t)V, (int)D, (int)ceil_div(D, group), 0, 0, scale};
-    const hipStream_t st = as_stream(stream);
-    int status = MKQ_OK;
-    with_elem(out_dtype, [&](auto o) {
-        with_index(token_bits, [&](auto i) {
-            using O = decltype(o);
-            using I = decltype(i);
-            if (group == 32) status = launch_lookup<NibbleRow<32>, O, I>(p, st);
-            else if (group == 64) status = launch_lookup<NibbleRow<64>, O, I>(p, st);
-            else status = launch_lookup<NibbleRow<128>, O, I>(p, st);
-        });
-    });
-    return status;
+    const LookupParams p = {tokens, Wq, s_w, out, M, ceil_div(D, 32) * 4, ld_out, (uint32_t)V, (int)D, (int)ceil_div(D, group),
+                            group == 32 ? 5 : group == 64 ? 6 : 7, token_bits, 0, scale};
+    return launch_lookup<NibbleRow>(p, true, out_dtype, as_stream(stream));
 }
 
 extern "C" size_t mkq_embedding_gradient_workspace_bytes(int64_t M, int64_t D)

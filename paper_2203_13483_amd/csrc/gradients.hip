@@ -71,7 +71,8 @@ struct Vector {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (E::BYTES == 4) w[i] = __float_as_uint(get(i) * c);
-            else w[i] = std::is_same<E, ElemF16>::value ? pack2_f16(get(2 * i) * c, get(2 * i + 1) * c) : pack2_bf16(get(2 * i) * c, get(2 * i + 1) * c);
+            else w[i] = std::is_same<E, ElemF16>::value ? pack2_f16(product(get(2 * i), c), product(get(2 * i + 1), c))
+                                                        : pack2_bf16(product(get(2 * i), c), product(get(2 * i + 1), c));
         }
         raw = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -158,7 +159,7 @@ __device__ __forceinline__ void scale_values(const void *p, void *q, int64_t at,
                 reinterpret_cast<uint4 *>(out)[v + k * 256] = x[k].raw;
             }
         },
-        [&](int i) { out[i] = E::put(E::get(g[i]) * c); });
+        [&](int i) { out[i] = E::put(product(E::get(g[i]), c)); });
 }
 
 // Every workgroup adds up the partial sums itself (16 KB out of the L2), which spares a launch between the two passes.
