@@ -664,15 +664,33 @@ def _rows(t, what: str):
     raise ValueError(f"{what}: a matrix with contiguous rows")
 
 
-def _same_device(*tensors):
-    """All on the current GPU.  (get_device is a number, -1 on the host; comparing device objects took 2 us of a call.)"""
-    torch = _torch()
+_current_device = None
+
+
+def _same_device(*tensors) -> int:
+    """The number of the current GPU, on which all tensors have to be.  (Numbers, -1 on the host: comparing device objects took 2 us
+    of a call.)"""
+    global _current_device
+    if _current_device is None:
+        torch = _torch()
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     dev = tensors[0].get_device()
-    if dev < 0 or dev != (torch._C._cuda_getDevice() if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device()):
+    if dev < 0 or dev != _current_device():
         raise ValueError("tensors live on the current GPU")
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError("tensors live on one GPU")
+    return dev
+
+
+def _stream_on(dev: int, stream):
+    """_stream where a tensor on the GPU has shown that it is set up."""
+    if stream is None:
+        try:
+            return _torch_module._C._cuda_getCurrentRawStream(dev)
+        except AttributeError:
+            pass
+    return _stream(stream)
 
 
 def _new(shape, dtype, device, stream):
@@ -699,7 +717,7 @@ def mkq_pack_weights_int4_group(W, group: int = 64, s_w_in=None, stream=None):
     torch = _torch()
     ldw = _rows(W, "W")
     N, K = W.shape
-    _same_device(W, s_w_in)
+    dev = _same_device(W, s_w_in)
     groups = -(-K // group) if group > 0 else 0
     if s_w_in is not None:
         _need(s_w_in.dtype == torch.float32 and s_w_in.is_contiguous() and tuple(s_w_in.shape) == (N, groups),
@@ -707,7 +725,7 @@ def mkq_pack_weights_int4_group(W, group: int = 64, s_w_in=None, stream=None):
     Wq = _new((N, -(-K // 32) * 16), torch.uint8, W.device, stream)
     s_w = _new((N, groups), torch.float32, W.device, stream)
     _check(load().mkq_pack_weights_int4_group(_ptr(W), _dtype_code(W), N, K, ldw, int(group), _ptr(s_w_in), _ptr(s_w),
-                                              _ptr(Wq), _stream(stream)), "mkq_pack_weights_int4_group")
+                                              _ptr(Wq), _stream_on(dev, stream)), "mkq_pack_weights_int4_group")
     return Wq, s_w
 
 
@@ -726,7 +744,7 @@ def mkq_linear_int4_group(x, Wq, s_w, bias, N: int, K: int, group: int = 64, out
     ldx = _rows(x, "x")
     M = x.size(0)
     _need(x.size(1) == K, "x: [M, K]")
-    _same_device(x, Wq, s_w, bias, residual, out)
+    dev = _same_device(x, Wq, s_w, bias, residual, out)
     _group_table(Wq, s_w, N, K, group)
     _need(bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == N), "bias: float32 [N]")
     if out_dtype is None:
@@ -741,7 +759,7 @@ def mkq_linear_int4_group(x, Wq, s_w, bias, N: int, K: int, group: int = 64, out
         epi = C.byref(Epilogue(act=int(act), residual=_ptr(residual),
                                residual_dtype=_dtype_code(residual) if residual is not None else MKQ_F32))
     _check(load().mkq_linear_int4_group(_ptr(x), _dtype_code(x), ldx, _ptr(Wq), _ptr(s_w), int(group), _ptr(bias), M, N, K,
-                                        _ptr(out), int(out_dtype), epi, _stream(stream)), "mkq_linear_int4_group")
+                                        _ptr(out), int(out_dtype), epi, _stream_on(dev, stream)), "mkq_linear_int4_group")
     return out
 
 
@@ -766,12 +784,12 @@ def mkq_embedding(tokens, table, scale: float = 1.0, out_dtype: int | None = Non
     bits = _tokens(tokens)
     ld_table = _rows(table, "table")
     V, D = table.shape
-    _same_device(tokens, table, out)
+    dev = _same_device(tokens, table, out)
     if out_dtype is None:
         out_dtype = _dtype_code(table)
     out, ld_out = _token_rows(tokens, D, out, out_dtype, stream)
     _check(load().mkq_embedding(_ptr(tokens), bits, tokens.numel(), _ptr(table), _dtype_code(table), V, D, ld_table, float(scale),
-                                _ptr(out), int(out_dtype), ld_out, _stream(stream)), "mkq_embedding")
+                                _ptr(out), int(out_dtype), ld_out, _stream_on(dev, stream)), "mkq_embedding")
     return out
 
 
@@ -779,11 +797,11 @@ def mkq_embedding_int4_group(tokens, Wq, s_w, V: int, D: int, group: int = 64, s
                              out=None, stream=None):
     """Rows of a group-scaled 4-bit table (mkq_pack_weights_int4_group with N = V, K = D) times scale -> [M,D] of out_dtype."""
     bits = _tokens(tokens)
-    _same_device(tokens, Wq, s_w, out)
+    dev = _same_device(tokens, Wq, s_w, out)
     _group_table(Wq, s_w, V, D, group)
     out, ld_out = _token_rows(tokens, D, out, out_dtype, stream)
     _check(load().mkq_embedding_int4_group(_ptr(tokens), bits, tokens.numel(), _ptr(Wq), _ptr(s_w), int(group), V, D, float(scale),
-                                           _ptr(out), int(out_dtype), ld_out, _stream(stream)), "mkq_embedding_int4_group")
+                                           _ptr(out), int(out_dtype), ld_out, _stream_on(dev, stream)), "mkq_embedding_int4_group")
     return out
 
 
@@ -799,7 +817,7 @@ def mkq_embedding_gradient(tokens, dy, V: int, scale: float = 1.0, grad_dtype: i
     ld_dy = _rows(dy, "dy")
     M, D = dy.shape
     _need(tokens.numel() == M, "dy: a row for every token")
-    _same_device(tokens, dy, grad, workspace)
+    dev = _same_device(tokens, dy, grad, workspace)
     _need(grad is not None or not accumulate, "accumulate: needs the gradient to add to")
     if grad is None:
         grad, ld_grad = _new_matrix(V, D, _torch_dtype(grad_dtype), dy.device, stream), D
@@ -810,7 +828,7 @@ def mkq_embedding_gradient(tokens, dy, V: int, scale: float = 1.0, grad_dtype: i
         workspace = _new(mkq_embedding_gradient_workspace_bytes(M, D), torch.uint8, dy.device, stream)
     _check(load().mkq_embedding_gradient(_ptr(tokens), bits, M, _ptr(dy), _dtype_code(dy), ld_dy, V, D, float(scale), int(padding_token),
                                          int(accumulate), _ptr(grad), int(grad_dtype), ld_grad, _ptr(workspace), workspace.nbytes,
-                                         _stream(stream)), "mkq_embedding_gradient")
+                                         _stream_on(dev, stream)), "mkq_embedding_gradient")
     return grad
 
 
@@ -845,11 +863,11 @@ def mkq_gradient_norm(grads, norm_out=None, workspace=None, stream=None):
     """Norm over all values of a list of contiguous tensors (float32 / float16 / bfloat16, mixed) -> float32 tensor [1]."""
     grads = list(grads)
     counts, dtypes, at = _tensor_list(grads, "grads")
-    _same_device(grads[0], norm_out, workspace)
+    dev = _same_device(grads[0], norm_out, workspace)
     norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
     counts, codes = array("q", counts), array("i", map(_dtype_codes.__getitem__, dtypes))
     _check(load().mkq_gradient_norm(len(grads), at.buffer_info()[0], counts.buffer_info()[0], codes.buffer_info()[0], _ptr(norm_out),
-                                    _ptr(workspace), workspace.nbytes, _stream(stream)), "mkq_gradient_norm")
+                                    _ptr(workspace), workspace.nbytes, _stream_on(dev, stream)), "mkq_gradient_norm")
     return norm_out
 
 
@@ -858,7 +876,7 @@ def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, work
     norm before, float32 tensor [1]."""
     grads = list(grads)
     counts, dtypes, at = _tensor_list(grads, "grads")
-    _same_device(grads[0], norm_out, workspace)
+    dev = _same_device(grads[0], norm_out, workspace)
     out_at = at
     if outs is not None:
         outs = list(outs)
@@ -869,7 +887,7 @@ def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, work
     counts, codes = array("q", counts), array("i", map(_dtype_codes.__getitem__, dtypes))
     _check(load().mkq_clip_gradients(len(grads), at.buffer_info()[0], out_at.buffer_info()[0], counts.buffer_info()[0],
                                      codes.buffer_info()[0], float(max_norm), _ptr(norm_out), _ptr(workspace), workspace.nbytes,
-                                     _stream(stream)), "mkq_clip_gradients")
+                                     _stream_on(dev, stream)), "mkq_clip_gradients")
     return norm_out
 
 

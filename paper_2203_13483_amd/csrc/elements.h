@@ -53,18 +53,32 @@ __device__ __forceinline__ void get8(const typename E::raw *p, float (&v)[8])
     }
 }
 
-template <class E>
+// 16 bytes that this kernel does not touch again, past the caches where STREAM
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <bool STREAM>
+__device__ __forceinline__ void store16(void *p, uint4 v)
+{
+    if constexpr (STREAM) {
+        const u32x4 x = {v.x, v.y, v.z, v.w};
+        __builtin_nontemporal_store(x, static_cast<u32x4 *>(p));
+    } else {
+        *static_cast<uint4 *>(p) = v;
+    }
+}
+
+template <class E, bool STREAM = false>
 __device__ __forceinline__ void put8(typename E::raw *p, const float (&v)[8])
 {
     if constexpr (E::BYTES == 4) {
-        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+        for (int i = 0; i < 8; i += 4)
+            store16<STREAM>(p + i, make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])));
     } else {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             w[i] = std::is_same<E, ElemF16>::value ? pack2_f16(v[2 * i], v[2 * i + 1]) : pack2_bf16(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        store16<STREAM>(p, make_uint4(w[0], w[1], w[2], w[3]));
     }
 }
 

@@ -71,7 +71,8 @@ struct NibbleRow {
 };
 
 // threads_per_row neighbouring threads write a token's row, and ROWS of them at a time, so that as many tokens, then as many rows are
-// on their way together (65536 binary16 rows of 1024 one at a time 46 us).  VEC: D is a multiple of 8 and all rows of 16 bytes, a
+// on their way together.  Rows are written through the caches: past them 65536 binary16 rows of 1024 take 30 instead of 47 us, but with
+// the LayerNorm that reads them 99 instead of 97, 32768 rows 55 instead of 47.  VEC: D is a multiple of 8 and all rows of 16 bytes, a
 // thread has eight neighbouring values; otherwise eight that are threads_per_row apart.
 template <class Row, class O, bool VEC, int ROWS>
 __global__ __launch_bounds__(256) void lookup_kernel(const LookupParams p)

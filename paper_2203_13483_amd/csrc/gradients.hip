@@ -4,7 +4,7 @@
 //
 // Bound by HBM: every value is read once for the norm and once more, behind it, to be scaled and written.  Squares and their
 // sums are binary64, in an order that does not depend on which workgroup is done first, so the norm of gradients beyond
-// 1e19 does not overflow and equal inputs give equal bits.
+// 1e19 does not overflow and equal inputs give equal bits.  Measured: 81 million binary32 values 157 us (6.2 TB/s), 13 million 31 us.
 #include "elements.h"
 #include "gemm_common.h"
 
@@ -142,6 +142,8 @@ __global__ __launch_bounds__(256) void norm_kernel(const double *__restrict__ pa
     if (threadIdx.x == 0) *norm_out = (float)norm;
 }
 
+// Results go past the caches: left dirty there, they are written back under the next pass over as many bytes (81 million binary32
+// values clipped 189 -> 157 us, with an update that reads them behind it 352 -> 335; 13 million 31 and 31, 63 -> 59).
 template <class E>
 __device__ __forceinline__ void scale_values(const void *p, void *q, int64_t at, int values, float c)
 {
@@ -156,7 +158,7 @@ __device__ __forceinline__ void scale_values(const void *p, void *q, int64_t at,
 #pragma unroll
             for (int k = 0; k < decltype(n)::value; ++k) {
                 x[k].scale(c);
-                reinterpret_cast<uint4 *>(out)[v + k * 256] = x[k].raw;
+                store16<true>(reinterpret_cast<uint4 *>(out) + v + k * 256, x[k].raw);
             }
         },
         [&](int i) { out[i] = E::put(product(E::get(g[i]), c)); });
