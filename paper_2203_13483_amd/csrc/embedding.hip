@@ -293,29 +293,29 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(const SortPara
     };
     fetch(from);
     {
-        const int digit = tid % SORT_BINS, half = tid / SORT_BINS;  // (a half of the threads has every other workgroup's counts)
+        // digit tid % 2^bits, of every sharers-th workgroup: one round trip to memory for up to 8 sharers workgroups
+        const int digits = 1 << p.bits, digit = tid & (digits - 1), share = tid >> p.bits, sharers = SORT_THREADS >> p.bits;
+        if (tid < SORT_BINS) part[0][tid] = part[1][tid] = 0;
         uint32_t before = 0, all = 0;
-        for (int b = half; b < p.blocks; b += 32) {
-            uint32_t c[16];
+        for (int b = share; b < p.blocks; b += 8 * sharers) {
+            uint32_t c[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) c[i] = p.counts[(b + 2 * i < p.blocks ? b + 2 * i : b) * SORT_BINS + digit];
+            for (int i = 0; i < 8; ++i) c[i] = p.counts[(b + i * sharers < p.blocks ? b + i * sharers : b) * SORT_BINS + digit];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (b + 2 * i >= p.blocks) break;
-                all += c[i];
-                if (b + 2 * i < (int)blockIdx.x) before += c[i];
+            for (int i = 0; i < 8; ++i) {
+                const int from_block = b + i * sharers;
+                all += from_block < p.blocks ? c[i] : 0;
+                before += from_block < (int)blockIdx.x ? c[i] : 0;
             }
         }
-        if (half) {
-            part[0][digit] = before;
-            part[1][digit] = all;
-        }
+        __syncthreads();
+        atomicAdd(&part[0][digit], before);
+        atomicAdd(&part[1][digit], all);
         __syncthreads();
         uint32_t upto = 0;
-        if (!half) {  // sums over the digits: within a wave, then over the waves before
-            before += part[0][digit];
-            all += part[1][digit];
-            upto = all;
+        if (tid < SORT_BINS) {  // sums over the digits: within a wave, then over the waves before
+            before = part[0][tid];
+            all = upto = part[1][tid];
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const uint32_t v = __shfl_up(upto, off, 64);
@@ -324,9 +324,9 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(const SortPara
             if (lane == 63) sums[wave] = upto;
         }
         __syncthreads();
-        if (!half) {
+        if (tid < SORT_BINS) {
             for (int w = 0; w < wave; ++w) upto += sums[w];
-            start[digit] = upto - all + before;
+            start[tid] = upto - all + before;
         }
     }
     for (int64_t tile = from; tile < to; tile += SORT_TILE) {
@@ -625,6 +625,7 @@ static int launch_lookup(LookupParams p, bool table_vec, int out_dtype, hipStrea
 // Chunks of sorted positions: about a thousand workgroups of them, 8 to 64 rows each
 static int grad_chunk(int64_t M)
 {
+    if (M <= 64) return 64;  // one, which needs no joining
     int chunk = 8;
     while (chunk < 64 && M > (int64_t)chunk * 1024) chunk *= 2;
     return chunk;

@@ -9,9 +9,9 @@
 // (8 + 8 + 8 bits).
 //
 // Bound: the weights' bytes for few tokens, by the instructions that turn codes into operands from about 30 on.  Measured, us:
-// one token, K = 768, N = 30522, groups of 64 6.3 (2.1 TB/s); K = 8192, N = 28672, groups of 128: 1 token 31 (4.0 TB/s; the same loads
-// with the arithmetic left out 23.5), 16 tokens 34 (3.7), 32 tokens 43, 64 tokens 63 (475 TFLOP/s); 120 tokens, K = 1024,
-// N = 30522 15.9 (473 TFLOP/s).
+// one token, K = 768, N = 30522, groups of 64 6.2 (2.1 TB/s); K = 8192, N = 28672, groups of 128: 1 token 26 (4.8 TB/s; the same loads
+// with the arithmetic left out 23.5), 16 tokens 34 (3.7), 32 tokens 43, 64 tokens 53 (566 TFLOP/s); 120 tokens, K = 1024,
+// N = 30522 14.5 (516 TFLOP/s).
 #include <type_traits>
 
 #include "elements.h"
@@ -283,34 +283,34 @@ __device__ __forceinline__ void store_tile(const Group4Params &p, typename Tile<
 }
 
 // Steps of 128 codes between two hand-overs of activations: what 64 KB of LDS and eight vectors a thread allow
-template <class E, int G, int TN, int MT, int KS>
+template <class E, int G, int TN, int MT, int WAVES, int KS>
 struct Shape {
     static constexpr int PARTS = Product<E>::PARTS, ROWS = TN * MT;
     static constexpr int FIT = 65536 / (512 * KS * ROWS * PARTS);
     static constexpr int U = FIT >= 4 ? 4 : 2;
     static constexpr int KC = 128 * U, PITCH = KC * 2 + 16;  // (bytes; 16 more than a multiple of 128: no bank conflicts among rows)
-    static constexpr int VECTORS = (ROWS * (KC / 8) * KS + 255) / 256;
+    static constexpr int VECTORS = (ROWS * (KC / 8) * KS + 64 * WAVES - 1) / (64 * WAVES);
     // steps of a wave's channels for a chunk, and where they are in LDS: rows of an odd number of words (no bank conflicts)
-    static constexpr int SCALES = KC / G, SPITCH = SCALES | 1, SCALE_BYTES = 4 * TN * SPITCH * 4;
+    static constexpr int SCALES = KC / G, SPITCH = SCALES | 1, SCALE_BYTES = WAVES * TN * SPITCH * 4;
     static constexpr size_t lds(int rows)
     {
-        const size_t x = SCALE_BYTES + (size_t)2 * KS * PARTS * rows * PITCH, sums = KS > 1 ? (size_t)256 * MT * Tile<TN>::ACC * 4 : 0;
+        const size_t x = SCALE_BYTES + (size_t)2 * KS * PARTS * rows * PITCH, sums = KS > 1 ? (size_t)64 * WAVES * MT * Tile<TN>::ACC * 4 : 0;
         return x > sums ? x : sums;
     }
 };
 
-// Four waves; KS of them share the k loop of a tile (chunks of KC codes in turn) and their sums meet in LDS at the end; the
-// other 4 / KS tiles of the workgroup are neighbours and share the activations, which come through LDS, converted once, two
+// KS of the WAVES waves share the k loop of a tile (chunks of KC codes in turn) and their sums meet in LDS at the end; the
+// WAVES / KS tiles of the workgroup are neighbours and share the activations, which come through LDS, converted once, two
 // chunks in turn: one is multiplied while the next is on its way in registers.  Weights and steps go from memory to registers,
 // one chunk ahead.
-template <class E, int G, int TN, int MT, int KS>
-__global__ __launch_bounds__(256, TN == 16 ? (KS == 1 ? 4 : 3) : 2) void group4_kernel(const Group4Params p)
+template <class E, int G, int TN, int MT, int WAVES, int KS>
+__global__ __launch_bounds__(64 * WAVES, TN == 16 ? (WAVES == 8 || KS == 1 ? 4 : 3) : 2) void group4_kernel(const Group4Params p)
 {
-    using S = Shape<E, G, TN, MT, KS>;
+    using S = Shape<E, G, TN, MT, WAVES, KS>;
     using T = Tile<TN>;
     using P = Product<E>;
     using Acc = typename T::Acc;
-    constexpr int U = S::U, KC = S::KC, ACC = T::ACC, CG = 4 / KS, XT = 256 / KS;
+    constexpr int U = S::U, KC = S::KC, ACC = T::ACC, CG = WAVES / KS, XT = 64 * WAVES / KS, THREADS = 64 * WAVES;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nl = lane % TN, q = lane / TN;
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(256, TN == 16 ? (KS == 1 ? 4 : 3) : 2) void group4_
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int i = 0; i < ACC; ++i) part[(t * ACC + i) * 256 + tid] = total[t][i];
+            for (int i = 0; i < ACC; ++i) part[(t * ACC + i) * THREADS + tid] = total[t][i];
         lds_barrier();
         if (slice != 0) return;
 #pragma unroll
@@ -495,48 +495,53 @@ __global__ __launch_bounds__(256, TN == 16 ? (KS == 1 ? 4 : 3) : 2) void group4_
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int i = 0; i < ACC; ++i) total[t][i] += part[(t * ACC + i) * 256 + tid + s * XT];
+                for (int i = 0; i < ACC; ++i) total[t][i] += part[(t * ACC + i) * THREADS + tid + s * XT];
     }
     store_tile<TN, MT>(p, total, n, m0, rows, q);
 }
 
-template <class E, int G, int TN, int MT, int KS>
+template <class E, int G, int TN, int MT, int WAVES, int KS>
 static int launch_group4(Group4Params p, hipStream_t st)
 {
-    using S = Shape<E, G, TN, MT, KS>;
+    using S = Shape<E, G, TN, MT, WAVES, KS>;
     static_assert(S::lds(S::ROWS) <= 160 * 1024, "LDS is 160 KiB per CU");
     p.lds_rows = p.M < S::ROWS ? p.M : S::ROWS;
-    p.blocks_n = (int)ceil_div(p.N, TN * (4 / KS));
+    p.blocks_n = (int)ceil_div(p.N, TN * (WAVES / KS));
     const int64_t workgroups = (int64_t)p.blocks_n * ceil_div(p.M, S::ROWS);
-    if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
+    if (!grid_ok(workgroups, 64 * WAVES)) return MKQ_ERR_UNSUPPORTED;
     static PerDeviceOnce once;  // (more than 64 KB of LDS have to be asked for)
     if (once.get([]() -> int {
-            return hipFuncSetAttribute(reinterpret_cast<const void *>(&group4_kernel<E, G, TN, MT, KS>), hipFuncAttributeMaxDynamicSharedMemorySize,
+            return hipFuncSetAttribute(reinterpret_cast<const void *>(&group4_kernel<E, G, TN, MT, WAVES, KS>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)S::lds(S::ROWS)) == hipSuccess ? 1 : -1;
         }) <= 0)
         return MKQ_ERR_HIP;
-    group4_kernel<E, G, TN, MT, KS><<<(unsigned)workgroups, 256, S::lds(p.lds_rows), st>>>(p);
+    group4_kernel<E, G, TN, MT, WAVES, KS><<<(unsigned)workgroups, 64 * WAVES, S::lds(p.lds_rows), st>>>(p);
     return launch_status();
 }
 
-// Which tile, and how many waves share its k loop: the largest tile whose workgroups fill the chip, since a tile of more
-// tokens converts a code for more of them, and a k loop shared by fewer waves reads x fewer times.  us, binary16 (tile and
-// waves): one token, K = 768, N = 30522 6.4 (16, 1), 8.0 (16, 2); K = 4096, N = 16384 12.7 (16, 1), 10.9 (16, 2), 12.1 (16, 4);
-// K = N = 8192 21.3, 13.9, 11.8; 24 tokens, K = 8192, N = 28672 56.7 (16, 1), 41.2 (32, 1), 44.7 (32, 2); 64 tokens there 67.7
-// (32, 1), 63.4 (64, 1), but with K = N = 4096 14.4 (16, 1), 13.2 (16, 2), 24.1 (32, 1), 36.2 (64, 1); 128 tokens, K = N = 4096 22.5
-// (16, 1), 28.1 (32, 1), 20.4 (32, 2), but K = 1024 8.2, 12.1, 9.9.  binary32 has 16 tokens a tile: its three parts leave a larger tile
-// short chunks (64 tokens, K = 8192, N = 28672 197 and 172, K = 768, N = 30522 of 48 20.2 and 23.6).
+// Which tile, and how many of a workgroup's eight waves share its k loop: the largest tile whose workgroups fill the chip, since a tile
+// of more tokens converts a code for more of them, and channels that share a workgroup read x once.  us, binary16, tokens of a tile and
+// sharing waves: 120 tokens, K = 1024, N = 30522 14.5 (64, 1), 19.5 (64, 2), 20.8 (32, 2); 64 tokens, K = 8192, N = 28672 77.6 (64, 1), 53.1
+// (64, 2), 67.6 (32, 2), 94.9 (16, 2); 128 tokens, K = 4096, N = 8192 26.7 (64, 2), 19.5 (32, 2), 25.9 (32, 4), 35.6 (16, 4), K = 1024, N = 4096
+// 11.3, 8.8, 7.4, 10.0; 64 tokens, K = N = 4096 25.7 (64, 2), 13.3 (32, 4), 11.2 (16, 2), 10.9 (16, 4); one token, K = 768, N = 30522 6.2
+// (16, 2), 7.5 (16, 4), K = 4096, N = 16384 11.1 and 9.6.  Workgroups of four waves where even the last leave CUs idle: 16 tokens,
+// K = N = 4096 7.5 instead of 7.8, one token, K = N = 768 3.3 instead of 3.6.  binary32 has 16 tokens a tile: its three parts leave larger tiles
+// short chunks; 48 tokens, K = 768, N = 30522 17.0 (16, 1), 31.7 (16, 2), 16 tokens, K = 4096, N = 8192 27.8 and 19.8.
 template <class E, int G>
 static int choose_group4(const Group4Params &p, hipStream_t st)
 {
-    auto workgroups = [&](int tn, int mt, int ks) { return ceil_div(p.N, tn * (4 / ks)) * ceil_div(p.M, tn * mt); };
-    if constexpr (E::BYTES == 2) {
-        if (p.M > 32 && workgroups(32, 2, 1) >= 200) return launch_group4<E, G, 32, 2, 1>(p, st);
-        if (p.M > 16 && workgroups(32, 1, 1) >= 200) return launch_group4<E, G, 32, 1, 1>(p, st);
-        if (p.M > 16 && p.K >= 2048 && workgroups(32, 1, 2) >= 200) return launch_group4<E, G, 32, 1, 2>(p, st);
-        if (workgroups(16, 1, 1) < 300 && workgroups(16, 1, 2) < 400) return launch_group4<E, G, 16, 1, 4>(p, st);
+    auto workgroups = [&](int tokens, int channels) { return ceil_div(p.N, channels) * ceil_div(p.M, tokens); };
+    if constexpr (E::BYTES == 4) {
+        return workgroups(16, 128) >= 400 ? launch_group4<E, G, 16, 1, 8, 1>(p, st) : launch_group4<E, G, 16, 1, 8, 2>(p, st);
+    } else {
+        if (p.M > 32 && workgroups(64, 256) >= 200) return launch_group4<E, G, 32, 2, 8, 1>(p, st);
+        if (p.M > 32 && workgroups(64, 128) >= 200) return launch_group4<E, G, 32, 2, 8, 2>(p, st);
+        if (p.M > 16 && workgroups(32, 128) >= 200) return launch_group4<E, G, 32, 1, 8, 2>(p, st);
+        if (p.M > 16 && workgroups(32, 64) >= 200) return launch_group4<E, G, 32, 1, 8, 4>(p, st);
+        if (workgroups(16, 64) >= 400) return launch_group4<E, G, 16, 1, 8, 2>(p, st);
+        if (workgroups(16, 32) >= 200) return launch_group4<E, G, 16, 1, 8, 4>(p, st);
+        return launch_group4<E, G, 16, 1, 4, 4>(p, st);
     }
-    return workgroups(16, 1, 1) >= 300 ? launch_group4<E, G, 16, 1, 1>(p, st) : launch_group4<E, G, 16, 1, 2>(p, st);
 }
 
 static bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }

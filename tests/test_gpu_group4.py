@@ -125,7 +125,7 @@ def test_whole_numbers_are_exact(mkq, M, xt, group):
 
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("xt", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("M,N,K", [(3, 20003, 136), (16, 13001, 1030), (20, 26001, 392), (45, 26001, 160), (100, 25999, 520), (128, 3205, 2056), (130, 3250, 4100),
+@pytest.mark.parametrize("M,N,K", [(3, 20003, 136), (5, 25700, 264), (16, 13001, 1030), (20, 26001, 392), (45, 26001, 160), (100, 25999, 520), (128, 3205, 2056), (130, 3250, 4100),
                                    (16, 40, 4360), (7, 6500, 2056), (64, 4000, 1240)])
 def test_every_tile_is_exact_on_whole_numbers(mkq, M, N, K, xt, group):
     """As above where the grid is large enough for tiles of 32 and 64 tokens and for waves that share nothing, with K that ends
