@@ -430,7 +430,7 @@ int mkq_pack_weights_int4_group(const void *W, int w_dtype, int64_t N, int64_t K
  *     y[m,n] = sum_g s_w[n,g] ( sum_{k in g} x[m,k] c[n,k] ) + bias[n],  + residual, act, narrowed once to out_dtype
  * Activations and codes enter the products exactly (binary32 ones too), all sums are binary32.  Infinities and NaN in a row
  * of x reach that row of y, as in IEEE arithmetic on the dequantized weights.
- *   x     [M, K] of x_dtype (F32, F16, BF16), row stride ldx (any alignment of the rows: a multiple of 16 bytes is faster)
+ *   x     [M, K] of x_dtype (F32, F16, BF16), row stride ldx (any; K a multiple of 8 in rows of a multiple of 16 bytes is faster)
  *   Wq, s_w  from mkq_pack_weights_int4_group with the same group;  bias [N] binary32 or NULL
  *   out   [M, N] of out_dtype (F32, F16, BF16)
  *   epi   NULL, or act and residual (residual_dtype F32, F16 or BF16); its code and accumulator outputs: UNSUPPORTED
@@ -447,7 +447,7 @@ int mkq_linear_int4_group(const void *x, int x_dtype, int64_t ldx, const uint8_t
  *           mkq_pack_weights_int4_group (N = V, K = D): then a value is scale * (code * step), both products in binary32
  *   out     [M, D] of out_dtype (F32, F16, BF16), row stride ld_out (what lies between the rows is left as it is)
  *   scale   finite (sqrt(D) in some models, else 1)
- * Any D; rows that are multiples of 16 bytes are faster.  M == 0 is a no-op.
+ * Any D; multiples of 8 in rows that are multiples of 16 bytes are faster.  M == 0 is a no-op.
  * Errors: NULL, SHAPE, ALIGN, SCALE, DTYPE (token_bits too), UNSUPPORTED (V or D from about 2^31 on), HIP. */
 int mkq_embedding(const void *tokens, int token_bits, int64_t M, const void *table, int table_dtype, int64_t V, int64_t D,
                   int64_t ld_table, float scale, void *out, int out_dtype, int64_t ld_out, void *stream);
@@ -462,7 +462,8 @@ int mkq_embedding_int4_group(const void *tokens, int token_bits, int64_t M, cons
  * rounding to grad_dtype, behind the scale and the addition.
  *   dy    [M, D] of dy_dtype (F32, F16, BF16), row stride ld_dy
  *   grad  [V, D] of grad_dtype (F32, F16, BF16), row stride ld_grad (what lies between the rows is left as it is)
- *   workspace  at least mkq_embedding_gradient_workspace_bytes(M, D) bytes, 16-byte aligned; no preparation
+ *   workspace  at least mkq_embedding_gradient_workspace_bytes(M, D) bytes, 16-byte aligned; no preparation.  Two calls that may
+ *              run at the same time need two.
  * M == 0 writes the zeros only (no workspace needed).
  * Errors: NULL, SHAPE, ALIGN, SCALE, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
 size_t mkq_embedding_gradient_workspace_bytes(int64_t M, int64_t D);
@@ -476,10 +477,11 @@ int mkq_embedding_gradient(const void *tokens, int token_bits, int64_t M, const 
  *   grads_host, counts_host, dtypes_host   host arrays [n]: device pointers, numbers of values, F32 / F16 / BF16 each; a tensor
  *                 is contiguous and aligned to its own element size (16 bytes are faster); one without values may be NULL
  *   outs_host     host array [n] of device pointers; outs_host[t] == grads_host[t] clips in place, otherwise it overlaps no
- *                 gradient
+ *                 gradient; no two of them overlap (a tensor that is in the list twice would be scaled twice)
  *   norm_out      device, the norm before clipping, binary32
  *   max_norm      > 0 (infinity: copies only)
- *   workspace     at least mkq_gradient_norm_workspace_bytes(n) bytes, 16-byte aligned; no preparation
+ *   workspace     at least mkq_gradient_norm_workspace_bytes(n) bytes, 16-byte aligned; no preparation.  Two calls that may run
+ *                 at the same time need two.
  * A NaN among the gradients makes the norm and all results NaN; an infinity makes the norm infinite, c = 0 and itself NaN.
  * n == 0: the norm is 0.  Errors: NULL, SHAPE, ALIGN, SCALE, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
 size_t mkq_gradient_norm_workspace_bytes(int64_t n);

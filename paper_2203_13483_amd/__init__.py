@@ -883,6 +883,9 @@ def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, work
         out_counts, out_dtypes, out_at = _tensor_list(outs, "outs")
         _same_device(grads[0], outs[0])
         _need(out_counts == counts and out_dtypes == dtypes, "outs: the gradients' types and sizes")
+    if len(set(out_at)) != len(out_at):  # (tensors without values share an address)
+        written = [a for a, n in zip(out_at, counts) if n]
+        _need(len(set(written)) == len(written), "no tensor twice: it would be scaled twice")
     norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
     counts, codes = array("q", counts), array("i", map(_dtype_codes.__getitem__, dtypes))
     _check(load().mkq_clip_gradients(len(grads), at.buffer_info()[0], out_at.buffer_info()[0], counts.buffer_info()[0],

@@ -961,6 +961,7 @@ static int epilogue_scratch(const mkq_epilogue *epi, SplitKScratch *scr, bool *h
 
 namespace mkq {
 int setup_gemm_f16();  // gemm_f16.hip
+int setup_group4();  // group4.hip
 int setup_attention();  // attention.hip
 }
 
@@ -1033,6 +1034,7 @@ extern "C" int mkq_init(void)
     }
     if (rc == MKQ_OK) rc = setup_gemm_few();
     if (rc == MKQ_OK) rc = setup_gemm_f16();
+    if (rc == MKQ_OK) rc = setup_group4();
     if (rc == MKQ_OK) rc = setup_attention();
     if (rc == MKQ_OK) rc = setup_qkv_attention();
     if (rc == MKQ_OK) rc = setup_layer_tail();

@@ -10,7 +10,7 @@
 //
 // Bound: the weights' bytes for few tokens, by the instructions that turn codes into operands from about 30 on.  Measured, us:
 // one token, K = 768, N = 30522, groups of 64 6.2 (2.1 TB/s); K = 8192, N = 28672, groups of 128: 1 token 26 (4.8 TB/s; the same loads
-// with the arithmetic left out 23.5), 16 tokens 34 (3.7), 32 tokens 43, 64 tokens 53 (566 TFLOP/s); 120 tokens, K = 1024,
+// with the arithmetic left out 23.5), 16 tokens 33 (3.8), 32 tokens 43, 64 tokens 53 (566 TFLOP/s); 120 tokens, K = 1024,
 // N = 30522 14.5 (516 TFLOP/s).
 #include <type_traits>
 
@@ -74,6 +74,7 @@ struct Group4Params {
     int blocks_n;                 // workgroups along N
     int x_vec;                    // rows of x are multiples of 16 bytes, K of 8
     int lds_rows;                 // rows of x that a workgroup keeps: min(M, its tokens)
+    bool setup_only;              // host side only: do the kernel's once-per-device setup, launch nothing
 };
 
 // Eight codes of a word as the matrix instruction takes them.
@@ -94,15 +95,24 @@ __device__ __forceinline__ v8h codes_f16(uint32_t w)
     return __builtin_bit_cast(v8h, r);
 }
 
+// c / 16 of the code in the low nibble of byte BYTE.  (The byte is picked by the instruction itself; the compiler shifts first, for
+// seven of eight codes: 16 bfloat16 tokens, K = 8192, N = 28672 38 -> 36.5 us.)
+template <int BYTE>
+__device__ __forceinline__ float code_of_byte(uint32_t w)
+{
+    float r;
+    if constexpr (BYTE == 0) asm("v_cvt_off_f32_i4_e32 %0, %1" : "=v"(r) : "v"(w));
+    if constexpr (BYTE == 1) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(r) : "v"(w));
+    if constexpr (BYTE == 2) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(r) : "v"(w));
+    if constexpr (BYTE == 3) asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(r) : "v"(w));
+    return r;
+}
 __device__ __forceinline__ v8b codes_bf16(uint32_t w)
 {
-    uint32_t r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float a = __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (8 * i)));
-        const float b = __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (8 * i + 4)));
-        r[i] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-    }
+    const uint32_t odd = w >> 4;
+    auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+    const uint32_t r[4] = {pair(code_of_byte<0>(w), code_of_byte<0>(odd)), pair(code_of_byte<1>(w), code_of_byte<1>(odd)),
+                           pair(code_of_byte<2>(w), code_of_byte<2>(odd)), pair(code_of_byte<3>(w), code_of_byte<3>(odd))};
     return __builtin_bit_cast(v8b, r);
 }
 
@@ -304,7 +314,7 @@ struct Shape {
 // chunks in turn: one is multiplied while the next is on its way in registers.  Weights and steps go from memory to registers,
 // one chunk ahead.
 template <class E, int G, int TN, int MT, int WAVES, int KS>
-__global__ __launch_bounds__(64 * WAVES, TN == 16 ? (WAVES == 8 || KS == 1 ? 4 : 3) : 2) void group4_kernel(const Group4Params p)
+__global__ __launch_bounds__(64 * WAVES, TN == 16 ? (WAVES >= 8 || KS == 1 ? 4 : 3) : 2) void group4_kernel(const Group4Params p)
 {
     using S = Shape<E, G, TN, MT, WAVES, KS>;
     using T = Tile<TN>;
@@ -508,23 +518,27 @@ static int launch_group4(Group4Params p, hipStream_t st)
     p.lds_rows = p.M < S::ROWS ? p.M : S::ROWS;
     p.blocks_n = (int)ceil_div(p.N, TN * (WAVES / KS));
     const int64_t workgroups = (int64_t)p.blocks_n * ceil_div(p.M, S::ROWS);
-    if (!grid_ok(workgroups, 64 * WAVES)) return MKQ_ERR_UNSUPPORTED;
+    if (!p.setup_only && !grid_ok(workgroups, 64 * WAVES)) return MKQ_ERR_UNSUPPORTED;
     static PerDeviceOnce once;  // (more than 64 KB of LDS have to be asked for)
     if (once.get([]() -> int {
             return hipFuncSetAttribute(reinterpret_cast<const void *>(&group4_kernel<E, G, TN, MT, WAVES, KS>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)S::lds(S::ROWS)) == hipSuccess ? 1 : -1;
         }) <= 0)
         return MKQ_ERR_HIP;
+    if (p.setup_only) return MKQ_OK;
     group4_kernel<E, G, TN, MT, WAVES, KS><<<(unsigned)workgroups, 64 * WAVES, S::lds(p.lds_rows), st>>>(p);
     return launch_status();
 }
 
-// Which tile, and how many of a workgroup's eight waves share its k loop: the largest tile whose workgroups fill the chip, since a tile
+// Which tile, and how many of a workgroup's waves (eight) share its k loop: the largest tile whose workgroups fill the chip, since a tile
 // of more tokens converts a code for more of them, and channels that share a workgroup read x once.  us, binary16, tokens of a tile and
 // sharing waves: 120 tokens, K = 1024, N = 30522 14.5 (64, 1), 19.5 (64, 2), 20.8 (32, 2); 64 tokens, K = 8192, N = 28672 77.6 (64, 1), 53.1
 // (64, 2), 67.6 (32, 2), 94.9 (16, 2); 128 tokens, K = 4096, N = 8192 26.7 (64, 2), 19.5 (32, 2), 25.9 (32, 4), 35.6 (16, 4), K = 1024, N = 4096
 // 11.3, 8.8, 7.4, 10.0; 64 tokens, K = N = 4096 25.7 (64, 2), 13.3 (32, 4), 11.2 (16, 2), 10.9 (16, 4); one token, K = 768, N = 30522 6.2
-// (16, 2), 7.5 (16, 4), K = 4096, N = 16384 11.1 and 9.6.  Workgroups of four waves where even the last leave CUs idle: 16 tokens,
+// (16, 2), 7.5 (16, 4), K = 4096, N = 16384 11.1 and 9.6.  Sixteen waves where x is much of what is read: K = 8192, N = 28672 16 tokens 33.5
+// instead of 35.2, 8 tokens 32.0 instead of 32.8, but one token 28.5 instead of 27.6; and eight of them on one k loop where that is
+// long: one token, K = 28672, N = 8192 30.7 instead of 37.8, K = N = 8192 10.3 instead of 11.3, but K = 4096, N = 16384 12.1 instead of 9.6.
+// Workgroups of four waves where even the last leave CUs idle: 16 tokens,
 // K = N = 4096 7.5 instead of 7.8, one token, K = N = 768 3.3 instead of 3.6.  binary32 has 16 tokens a tile: its three parts leave larger tiles
 // short chunks; 48 tokens, K = 768, N = 30522 17.0 (16, 1), 31.7 (16, 2), 16 tokens, K = 4096, N = 8192 27.8 and 19.8.
 template <class E, int G>
@@ -538,8 +552,9 @@ static int choose_group4(const Group4Params &p, hipStream_t st)
         if (p.M > 32 && workgroups(64, 128) >= 200) return launch_group4<E, G, 32, 2, 8, 2>(p, st);
         if (p.M > 16 && workgroups(32, 128) >= 200) return launch_group4<E, G, 32, 1, 8, 2>(p, st);
         if (p.M > 16 && workgroups(32, 64) >= 200) return launch_group4<E, G, 32, 1, 8, 4>(p, st);
+        if (p.M > 4 && workgroups(16, 128) >= 200) return launch_group4<E, G, 16, 1, 16, 2>(p, st);
         if (workgroups(16, 64) >= 400) return launch_group4<E, G, 16, 1, 8, 2>(p, st);
-        if (workgroups(16, 32) >= 200) return launch_group4<E, G, 16, 1, 8, 4>(p, st);
+        if (workgroups(16, 32) >= 200) return p.K >= 8192 ? launch_group4<E, G, 16, 1, 16, 8>(p, st) : launch_group4<E, G, 16, 1, 8, 4>(p, st);
         return launch_group4<E, G, 16, 1, 4, 4>(p, st);
     }
 }
@@ -552,6 +567,33 @@ static void with_group(int group, F &&f)
     if (group == 32) f(std::integral_constant<int, 32>());
     else if (group == 64) f(std::integral_constant<int, 64>());
     else f(std::integral_constant<int, 128>());
+}
+
+// Once-per-device setup of every tile (mkq_init)
+int setup_group4()
+{
+    Group4Params p = {};
+    p.M = p.N = p.K = 1;
+    p.setup_only = true;
+    int rc = MKQ_OK;
+    auto all = [&](auto... statuses) { ((rc = rc == MKQ_OK ? statuses : rc), ...); };
+    for (int dtype : {MKQ_F32, MKQ_F16, MKQ_BF16})
+        for (int group : {32, 64, 128})
+            with_elem(dtype, [&](auto e) {
+                with_group(group, [&](auto g) {
+                    using E = decltype(e);
+                    constexpr int G = decltype(g)::value;
+                    if constexpr (E::BYTES == 4)
+                        all(launch_group4<E, G, 16, 1, 8, 1>(p, nullptr), launch_group4<E, G, 16, 1, 8, 2>(p, nullptr));
+                    else
+                        all(launch_group4<E, G, 32, 2, 8, 1>(p, nullptr), launch_group4<E, G, 32, 2, 8, 2>(p, nullptr),
+                            launch_group4<E, G, 32, 1, 8, 2>(p, nullptr), launch_group4<E, G, 32, 1, 8, 4>(p, nullptr),
+                            launch_group4<E, G, 16, 1, 16, 2>(p, nullptr), launch_group4<E, G, 16, 1, 8, 2>(p, nullptr),
+                            launch_group4<E, G, 16, 1, 16, 8>(p, nullptr), launch_group4<E, G, 16, 1, 8, 4>(p, nullptr),
+                            launch_group4<E, G, 16, 1, 4, 4>(p, nullptr));
+                });
+            });
+    return rc;
 }
 
 }  // namespace mkq

@@ -197,6 +197,32 @@ def test_gradient_rows_with_gaps(mkq, ld_y, ld_g, accumulate):
         assert bool((room[:V, D:] == -5).all()) and bool((room[V] == -5).all())
 
 
+def test_gradient_past_32_bits(mkq):
+    """A gradient, then gradients' rows, of more than 2^31 values"""
+    V, D = 70000, 32768
+    t = torch.tensor([0, 69999, 65536, 69999, 1])
+    dy = torch.randint(-9, 10, (5, D), generator=torch.Generator().manual_seed(1)).half()
+    grad = torch.full((V, D), 3.0, dtype=torch.float16, device="cuda")
+    mkq.mkq_embedding_gradient(t.cuda(), dy.cuda(), V, 1.0, mkq.MKQ_F16, grad=grad)
+    rows = {0: dy[0], 69999: dy[1] + dy[3], 65536: dy[2], 1: dy[4]}
+    for r, want in rows.items():
+        assert torch.equal(grad[r].cpu(), want)
+    counts = torch.count_nonzero(grad, dim=1).cpu()
+    assert all(int(counts[r]) == int(torch.count_nonzero(w)) for r, w in rows.items()) and int(counts.sum()) == sum(int(torch.count_nonzero(w)) for w in rows.values())
+    del grad
+    M = 70000
+    t = torch.arange(M) % 3
+    dy = torch.zeros(M, D, dtype=torch.float16, device="cuda")
+    dy[::1000, 5] = 2.0
+    dy[M - 1] = 1.0
+    got = mkq.mkq_embedding_gradient(t.cuda(), dy, 4)
+    want = torch.zeros(4, D)
+    for i in range(0, M, 1000):
+        want[i % 3, 5] += 2.0
+    want[(M - 1) % 3] += 1.0
+    assert torch.equal(got.cpu(), want)
+
+
 def test_gradient_of_no_tokens(mkq):
     grad = torch.full((9, 20), 4.0, device="cuda")
     t, dy = torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, 20, device="cuda")

@@ -126,3 +126,25 @@ def test_other_stream(mkq):
     norm = mkq.mkq_clip_gradients(ts, 1.0, stream=side)
     side.synchronize()
     assert float(norm) > 1 and abs(true_norm(ts) - 1.0) < 2e-3
+
+
+def test_a_tensor_twice(mkq):
+    """Counted twice by the norm; refused where it would be scaled twice"""
+    t = torch.full((100,), 3.0, device="cuda")
+    assert abs(float(mkq.mkq_gradient_norm([t, t])) - 30 * math.sqrt(2)) < 1e-5
+    with pytest.raises(ValueError):
+        mkq.mkq_clip_gradients([t, t], 1.0)
+    with pytest.raises(ValueError):
+        mkq.mkq_clip_gradients([t, t.clone()], 1.0, outs=[t, t])
+    assert bool((t == 3).all())
+
+
+def test_more_than_32_bits_of_values(mkq):
+    n = 2 ** 31 + 12345
+    t = torch.zeros(n, dtype=torch.float16, device="cuda")
+    at = torch.tensor([0, 1, 2 ** 31 - 1, 2 ** 31, n - 1], device="cuda")
+    t[at] = torch.tensor([3.0, 4.0, 12.0, 84.0, 3612.0], device="cuda").half()
+    true = math.sqrt(9 + 16 + 144 + 84 ** 2 + 3612 ** 2)  # 3613
+    assert abs(float(mkq.mkq_clip_gradients([t], 361.3)) - true) < 2.0 ** -23 * true
+    want = torch.tensor([3.0, 4.0, 12.0, 84.0, 3612.0]).double() * 0.1
+    assert bool(((t[at].cpu().double() - want).abs() <= 2.0 ** -10 * want).all()) and int((t != 0).sum()) == 5

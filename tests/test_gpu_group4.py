@@ -126,7 +126,7 @@ def test_whole_numbers_are_exact(mkq, M, xt, group):
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("xt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("M,N,K", [(3, 20003, 136), (5, 25700, 264), (16, 13001, 1030), (20, 26001, 392), (45, 26001, 160), (100, 25999, 520), (128, 3205, 2056), (130, 3250, 4100),
-                                   (16, 40, 4360), (7, 6500, 2056), (64, 4000, 1240)])
+                                   (16, 40, 4360), (7, 6500, 2056), (2, 6401, 8200), (9, 25601, 300), (64, 4000, 1240)])
 def test_every_tile_is_exact_on_whole_numbers(mkq, M, N, K, xt, group):
     """As above where the grid is large enough for tiles of 32 and 64 tokens and for waves that share nothing, with K that ends
     within a chunk, within a step and within a piece"""
@@ -215,6 +215,21 @@ def test_large(mkq, M, N, K, xt):
     codes = torch.stack((b % 16, b // 16), -1).flatten(1)
     codes = torch.where(codes > 7, codes - 16, codes)
     check(got[:, rows.cuda()], x.cpu(), codes, s[rows.cuda()].cpu(), group)
+
+
+def test_weights_past_32_bits(mkq):
+    """More than 2^32 bytes of weights: the first and last channels, exact on whole numbers"""
+    N, K, group = 70000, 131072, 128
+    g = torch.Generator("cuda").manual_seed(3)
+    Wq = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda", generator=g)
+    s = 2.0 ** torch.randint(-2, 2, (N, K // group), device="cuda", generator=g).float()
+    x = torch.randint(-3, 4, (2, K), device="cuda", generator=g).half()
+    got = mkq.mkq_linear_int4_group(x, Wq, s, None, N, K, group, mkq.MKQ_F32)
+    rows = torch.tensor([0, 1, 32767, 32768, 65535, 65536, 69999], device="cuda")
+    b = Wq[rows].long()
+    codes = torch.stack((b % 16, b // 16), -1).flatten(1)
+    w = torch.where(codes > 7, codes - 16, codes).double() * s[rows].double().repeat_interleave(group, 1)
+    assert torch.equal(got[:, rows].double(), x.double() @ w.T.contiguous())
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
