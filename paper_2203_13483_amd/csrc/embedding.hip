@@ -585,7 +585,7 @@ __global__ __launch_bounds__(256) void join_runs_kernel(const GradParams p)
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
-constexpr int64_t MAX_ROWS = 0x7FFFFFF0;
+constexpr int64_t MAX_ROWS = 0x7FFFFFF0, MAX_COLUMNS = 0x7FFF0000;  // (columns are counted up in ints, past the last by up to 2048)
 
 static bool finite(float v) { return v - v == 0.0f; }
 static bool tokens_aligned(const void *p, int bits) { return reinterpret_cast<uintptr_t>(p) % (bits / 8) == 0; }
@@ -671,7 +671,7 @@ extern "C" int mkq_embedding(const void *tokens, int token_bits, int64_t M, cons
     if (M == 0) return MKQ_OK;
     if (!tokens || !table || !out) return MKQ_ERR_NULL;
     if (!tokens_aligned(tokens, token_bits) || !aligned16(table) || !aligned16(out)) return MKQ_ERR_ALIGN;
-    if (V > MAX_ROWS || D > MAX_ROWS) return MKQ_ERR_UNSUPPORTED;
+    if (V > MAX_ROWS || D > MAX_COLUMNS) return MKQ_ERR_UNSUPPORTED;
     const LookupParams p = {tokens, table, nullptr, out, M, ld_table, ld_out, (uint32_t)V, (int)D, 0, 0, token_bits, 0, scale};
     const hipStream_t st = as_stream(stream);
     int status = MKQ_OK;
@@ -688,7 +688,7 @@ extern "C" int mkq_embedding_int4_group(const void *tokens, int token_bits, int6
     if (M == 0) return MKQ_OK;
     if (!tokens || !Wq || !s_w || !out) return MKQ_ERR_NULL;
     if (!tokens_aligned(tokens, token_bits) || !aligned16(Wq) || !aligned4(s_w) || !aligned16(out)) return MKQ_ERR_ALIGN;
-    if (V > MAX_ROWS || D > MAX_ROWS) return MKQ_ERR_UNSUPPORTED;
+    if (V > MAX_ROWS || D > MAX_COLUMNS) return MKQ_ERR_UNSUPPORTED;
     const LookupParams p = {tokens, Wq, s_w, out, M, ceil_div(D, 32) * 4, ld_out, (uint32_t)V, (int)D, (int)ceil_div(D, group),
                             group == 32 ? 5 : group == 64 ? 6 : 7, token_bits, 0, scale};
     return launch_lookup<NibbleRow>(p, true, out_dtype, as_stream(stream));
@@ -696,7 +696,7 @@ extern "C" int mkq_embedding_int4_group(const void *tokens, int token_bits, int6
 
 extern "C" size_t mkq_embedding_gradient_workspace_bytes(int64_t M, int64_t D)
 {
-    if (M <= 0 || D <= 0 || M > MAX_ROWS || D > MAX_ROWS) return 0;
+    if (M <= 0 || D <= 0 || M > MAX_ROWS || D > MAX_COLUMNS) return 0;
     return grad_workspace(M, D).total;
 }
 
@@ -709,7 +709,7 @@ extern "C" int mkq_embedding_gradient(const void *tokens, int token_bits, int64_
     if (!finite(scale)) return MKQ_ERR_SCALE;
     if (!grad || (M > 0 && (!tokens || !dy))) return MKQ_ERR_NULL;
     if ((M > 0 && (!tokens_aligned(tokens, token_bits) || !aligned16(dy))) || !aligned16(grad)) return MKQ_ERR_ALIGN;
-    if (M > MAX_ROWS || V > MAX_ROWS || D > MAX_ROWS) return MKQ_ERR_UNSUPPORTED;
+    if (M > MAX_ROWS || V > MAX_ROWS || D > MAX_COLUMNS) return MKQ_ERR_UNSUPPORTED;
     const hipStream_t st = as_stream(stream);
     GradParams g = {};
     g.dy = dy;

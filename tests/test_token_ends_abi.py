@@ -67,6 +67,8 @@ def test_lookup_refusals(lib):
         assert f(out=ODD) == f(t=VERY_ODD) == f(t=ODD, bits=64) == mkq.MKQ_ERR_ALIGN
         assert f(scale=float("nan")) == f(scale=float("inf")) == mkq.MKQ_ERR_SCALE
         assert f(V=2 ** 31) == mkq.MKQ_ERR_UNSUPPORTED
+        wide = dict(D=2 ** 31 - 1000, ldo=2 ** 31)
+        assert f(**(wide if f is look4 else dict(wide, ldt=2 ** 31))) == mkq.MKQ_ERR_UNSUPPORTED
         assert f(M=0, t=None, out=None) == mkq.MKQ_OK
     assert look(table=None) == look4(Wq=None) == look4(s_w=None) == mkq.MKQ_ERR_NULL
     assert look(dt=mkq.MKQ_I4) == mkq.MKQ_ERR_DTYPE and look(ldt=63) == mkq.MKQ_ERR_SHAPE and look4(group=8) == mkq.MKQ_ERR_SHAPE
@@ -86,7 +88,8 @@ def test_table_gradient_refusals(lib):
     assert grad(dy=ODD) == grad(g=ODD) == grad(t=VERY_ODD) == grad(t=ODD, bits=64) == grad(ws=ODD) == mkq.MKQ_ERR_ALIGN
     assert grad(scale=float("nan")) == mkq.MKQ_ERR_SCALE
     assert grad(ws=None) == grad(nb=need - 1) == mkq.MKQ_ERR_WORKSPACE
-    assert grad(V=2 ** 31) == grad(M=2 ** 31) == mkq.MKQ_ERR_UNSUPPORTED
+    assert grad(V=2 ** 31) == grad(M=2 ** 31) == grad(D=2 ** 31 - 1000, ldy=2 ** 31, ldg=2 ** 31) == mkq.MKQ_ERR_UNSUPPORTED
+    assert lib.mkq_embedding_gradient_workspace_bytes(4, 2 ** 31 - 1000) == 0
 
 
 def test_clip_refusals(lib):
