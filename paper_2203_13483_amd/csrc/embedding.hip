@@ -141,9 +141,15 @@ __device__ __forceinline__ void zero_rows(const ZeroParams &z)
     const int64_t threads = (int64_t)(gridDim.x - z.first) * blockDim.x, t = (int64_t)(blockIdx.x - z.first) * blockDim.x + threadIdx.x;
     uint8_t *const base = static_cast<uint8_t *>(z.grad) + z.rows_from * z.ld * z.bytes;
     const int64_t rows = z.rows_to - z.rows_from;
-    if (z.ld == z.D && z.vec) {
-        const int64_t total = rows * z.D * z.bytes / 16;
-        for (int64_t i = t; i < total; i += threads) reinterpret_cast<uint4 *>(base)[i] = make_uint4(0, 0, 0, 0);
+    if (z.ld == z.D) {  // one piece of memory, whatever its rows: 16 bytes a store between its first and last multiple of 16
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(base), end = begin + (uintptr_t)(rows * z.D * z.bytes);
+        const uintptr_t inner = (begin + 15) / 16 * 16, outer = end / 16 * 16;
+        for (uintptr_t p = inner + 16 * (uintptr_t)t; p < outer; p += 16 * (uintptr_t)threads) *reinterpret_cast<uint4 *>(p) = make_uint4(0, 0, 0, 0);
+        if (t < 16) {  // (two bytes each: up to seven before and seven behind, all of it where it is shorter)
+            const uintptr_t head = begin + 2 * (uintptr_t)t, tail = (outer > begin ? outer : begin) + 2 * (uintptr_t)t;
+            if (head < inner && head < end) *reinterpret_cast<uint16_t *>(head) = 0;
+            if (tail < end) *reinterpret_cast<uint16_t *>(tail) = 0;
+        }
         return;
     }
     const int per = z.vec ? 16 / z.bytes : 1, units = (z.D + per - 1) / per;
@@ -171,7 +177,7 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(const ZeroParams z) { ze
 // (least significant digit first, up to nine bits a pass).  A gradient of V = 30522, D = 768, us: 12000 tokens 39.6 counted directly, 16384
 // 56.8, sorted by digits 51.7.
 constexpr int SORT_BINS = 512, SORT_THREADS = 1024, SORT_WAVES = 16, SORT_ROUNDS = 2, SORT_TILE = SORT_THREADS * SORT_ROUNDS, SORT_BLOCKS = 256;
-constexpr int RANK_MAX = 12288, RANK_KEYS = 64, RANK_THREADS = 1024;
+constexpr int RANK_MAX = 12288, RANK_FEW = 4096, RANK_THREADS = 1024;
 
 struct SortParams {
     const void *tokens;
@@ -193,9 +199,12 @@ __device__ __forceinline__ uint32_t sort_key(const SortParams &p, int i)
     return t >= 0 && t < (int64_t)p.V && t != p.padding ? (uint32_t)t : p.V;
 }
 
-// A lane per position, 64 of them a workgroup, whose 16 waves share all M keys: two operations for a pair.  Keys behind a
-// workgroup's own count if they are smaller, keys before it also if they are equal.
-template <class I>
+// KEYS positions a workgroup, whose 16 waves share all M keys, and in a wave 64 / KEYS lanes share a position's: two operations
+// for a pair of keys.  Every workgroup reads all tokens, so few positions a workgroup suit short batches, which would leave most CUs
+// without any, and many the longer ones.  16 | 64, a whole gradient of V = 2000, D = 768, us: 100 tokens 8.9 | 11.2, 2048 13.1 | 16.4,
+// 4096 15.5 | 19.8, 12000 35.7 | 33.4; V = 30522, with the zeros of 27000 rows beside it: 4096 27.1 | 28.1, 6000 36.1 | 30.9,
+// 12000 51.1 | 42.3.  Keys behind a workgroup's group of 64 count if they are smaller, keys before it also if they are equal.
+template <class I, int KEYS>
 __global__ __launch_bounds__(RANK_THREADS) void rank_kernel(const SortParams p)
 {
     if (blockIdx.x >= p.zero.first) {
@@ -203,24 +212,33 @@ __global__ __launch_bounds__(RANK_THREADS) void rank_kernel(const SortParams p)
         return;
     }
     __shared__ __attribute__((aligned(16))) uint32_t keys[RANK_MAX];
-    __shared__ uint32_t part[RANK_THREADS / 64][RANK_KEYS];
+    __shared__ uint32_t part[RANK_THREADS / 64][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int groups = (p.M + 63) / 64, own = blockIdx.x;
-    for (int i = tid; i < groups * 64; i += RANK_THREADS) keys[i] = i < p.M ? sort_key<I, true>(p, i) : 0xFFFFFFFFu;
+    const int groups = (p.M + 63) / 64, own = blockIdx.x * KEYS / 64;
+    for (int i = tid; i < groups * 64; i += 4 * RANK_THREADS) {  // (four on their way at a time)
+        uint32_t k[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = i + j * RANK_THREADS < p.M ? sort_key<I, true>(p, i + j * RANK_THREADS) : 0xFFFFFFFFu;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + j * RANK_THREADS < groups * 64) keys[i + j * RANK_THREADS] = k[j];
+    }
     __syncthreads();
-    const uint32_t key = keys[own * 64 + lane];
+    const int mine = blockIdx.x * KEYS + lane % KEYS, sharer = lane / KEYS;
+    const uint32_t key = keys[mine];
     uint32_t count = 0;
     for (int g = wave; g < groups; g += RANK_THREADS / 64) {
-        const uint4 *at = reinterpret_cast<const uint4 *>(keys + g * 64);
+        const int first = g * 64 + sharer * KEYS;
+        const uint4 *at = reinterpret_cast<const uint4 *>(keys + first);
         if (g == own) {
-            for (int j = 0; j < 64; ++j) {
-                const uint32_t k = keys[g * 64 + j];
-                count += k < key || (k == key && j < lane);
+            for (int j = 0; j < KEYS; ++j) {
+                const uint32_t k = keys[first + j];
+                count += k < key || (k == key && first + j < mine);
             }
         } else {
             const uint32_t limit = g < own ? key + 1 : key;  // (keys are at most V < 2^31, but for the places behind M, which nobody asks for)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
+            for (int j = 0; j < KEYS / 4; ++j) {
                 const uint4 k = at[j];
                 count += k.x < limit;
                 count += k.y < limit;
@@ -231,11 +249,14 @@ __global__ __launch_bounds__(RANK_THREADS) void rank_kernel(const SortParams p)
     }
     part[wave][lane] = count;
     __syncthreads();
-    if (wave != 0 || own * 64 + lane >= p.M) return;
+    if (wave != 0) return;
 #pragma unroll
     for (int w = 1; w < RANK_THREADS / 64; ++w) count += part[w][lane];
+#pragma unroll
+    for (int d = KEYS; d < 64; d *= 2) count += __shfl_xor(count, d, 64);
+    if (sharer != 0 || mine >= p.M) return;
     p.keys_out[count] = key;
-    p.order_out[count] = (uint32_t)(own * 64 + lane);
+    p.order_out[count] = (uint32_t)mine;
 }
 
 template <class I, bool FIRST>
@@ -415,7 +436,7 @@ __device__ __forceinline__ void write_row8(const GradParams &p, uint32_t row, in
 template <class E, class O, bool VEC, bool ADD>
 __global__ __launch_bounds__(256) void sum_runs_kernel(const GradParams p)
 {
-    constexpr int AHEAD = !VEC ? 2 : E::BYTES == 4 ? 4 : 8;
+    constexpr int AHEAD = VEC && E::BYTES == 2 ? 8 : 4;
     constexpr uint32_t NONE = 0xFFFFFFFFu;
     struct alignas(16) Eight {
         typename E::raw v[8];
@@ -559,7 +580,10 @@ __global__ __launch_bounds__(256) void join_runs_kernel(const GradParams p)
         u1 = u0 + per < units ? u0 + per : units;
     }
     for (; u0 < u1; u0 += 256) {
-        const int tx = u1 - u0 < 256 ? u1 - u0 : 256, sharers = 256 / tx;
+        const int tx = u1 - u0 < 256 ? u1 - u0 : 256;
+        int sharers = 256 / tx;  // (no more than there are chunks for, and their sums are added one by one: all 51 of 39 columns took 8 us more)
+        sharers = sharers < 32 ? sharers : 32;
+        sharers = sharers < last - c + 1 ? sharers : last - c + 1;
         const int r = tid / tx, u = u0 + tid - r * tx;
         float sum[8] = {};
         if (r < sharers) {
@@ -622,12 +646,14 @@ static int launch_lookup(LookupParams p, bool table_vec, int out_dtype, hipStrea
     return launch_status();
 }
 
-// Chunks of sorted positions: about a thousand workgroups of them, 8 to 64 rows each
-static int grad_chunk(int64_t M)
+// Waves that sum a chunk, eight columns a lane
+static int grad_waves(int64_t D) { return D > 1536 ? 4 : (int)ceil_div(D, 512); }
+// Sorted positions of a chunk: 8 to 64, about 2000 waves of them.  (Half as many waves: 16453 bfloat16 rows of 429 20.5 instead of 13.2 us.)
+static int grad_chunk(int64_t M, int64_t D)
 {
     if (M <= 64) return 64;  // one, which needs no joining
     int chunk = 8;
-    while (chunk < 64 && M > (int64_t)chunk * 1024) chunk *= 2;
+    while (chunk < 64 && M * grad_waves(D) > (int64_t)chunk * 2048) chunk *= 2;
     return chunk;
 }
 
@@ -644,7 +670,7 @@ static GradWorkspace grad_workspace(int64_t M, int64_t D)
         at += (bytes + 255) / 256 * 256;
         return here;
     };
-    w.chunk = grad_chunk(M);
+    w.chunk = grad_chunk(M, D);
     w.chunks = (int)ceil_div(M, w.chunk);
     w.pitch = (int)(ceil_div(D, 8) * 8);
     for (int i = 0; i < 2; ++i) {
@@ -754,11 +780,20 @@ extern "C" int mkq_embedding_gradient(const void *tokens, int token_bits, int64_
     s.counts = reinterpret_cast<uint32_t *>(ws + w.counts);
     unsigned zeros;
     if (M <= RANK_MAX) {
-        const unsigned blocks = (unsigned)ceil_div(M, RANK_KEYS);
         s.keys_out = reinterpret_cast<uint32_t *>(ws + w.keys[0]);
         s.order_out = reinterpret_cast<uint32_t *>(ws + w.order[0]);
-        s.zero = zero_share(0, 1, blocks, RANK_THREADS, &zeros);
-        with_index(token_bits, [&](auto i) { rank_kernel<decltype(i)><<<blocks + zeros, RANK_THREADS, 0, st>>>(s); });
+        with_index(token_bits, [&](auto i) {
+            auto rank = [&](auto keys) {
+                constexpr int KEYS = decltype(keys)::value;
+                const unsigned blocks = (unsigned)ceil_div(M, KEYS);
+                s.zero = zero_share(0, 1, blocks, RANK_THREADS, &zeros);
+                rank_kernel<decltype(i), KEYS><<<blocks + zeros, RANK_THREADS, 0, st>>>(s);
+            };
+            if (M <= RANK_FEW)
+                rank(std::integral_constant<int, 16>());
+            else
+                rank(std::integral_constant<int, 64>());
+        });
     } else {
         s.per_block = (int)(ceil_div(ceil_div(M, SORT_BLOCKS), SORT_TILE) * SORT_TILE);
         s.blocks = (int)ceil_div(M, s.per_block);
@@ -791,7 +826,7 @@ extern "C" int mkq_embedding_gradient(const void *tokens, int token_bits, int64_
     g.chunks = w.chunks;
     g.pitch = w.pitch;
     const unsigned join_workgroups = (unsigned)(g.chunks - 1 + (g.chunks - 1) / JOIN_SHORT * JOIN_SHARES);
-    const int sum_threads = (int)(D > 1536 ? 256 : ceil_div(D, 512) * 64);  // eight columns each
+    const int sum_threads = 64 * grad_waves(D);
     with_elem(dy_dtype, [&](auto e) {
         with_elem(grad_dtype, [&](auto o) {
             with_bool(vec_grad && (ld_dy * decltype(e)::BYTES) % 16 == 0 && D % 8 == 0, [&](auto v) {
