@@ -4,7 +4,7 @@
 //
 // All are bound by bytes: the rows read and written, and for the gradient the whole of dT, whose rows without a token are
 // zeros.  A lookup is one multiplication in binary32 and one rounding per value.  Gradients, us: 4096 binary16 tokens of 768 into
-// binary32 [30522, 768] 28 (17 sorting beside the zeros, 5 sums, 6 joining), 65536 bfloat16 tokens of 1024 into [30522, 1024] 103 (44
+// binary32 [30522, 768] 28 (18 sorting beside the zeros, 5 sums, 7 joining), 65536 bfloat16 tokens of 1024 into [30522, 1024] 94 (35
 // sorting beside the zeros, 49 sums: 4.6 TB/s, 8 joining).
 #include "elements.h"
 
@@ -174,8 +174,8 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(const ZeroParams z) { ze
 // Positions are put in the order of their tokens, equal tokens in the order of the batch, so a row's sum does not depend on how
 // the work fell.  Tokens that count for nothing (the padding token, ids outside the table) get the key V, behind all others.
 // Short batches: a position's place is the number of positions before it, counted directly; longer ones: a stable radix sort
-// (least significant digit first, up to nine bits a pass).  A gradient of V = 30522, D = 768, us: 12000 tokens 39.6 counted directly, 16384
-// 56.8, sorted by digits 51.7.
+// (least significant digit first, up to nine bits a pass).  A gradient of V = 30522, D = 768, us: 12000 tokens 42.4 counted directly, 16384
+// 56.8, sorted by digits 50.2.
 constexpr int SORT_BINS = 512, SORT_THREADS = 1024, SORT_WAVES = 16, SORT_ROUNDS = 2, SORT_TILE = SORT_THREADS * SORT_ROUNDS, SORT_BLOCKS = 256;
 constexpr int RANK_MAX = 12288, RANK_FEW = 4096, RANK_THREADS = 1024;
 

@@ -197,6 +197,32 @@ def test_gradient_rows_with_gaps(mkq, ld_y, ld_g, accumulate):
         assert bool((room[:V, D:] == -5).all()) and bool((room[V] == -5).all())
 
 
+@pytest.mark.parametrize("V,D", [(1, 1), (1, 7), (2, 4), (3, 5), (9, 33), (5000, 39)])
+@pytest.mark.parametrize("gt", ["f32", "f16", "bf16"])
+def test_gradient_rows_of_any_length_without_gaps(mkq, V, D, gt):
+    """Rows that begin at every alignment: all of them are written, nothing beside them; a gradient that is not aligned itself is refused"""
+    t = torch.tensor([V - 1, 0, -100, V // 2])
+    dy = torch.randn(4, D, generator=torch.Generator().manual_seed(D)).to(T[gt])
+    for none in (False, True):
+        room = torch.full((V * D + 32,), -5.0, dtype=T[gt], device="cuda")
+        grad = room[16:16 + V * D].view(V, D)
+        tokens = torch.full((4,), -100) if none else t
+        mkq.mkq_embedding_gradient(tokens.cuda(), dy.cuda(), V, 1.0, code(mkq, gt), grad=grad)
+        check_gradient(grad, tokens, dy, V, 1.0)
+        assert bool((room[:16] == -5).all()) and bool((room[16 + V * D:] == -5).all())
+    with pytest.raises(mkq.MkqError, match="aligned"):
+        mkq.mkq_embedding_gradient(t.cuda(), dy.cuda(), V, 1.0, code(mkq, gt), grad=room[17:17 + V * D].view(V, D))
+
+
+@pytest.mark.parametrize("M", [4095, 4096, 4097, 4160, 6000])
+def test_gradient_at_both_ways_to_rank(mkq, M):
+    V, D = 900, 24
+    t = some_tokens(M, V, M)
+    t[::7] = 11
+    dy = torch.randn(M, D, generator=torch.Generator().manual_seed(3))
+    check_gradient(mkq.mkq_embedding_gradient(t.cuda(), dy.cuda(), V, padding_token=0), t, dy, V, 1.0, 0)
+
+
 def test_gradient_past_32_bits(mkq):
     """A gradient, then gradients' rows, of more than 2^31 values"""
     V, D = 70000, 32768
