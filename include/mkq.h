@@ -479,10 +479,11 @@ int mkq_embedding_gradient(const void *tokens, int token_bits, int64_t M, const 
  *   outs_host     host array [n] of device pointers; outs_host[t] == grads_host[t] clips in place, otherwise it overlaps no
  *                 gradient; no two of them overlap (a tensor that is in the list twice would be scaled twice)
  *   norm_out      device, the norm before clipping, binary32
- *   max_norm      > 0 (infinity: copies only)
+ *   max_norm      > 0 (infinity: copies only, whatever the norm is)
  *   workspace     at least mkq_gradient_norm_workspace_bytes(n) bytes, 16-byte aligned; no preparation.  Two calls that may run
  *                 at the same time need two.
- * A NaN among the gradients makes the norm and all results NaN; an infinity makes the norm infinite, c = 0 and itself NaN.
+ * A NaN among the gradients makes the norm and, under a finite max_norm, all results NaN; an infinity makes the norm infinite and, under
+ * a finite max_norm, c = 0 and itself NaN.
  * n == 0: the norm is 0.  Errors: NULL, SHAPE, ALIGN, SCALE, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
 size_t mkq_gradient_norm_workspace_bytes(int64_t n);
 int mkq_gradient_norm(int64_t n, const void *const *grads_host, const int64_t *counts_host, const int32_t *dtypes_host,

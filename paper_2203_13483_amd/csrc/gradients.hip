@@ -166,14 +166,15 @@ __device__ __forceinline__ void scale_values(const void *p, void *q, int64_t at,
 
 // Every workgroup adds up the partial sums itself (16 KB out of the L2), which spares a launch between the two passes.
 // Last pieces first: they were read last, and what the memory-side cache still holds of them need not come from HBM again.
-// A factor of 1 leaves gradients that are clipped in place as they are.
+// A factor of 1 leaves gradients that are clipped in place as they are.  Without a limit (max_norm = infinity) it is 1 whatever the
+// norm: infinity over an infinite norm would make every finite gradient a NaN.
 __global__ __launch_bounds__(256) void clip_kernel(const TensorList l, const double *__restrict__ partials, int count, float max_norm,
                                                    float *__restrict__ norm_out)
 {
     __shared__ double part[4];
     const double norm = norm_of(partials, count, part);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-    const double q = (double)max_norm / (norm + 1e-6);
+    const double q = max_norm == __builtin_inff() ? 1.0 : (double)max_norm / (norm + 1e-6);
     const float c = q < 1.0 || q != q ? (float)q : 1.0f;
     for_each_piece<true>(l, [&](int t, int64_t from, int values) {
         if (c == 1.0f && l.out[t] == l.grad[t]) return;

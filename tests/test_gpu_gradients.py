@@ -148,3 +148,19 @@ def test_more_than_32_bits_of_values(mkq):
     assert abs(float(mkq.mkq_clip_gradients([t], 361.3)) - true) < 2.0 ** -23 * true
     want = torch.tensor([3.0, 4.0, 12.0, 84.0, 3612.0]).double() * 0.1
     assert bool(((t[at].cpu().double() - want).abs() <= 2.0 ** -10 * want).all()) and int((t != 0).sum()) == 5
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_no_limit_copies_whatever_the_norm_is(mkq, bad, in_place):
+    """max_norm = infinity scales nothing: finite gradients beside one that is not keep their bits"""
+    for dtype in KINDS:
+        ts = tensors([100, 9000, 8192], 7, [dtype])
+        ts[1][8500] = bad
+        before = [t.clone() for t in ts]
+        outs = None if in_place else [torch.full_like(t, 9) for t in ts]
+        norm = mkq.mkq_clip_gradients(ts, math.inf, outs=outs)
+        assert math.isnan(float(norm)) if math.isnan(bad) else float(norm) == math.inf
+        for o, b in zip(ts if in_place else outs, before):
+            there = ~b.isnan()
+            assert torch.equal(o[there], b[there]) and bool(o[~there].isnan().all())
