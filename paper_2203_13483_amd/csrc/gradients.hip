@@ -164,6 +164,16 @@ __device__ __forceinline__ void scale_values(const void *p, void *q, int64_t at,
         [&](int i) { out[i] = E::put(product(E::get(g[i]), c)); });
 }
 
+// The same for a factor below binary32's normal numbers, which has few bits there or none: the product is binary64, rounded to binary32
+// and to the type.  (Norms near the end of binary32's range under a small limit; value by value, nothing else is bound by it.)
+template <class E>
+__device__ __forceinline__ void scale_values_small(const void *p, void *q, int64_t at, int values, double c)
+{
+    const typename E::raw *g = static_cast<const typename E::raw *>(p) + at;
+    typename E::raw *out = static_cast<typename E::raw *>(q) + at;
+    for (int i = threadIdx.x; i < values; i += 256) out[i] = E::put((float)((double)E::get(g[i]) * c));
+}
+
 // Every workgroup adds up the partial sums itself (16 KB out of the L2), which spares a launch between the two passes.
 // Last pieces first: they were read last, and what the memory-side cache still holds of them need not come from HBM again.
 // A factor of 1 leaves gradients that are clipped in place as they are.  Without a limit (max_norm = infinity) it is 1 whatever the
@@ -178,6 +188,12 @@ __global__ __launch_bounds__(256) void clip_kernel(const TensorList l, const dou
     const float c = q < 1.0 || q != q ? (float)q : 1.0f;
     for_each_piece<true>(l, [&](int t, int64_t from, int values) {
         if (c == 1.0f && l.out[t] == l.grad[t]) return;
+        if (q > 0.0 && q < 0x1p-126) {
+            if (l.dtype[t] == MKQ_F32) scale_values_small<ElemF32>(l.grad[t], l.out[t], from, values, q);
+            else if (l.dtype[t] == MKQ_F16) scale_values_small<ElemF16>(l.grad[t], l.out[t], from, values, q);
+            else scale_values_small<ElemBF16>(l.grad[t], l.out[t], from, values, q);
+            return;
+        }
         if (l.dtype[t] == MKQ_F32) scale_values<ElemF32>(l.grad[t], l.out[t], from, values, c);
         else if (l.dtype[t] == MKQ_F16) scale_values<ElemF16>(l.grad[t], l.out[t], from, values, c);
         else scale_values<ElemBF16>(l.grad[t], l.out[t], from, values, c);

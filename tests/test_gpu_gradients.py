@@ -164,3 +164,26 @@ def test_no_limit_copies_whatever_the_norm_is(mkq, bad, in_place):
         for o, b in zip(ts if in_place else outs, before):
             there = ~b.isnan()
             assert torch.equal(o[there], b[there]) and bool(o[~there].isnan().all())
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("max_norm", [1e-2, 1e-5, 1e-30])
+def test_factors_below_the_normal_numbers(mkq, max_norm, in_place):
+    """Gradients near the end of the range clipped to a small norm: a factor of 2^-134 to 2^-227, which binary32 has in few bits or not at all, and
+    results that it has.  Off by the rounding of the factor to 53 bits (nothing here), of the product to binary32 and to the tensor's type."""
+    ts = tensors([8192, 5000, 77, 8192, 30001], 11, [torch.float32, torch.bfloat16], 1e36)
+    flat = torch.randn(9000, device="cuda", generator=torch.Generator("cuda").manual_seed(12)) * 1e36
+    ts.append(flat[1:8999])  # (only its elements are aligned)
+    before = [t.clone() for t in ts]
+    want = true_norm(before)
+    assert max_norm / want < 2.0 ** -126
+    outs = ts if in_place else [torch.full_like(t, 9) for t in ts]
+    norm = mkq.mkq_clip_gradients(ts, max_norm, outs=None if in_place else outs)
+    assert abs(float(norm) - want) <= want * (2.0 ** -24 + 1e-12)
+    limit = float(torch.tensor(max_norm, dtype=torch.float32))
+    for o, b in zip(outs, before):
+        y = b.double() * (limit / (want + 1e-6))
+        tol = y.abs() * (2.0 ** -24 + 1e-12) + 2.0 ** -150
+        if o.dtype != torch.float32:
+            tol = tol + (y.abs() + tol) * torch.finfo(o.dtype).eps / 2 + torch.finfo(o.dtype).smallest_normal * torch.finfo(o.dtype).eps / 2
+        assert bool(((o.double() - y).abs() <= tol).all())
