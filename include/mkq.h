@@ -429,7 +429,7 @@ int mkq_pack_weights_int4_group(const void *W, int w_dtype, int64_t N, int64_t K
  * of decoding or of a classifier):
  *     y[m,n] = sum_g s_w[n,g] ( sum_{k in g} x[m,k] c[n,k] ) + bias[n],  + residual, act, narrowed once to out_dtype
  * Activations and codes enter the products exactly (binary32 ones too), all sums are binary32.  Infinities and NaN in a row
- * of x reach that row of y, as in IEEE arithmetic on the dequantized weights.
+ * of x reach that row of y, as in IEEE arithmetic on the dequantized weights (GELU as x Phi(x): +infinity stays one, -infinity gives a NaN).
  *   x     [M, K] of x_dtype (F32, F16, BF16), row stride ldx (any; K a multiple of 8 in rows of a multiple of 16 bytes is faster)
  *   Wq, s_w  from mkq_pack_weights_int4_group with the same group;  bias [N] binary32 or NULL
  *   out   [M, N] of out_dtype (F32, F16, BF16)

@@ -284,8 +284,8 @@ __device__ __forceinline__ void store_tile(const Group4Params &p, typename Tile<
         else add(ElemBF16());
     }
     if (p.act == MKQ_ACT_GELU) {
-        if (p.out_dtype == MKQ_F16) each([&](float &v, int64_t) { v = gelu_erf(v); });
-        else each([&](float &v, int64_t) { v = gelu_erf_tail(v); });
+        if (p.out_dtype == MKQ_F16) each([&](float &v, int64_t) { v = gelu_erf<true>(v); });
+        else each([&](float &v, int64_t) { v = gelu_erf_tail<true>(v); });
     }
     if (p.out_dtype == MKQ_F32) write(ElemF32());
     else if (p.out_dtype == MKQ_F16) write(ElemF16());

@@ -303,6 +303,14 @@ __device__ __forceinline__ uint32_t pack2_f16(float a, float b)
 // per value and wave.  The form before (Abramowitz & Stegun 7.1.26: reciprocal, five coefficients, exp(-x^2 / 2)) took
 // thirteen with two quarter-rate ones, 76 cycles.  Evaluated in binary32 against binary64: largest error on [-10, 10] 2.5e-7
 // (before 3.3e-7; most of it the rounding of results near 4), root mean square under unit Gaussian inputs 1.4e-8 (3.4e-8).
+// +infinity gives a NaN, infinity times a u of 0, but INFINITE, one operation more: there the product has the largest finite number in
+// its place, and the maximum is the infinity.  (-infinity is a NaN in both, as x Phi(x) is; a NaN reaches u.)
+template <bool INFINITE>
+__device__ __forceinline__ float gelu_factor(float x)
+{
+    return fabsf(INFINITE ? __builtin_amdgcn_fmed3f(x, -__builtin_inff(), 3.4028234663852886e38f) : x);
+}
+template <bool INFINITE = false>
 __device__ __forceinline__ float gelu_erf(float x)
 {
     const float ax = fabsf(x);
@@ -317,7 +325,7 @@ __device__ __forceinline__ float gelu_erf(float x)
     const float u = __builtin_amdgcn_exp2f(l);
     // max(x, 0) as a median of three: one instruction (fmaxf first quiets its operand with a second one); a
     // NaN still reaches the result through the product
-    return __builtin_fmaf(-ax, u, __builtin_amdgcn_fmed3f(x, 0.0f, __builtin_inff()));
+    return __builtin_fmaf(-gelu_factor<INFINITE>(x), u, __builtin_amdgcn_fmed3f(x, 0.0f, __builtin_inff()));
 }
 
 // The same for results that keep small values (binary32, bfloat16).  The fit above is absolute, as fine as the steps of codes
@@ -325,6 +333,7 @@ __device__ __forceinline__ float gelu_erf(float x)
 // -8.  Degree 12 (the same method, absolute error on [0, 5] and relative error on [5, 13.1] together) has 0.04 %, 0.13 %,
 // 0.11 % there and 0.9 % at -12.8, below which u ends with the normal numbers (7.1.26: 0.25 %, 0.5 %, 1 %, 3.7 %), and an
 // absolute error of 3e-9 on [-5, 0] before rounding.  16 cycles more than the form above.
+template <bool INFINITE = false>
 __device__ __forceinline__ float gelu_erf_tail(float x)
 {
     const float ax = fabsf(x);
@@ -341,7 +350,7 @@ __device__ __forceinline__ float gelu_erf_tail(float x)
     l = __builtin_fmaf(l, ax, -1.1511048507359467f);
     l = __builtin_fmaf(l, ax, -1.0f);
     const float u = __builtin_amdgcn_exp2f(l);
-    return __builtin_fmaf(-ax, u, __builtin_amdgcn_fmed3f(x, 0.0f, __builtin_inff()));
+    return __builtin_fmaf(-gelu_factor<INFINITE>(x), u, __builtin_amdgcn_fmed3f(x, 0.0f, __builtin_inff()));
 }
 
 }  // namespace mkq

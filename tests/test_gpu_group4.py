@@ -303,3 +303,32 @@ def test_captured(mkq):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("M", [6, 70])
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_gelu_of_infinities_and_nan(mkq, M, out):
+    """GELU is x Phi(x): +infinity stays one, -infinity times 0 is a NaN as in IEEE arithmetic, a NaN stays one"""
+    N, K, group = 40, 200, 64
+    codes, s = weights(N, K, group, 3)
+    codes[:, 7] = torch.where(codes[:, 7] == 0, 1, codes[:, 7])
+    sign = codes[:, 7].sign().float()
+    Wq, sd = pack_codes(codes).cuda(), s.cuda()
+    for xt in T:
+        x = torch.randn(M, K, generator=torch.Generator().manual_seed(4)).to(T[xt])
+        run = lambda x, **kw: mkq.mkq_linear_int4_group(x.cuda(), Wq, sd, kw.pop("bias", None), N, K, group, code(mkq, out), act=mkq.MKQ_ACT_GELU, **kw).cpu()
+        clean = run(x)
+        x[1, 7], x[2, 7], x[3, 7] = float("inf"), float("-inf"), float("nan")
+        got = run(x)
+        rows = [m for m in range(M) if m not in (1, 2, 3)]
+        assert torch.equal(got[rows], clean[rows]) and bool(got[3].isnan().all())
+        for row, up in ((1, sign > 0), (2, sign < 0)):
+            assert bool((got[row][up] == math.inf).all()) and bool(got[row][~up].isnan().all())
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(4))
+    clean = run(x)
+    bias, residual = torch.zeros(N), torch.zeros(M, N)
+    bias[3], residual[2, 5] = float("inf"), float("inf")
+    got = run(x, bias=bias.cuda(), residual=residual.cuda())
+    assert bool((got[:, 3] == math.inf).all()) and float(got[2, 5]) == math.inf
+    got[:, 3], got[2, 5] = clean[:, 3], clean[2, 5]
+    assert torch.equal(got, clean)
