@@ -654,6 +654,28 @@ def _need(ok, what: str):
         raise ValueError(what)
 
 
+_FLOATS = "float32, float16 or bfloat16"
+
+
+def _float_code(t, what: str) -> int:
+    """_dtype_code of a tensor of floats."""
+    _torch()
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: {_FLOATS}")
+    return code
+
+
+def _float_dtype(code: int, what: str):
+    """_torch_dtype of a code of floats."""
+    if not _torch_dtypes:
+        _torch_dtype(MKQ_F32)  # (fills the table)
+    dtype = _torch_dtypes.get(code)
+    if dtype is None:
+        raise ValueError(f"{what}: {_FLOATS}")
+    return dtype
+
+
 def _rows(t, what: str):
     """Row stride of a matrix whose rows are contiguous."""
     if t.dim() == 2:
@@ -715,7 +737,7 @@ def mkq_group_weight_bytes(N: int, K: int) -> int:
 def mkq_pack_weights_int4_group(W, group: int = 64, s_w_in=None, stream=None):
     """W [N,K] float32/float16/bfloat16 -> (Wq uint8 [N, ceil(K/32)*16], s_w float32 [N, ceil(K/group)])."""
     torch = _torch()
-    ldw = _rows(W, "W")
+    ldw, w_dtype = _rows(W, "W"), _float_code(W, "W")
     N, K = W.shape
     dev = _same_device(W, s_w_in)
     groups = -(-K // group) if group > 0 else 0
@@ -724,7 +746,7 @@ def mkq_pack_weights_int4_group(W, group: int = 64, s_w_in=None, stream=None):
               "s_w_in: contiguous float32 [N, ceil(K/group)]")
     Wq = _new((N, -(-K // 32) * 16), torch.uint8, W.device, stream)
     s_w = _new((N, groups), torch.float32, W.device, stream)
-    _check(load().mkq_pack_weights_int4_group(_ptr(W), _dtype_code(W), N, K, ldw, int(group), _ptr(s_w_in), _ptr(s_w),
+    _check(load().mkq_pack_weights_int4_group(_ptr(W), w_dtype, N, K, ldw, int(group), _ptr(s_w_in), _ptr(s_w),
                                               _ptr(Wq), _stream_on(dev, stream)), "mkq_pack_weights_int4_group")
     return Wq, s_w
 
@@ -741,24 +763,25 @@ def mkq_linear_int4_group(x, Wq, s_w, bias, N: int, K: int, group: int = 64, out
                           act: int = MKQ_ACT_NONE, residual=None, out=None, stream=None):
     """x [M,K] float times group-scaled 4-bit weights (mkq_pack_weights_int4_group) -> [M,N] of out_dtype (None: x's)."""
     torch = _torch()
-    ldx = _rows(x, "x")
+    ldx, x_dtype = _rows(x, "x"), _float_code(x, "x")
     M = x.size(0)
     _need(x.size(1) == K, "x: [M, K]")
+    if out_dtype is None:
+        out_dtype = x_dtype
+    dtype = _float_dtype(out_dtype, "out_dtype")
+    residual_dtype = _float_code(residual, "residual") if residual is not None else MKQ_F32
     dev = _same_device(x, Wq, s_w, bias, residual, out)
     _group_table(Wq, s_w, N, K, group)
     _need(bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == N), "bias: float32 [N]")
-    if out_dtype is None:
-        out_dtype = _dtype_code(x)
     if out is None:
-        out = _new_matrix(M, N, _torch_dtype(out_dtype), x.device, stream)
+        out = _new_matrix(M, N, dtype, x.device, stream)
     else:
-        _need(out.dtype == _torch_dtype(out_dtype) and out.is_contiguous() and tuple(out.shape) == (M, N), "out: contiguous [M, N] of out_dtype")
+        _need(out.dtype == dtype and out.is_contiguous() and tuple(out.shape) == (M, N), "out: contiguous [M, N] of out_dtype")
     epi = None
     if act or residual is not None:
         _need(residual is None or (residual.is_contiguous() and tuple(residual.shape) == (M, N)), "residual: contiguous [M, N]")
-        epi = C.byref(Epilogue(act=int(act), residual=_ptr(residual),
-                               residual_dtype=_dtype_code(residual) if residual is not None else MKQ_F32))
-    _check(load().mkq_linear_int4_group(_ptr(x), _dtype_code(x), ldx, _ptr(Wq), _ptr(s_w), int(group), _ptr(bias), M, N, K,
+        epi = C.byref(Epilogue(act=int(act), residual=_ptr(residual), residual_dtype=residual_dtype))
+    _check(load().mkq_linear_int4_group(_ptr(x), x_dtype, ldx, _ptr(Wq), _ptr(s_w), int(group), _ptr(bias), M, N, K,
                                         _ptr(out), int(out_dtype), epi, _stream_on(dev, stream)), "mkq_linear_int4_group")
     return out
 
@@ -769,26 +792,27 @@ def _tokens(tokens):
     return 64 if tokens.dtype == torch.int64 else 32
 
 
-def _token_rows(tokens, D: int, out, out_dtype: int, stream):
+def _token_rows(tokens, D: int, out, dtype, stream):
     """The caller's [M, D] rows, or new ones, and their stride."""
     M = tokens.numel()
     if out is None:
-        return _new_matrix(M, D, _torch_dtype(out_dtype), tokens.device, stream), D
+        return _new_matrix(M, D, dtype, tokens.device, stream), D
     ld = _rows(out, "out")
-    _need(out.dtype == _torch_dtype(out_dtype) and tuple(out.shape) == (M, D), "out: [M, D] of out_dtype")
+    _need(out.dtype == dtype and tuple(out.shape) == (M, D), "out: [M, D] of out_dtype")
     return out, ld
 
 
 def mkq_embedding(tokens, table, scale: float = 1.0, out_dtype: int | None = None, *, out=None, stream=None):
     """Rows of table [V,D] for tokens (int32 / int64, any shape, M of them) times scale -> [M,D] of out_dtype (None: the table's)."""
     bits = _tokens(tokens)
-    ld_table = _rows(table, "table")
+    ld_table, table_dtype = _rows(table, "table"), _float_code(table, "table")
     V, D = table.shape
-    dev = _same_device(tokens, table, out)
     if out_dtype is None:
-        out_dtype = _dtype_code(table)
-    out, ld_out = _token_rows(tokens, D, out, out_dtype, stream)
-    _check(load().mkq_embedding(_ptr(tokens), bits, tokens.numel(), _ptr(table), _dtype_code(table), V, D, ld_table, float(scale),
+        out_dtype = table_dtype
+    dtype = _float_dtype(out_dtype, "out_dtype")
+    dev = _same_device(tokens, table, out)
+    out, ld_out = _token_rows(tokens, D, out, dtype, stream)
+    _check(load().mkq_embedding(_ptr(tokens), bits, tokens.numel(), _ptr(table), table_dtype, V, D, ld_table, float(scale),
                                 _ptr(out), int(out_dtype), ld_out, _stream_on(dev, stream)), "mkq_embedding")
     return out
 
@@ -796,10 +820,10 @@ def mkq_embedding(tokens, table, scale: float = 1.0, out_dtype: int | None = Non
 def mkq_embedding_int4_group(tokens, Wq, s_w, V: int, D: int, group: int = 64, scale: float = 1.0, out_dtype: int = MKQ_F32, *,
                              out=None, stream=None):
     """Rows of a group-scaled 4-bit table (mkq_pack_weights_int4_group with N = V, K = D) times scale -> [M,D] of out_dtype."""
-    bits = _tokens(tokens)
+    bits, dtype = _tokens(tokens), _float_dtype(out_dtype, "out_dtype")
     dev = _same_device(tokens, Wq, s_w, out)
     _group_table(Wq, s_w, V, D, group)
-    out, ld_out = _token_rows(tokens, D, out, out_dtype, stream)
+    out, ld_out = _token_rows(tokens, D, out, dtype, stream)
     _check(load().mkq_embedding_int4_group(_ptr(tokens), bits, tokens.numel(), _ptr(Wq), _ptr(s_w), int(group), V, D, float(scale),
                                            _ptr(out), int(out_dtype), ld_out, _stream_on(dev, stream)), "mkq_embedding_int4_group")
     return out
@@ -814,19 +838,19 @@ def mkq_embedding_gradient(tokens, dy, V: int, scale: float = 1.0, grad_dtype: i
     """Gradient [V,D] of mkq_embedding's table from dy [M,D].  ``accumulate``: added to the ``grad`` that is passed in."""
     torch = _torch()
     bits = _tokens(tokens)
-    ld_dy = _rows(dy, "dy")
+    ld_dy, dy_dtype, dtype = _rows(dy, "dy"), _float_code(dy, "dy"), _float_dtype(grad_dtype, "grad_dtype")
     M, D = dy.shape
     _need(tokens.numel() == M, "dy: a row for every token")
     dev = _same_device(tokens, dy, grad, workspace)
     _need(grad is not None or not accumulate, "accumulate: needs the gradient to add to")
     if grad is None:
-        grad, ld_grad = _new_matrix(V, D, _torch_dtype(grad_dtype), dy.device, stream), D
+        grad, ld_grad = _new_matrix(V, D, dtype, dy.device, stream), D
     else:
         ld_grad = _rows(grad, "grad")
-        _need(grad.dtype == _torch_dtype(grad_dtype) and tuple(grad.shape) == (V, D), "grad: [V, D] of grad_dtype")
+        _need(grad.dtype == dtype and tuple(grad.shape) == (V, D), "grad: [V, D] of grad_dtype")
     if workspace is None:
         workspace = _new(mkq_embedding_gradient_workspace_bytes(M, D), torch.uint8, dy.device, stream)
-    _check(load().mkq_embedding_gradient(_ptr(tokens), bits, M, _ptr(dy), _dtype_code(dy), ld_dy, V, D, float(scale), int(padding_token),
+    _check(load().mkq_embedding_gradient(_ptr(tokens), bits, M, _ptr(dy), dy_dtype, ld_dy, V, D, float(scale), int(padding_token),
                                          int(accumulate), _ptr(grad), int(grad_dtype), ld_grad, _ptr(workspace), workspace.nbytes,
                                          _stream_on(dev, stream)), "mkq_embedding_gradient")
     return grad
@@ -836,8 +860,17 @@ def mkq_gradient_norm_workspace_bytes(n: int) -> int:
     return int(load().mkq_gradient_norm_workspace_bytes(n))
 
 
+def _float_codes(dtypes, what: str):
+    """_dtype_code of every tensor of a list."""
+    _torch()
+    try:
+        return array("i", map(_dtype_codes.__getitem__, dtypes))
+    except KeyError:
+        raise ValueError(f"{what}: {_FLOATS}") from None
+
+
 def _tensor_list(tensors, what: str):
-    """Numbers of values, types and addresses of contiguous tensors of the current GPU.  (One pass a question, in C: a loop over fifty
+    """Numbers of values and addresses of contiguous tensors of the current GPU.  (One pass a question, in C: a loop over fifty
     tensors and their outputs took 50 us of a call.)"""
     torch = _torch()
     T = torch.Tensor
@@ -846,7 +879,7 @@ def _tensor_list(tensors, what: str):
     _same_device(tensors[0])
     if len(set(map(T.get_device, tensors))) != 1:
         raise ValueError("tensors live on one GPU")
-    return list(map(T.numel, tensors)), [t.dtype for t in tensors], array("Q", map(T.data_ptr, tensors))
+    return list(map(T.numel, tensors)), array("Q", map(T.data_ptr, tensors))
 
 
 def _norm_buffers(n: int, device, norm_out, workspace, stream):
@@ -862,32 +895,35 @@ def _norm_buffers(n: int, device, norm_out, workspace, stream):
 def mkq_gradient_norm(grads, norm_out=None, workspace=None, stream=None):
     """Norm over all values of a list of contiguous tensors (float32 / float16 / bfloat16, mixed) -> float32 tensor [1]."""
     grads = list(grads)
-    counts, dtypes, at = _tensor_list(grads, "grads")
+    codes = _float_codes([t.dtype for t in grads], "grads")
+    counts, at = _tensor_list(grads, "grads")
     dev = _same_device(grads[0], norm_out, workspace)
     norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
-    counts, codes = array("q", counts), array("i", map(_dtype_codes.__getitem__, dtypes))
+    counts = array("q", counts)
     _check(load().mkq_gradient_norm(len(grads), at.buffer_info()[0], counts.buffer_info()[0], codes.buffer_info()[0], _ptr(norm_out),
                                     _ptr(workspace), workspace.nbytes, _stream_on(dev, stream)), "mkq_gradient_norm")
     return norm_out
 
 
 def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, workspace=None, stream=None):
-    """Scales a list of gradients to a norm of at most max_norm, in place or into ``outs`` (same types and sizes); returns the
-    norm before, float32 tensor [1]."""
+    """Scales a list of gradients (float32 / float16 / bfloat16, mixed; the float64 sums of mkq_scale_gradients are to be cast) to a
+    norm of at most max_norm, in place or into ``outs`` (same types and sizes); returns the norm before, float32 tensor [1]."""
     grads = list(grads)
-    counts, dtypes, at = _tensor_list(grads, "grads")
+    dtypes = [t.dtype for t in grads]
+    codes = _float_codes(dtypes, "grads")
+    counts, at = _tensor_list(grads, "grads")
     dev = _same_device(grads[0], norm_out, workspace)
     out_at = at
     if outs is not None:
         outs = list(outs)
-        out_counts, out_dtypes, out_at = _tensor_list(outs, "outs")
+        out_counts, out_at = _tensor_list(outs, "outs")
         _same_device(grads[0], outs[0])
-        _need(out_counts == counts and out_dtypes == dtypes, "outs: the gradients' types and sizes")
+        _need(out_counts == counts and [t.dtype for t in outs] == dtypes, "outs: the gradients' types and sizes")
     if len(set(out_at)) != len(out_at):  # (tensors without values share an address)
         written = [a for a, n in zip(out_at, counts) if n]
         _need(len(set(written)) == len(written), "no tensor twice: it would be scaled twice")
     norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
-    counts, codes = array("q", counts), array("i", map(_dtype_codes.__getitem__, dtypes))
+    counts = array("q", counts)
     _check(load().mkq_clip_gradients(len(grads), at.buffer_info()[0], out_at.buffer_info()[0], counts.buffer_info()[0],
                                      codes.buffer_info()[0], float(max_norm), _ptr(norm_out), _ptr(workspace), workspace.nbytes,
                                      _stream_on(dev, stream)), "mkq_clip_gradients")

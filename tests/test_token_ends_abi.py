@@ -134,3 +134,23 @@ def test_binding_refuses_what_it_would_read_wrongly(lib):
                  lambda: mkq.mkq_pack_weights_int4_group(x)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_binding_names_types_that_it_does_not_take(lib):
+    """Types that are neither binary32, binary16 nor bfloat16 (the binary64 sums of mkq_scale_gradients among them) are refused by name"""
+    x, t, d = torch.zeros(4, 64), torch.zeros(4, dtype=torch.int32), torch.zeros(4, 64, dtype=torch.float64)
+    Wq, s_w = torch.zeros(16, 32, dtype=torch.uint8), torch.zeros(16, 2)
+    for call in (lambda: mkq.mkq_linear_int4_group(d, Wq, s_w, None, 16, 64, 32),
+                 lambda: mkq.mkq_linear_int4_group(x, Wq, s_w, None, 16, 64, 32, mkq.MKQ_I4),
+                 lambda: mkq.mkq_linear_int4_group(x, Wq, s_w, None, 16, 64, 32, residual=torch.zeros(4, 16, dtype=torch.float64)),
+                 lambda: mkq.mkq_embedding(t, d),
+                 lambda: mkq.mkq_embedding(t, x.to(torch.int8)),
+                 lambda: mkq.mkq_embedding(t, x, 1.0, 9),
+                 lambda: mkq.mkq_embedding_int4_group(t, Wq, s_w, 16, 64, 32, 1.0, mkq.MKQ_I8),
+                 lambda: mkq.mkq_embedding_gradient(t, d, 100),
+                 lambda: mkq.mkq_embedding_gradient(t, x, 100, 1.0, mkq.MKQ_I4),
+                 lambda: mkq.mkq_gradient_norm([x, d]),
+                 lambda: mkq.mkq_clip_gradients([x, d], 1.0),
+                 lambda: mkq.mkq_pack_weights_int4_group(d)):
+        with pytest.raises(ValueError, match="float32, float16 or bfloat16"):
+            call()
