@@ -477,7 +477,7 @@ int mkq_embedding_gradient(const void *tokens, int token_bits, int64_t M, const 
  *   grads_host, counts_host, dtypes_host   host arrays [n]: device pointers, numbers of values, F32 / F16 / BF16 each; a tensor
  *                 is contiguous and aligned to its own element size (16 bytes are faster); one without values may be NULL
  *   outs_host     host array [n] of device pointers; outs_host[t] == grads_host[t] clips in place, otherwise it overlaps no
- *                 gradient; no two of them overlap (a tensor that is in the list twice would be scaled twice)
+ *                 gradient; no two of them overlap (a tensor that is in the list twice would be scaled twice): UNSUPPORTED
  *   norm_out      device, the norm before clipping, binary32
  *   max_norm      > 0 (infinity: copies only, whatever the norm is)
  *   workspace     at least mkq_gradient_norm_workspace_bytes(n) bytes, 16-byte aligned; no preparation.  Two calls that may run

@@ -919,14 +919,14 @@ def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, work
         out_counts, out_at = _tensor_list(outs, "outs")
         _same_device(grads[0], outs[0])
         _need(out_counts == counts and [t.dtype for t in outs] == dtypes, "outs: the gradients' types and sizes")
-    if len(set(out_at)) != len(out_at):  # (tensors without values share an address)
-        written = [a for a, n in zip(out_at, counts) if n]
-        _need(len(set(written)) == len(written), "no tensor twice: it would be scaled twice")
     norm_out, workspace = _norm_buffers(len(grads), grads[0].device, norm_out, workspace, stream)
     counts = array("q", counts)
-    _check(load().mkq_clip_gradients(len(grads), at.buffer_info()[0], out_at.buffer_info()[0], counts.buffer_info()[0],
-                                     codes.buffer_info()[0], float(max_norm), _ptr(norm_out), _ptr(workspace), workspace.nbytes,
-                                     _stream_on(dev, stream)), "mkq_clip_gradients")
+    status = load().mkq_clip_gradients(len(grads), at.buffer_info()[0], out_at.buffer_info()[0], counts.buffer_info()[0],
+                                       codes.buffer_info()[0], float(max_norm), _ptr(norm_out), _ptr(workspace), workspace.nbytes,
+                                       _stream_on(dev, stream))
+    if status == MKQ_ERR_UNSUPPORTED:
+        raise ValueError("no result over another one or over another gradient: it would be scaled twice")
+    _check(status, "mkq_clip_gradients")
     return norm_out
 
 

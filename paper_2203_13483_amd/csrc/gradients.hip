@@ -5,6 +5,10 @@
 // Bound by HBM: every value is read once for the norm and once more, behind it, to be scaled and written.  Squares and their
 // sums are binary64, in an order that does not depend on which workgroup is done first, so the norm of gradients beyond
 // 1e19 does not overflow and equal inputs give equal bits.  Measured: 81 million binary32 values 157 us (6.2 TB/s), 13 million 31 us.
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "elements.h"
 #include "gemm_common.h"
 
@@ -246,6 +250,44 @@ static int check_tensors(int64_t n, const void *const *grads, void *const *outs,
     return MKQ_OK;
 }
 
+// Whether no result lies over another one or over a gradient other than the one it is clipped from in place: a launch's workgroups
+// would read what others have scaled already.  In the order of their addresses every piece of memory has only to begin behind what was
+// written before it, and a result behind what was read, too.  (Two gradients may share memory.  Sorting takes 2.9 us for 50 tensors
+// with results of their own in any order, nothing for those of one allocation after the other.)
+struct Piece {
+    uintptr_t begin, end;
+    bool written;
+};
+static bool results_apart(Piece *pieces, int64_t n, const void *const *grads, void *const *outs, const int64_t *counts, const int32_t *dtypes)
+{
+    int64_t m = 0;
+    for (int64_t t = 0; t < n; ++t) {
+        if (counts[t] == 0) continue;
+        const uintptr_t bytes = (uintptr_t)(counts[t] * dtype_bytes(dtypes[t])), at = reinterpret_cast<uintptr_t>(outs[t]);
+        pieces[m++] = {at, at + bytes, true};
+        if (outs[t] != grads[t]) pieces[m++] = {reinterpret_cast<uintptr_t>(grads[t]), reinterpret_cast<uintptr_t>(grads[t]) + bytes, false};
+    }
+    const auto before = [](const Piece &a, const Piece &b) { return a.begin < b.begin; };
+    if (!std::is_sorted(pieces, pieces + m, before)) std::sort(pieces, pieces + m, before);
+    uintptr_t written = 0, read = 0;  // where they end
+    for (int64_t i = 0; i < m; ++i) {
+        const Piece &p = pieces[i];
+        if (p.begin < written || (p.written && p.begin < read)) return false;
+        uintptr_t &last = p.written ? written : read;
+        last = p.end > last ? p.end : last;
+    }
+    return true;
+}
+
+static int check_results_apart(int64_t n, const void *const *grads, void *const *outs, const int64_t *counts, const int32_t *dtypes)
+{
+    constexpr int64_t FEW = 256;
+    Piece few[2 * FEW];
+    if (n <= FEW) return results_apart(few, n, grads, outs, counts, dtypes) ? MKQ_OK : MKQ_ERR_UNSUPPORTED;
+    const std::unique_ptr<Piece[]> many(new (std::nothrow) Piece[2 * n]);
+    return many && results_apart(many.get(), n, grads, outs, counts, dtypes) ? MKQ_OK : MKQ_ERR_UNSUPPORTED;
+}
+
 // Launches the partial sums of all tensors; *count: how many there are
 static int launch_partials(int64_t n, const void *const *grads, const int64_t *counts, const int32_t *dtypes, double *partials, int *count,
                            hipStream_t st)
@@ -290,6 +332,7 @@ extern "C" int mkq_clip_gradients(int64_t n, const void *const *grads_host, void
     if (!aligned4(norm_out)) return MKQ_ERR_ALIGN;
     if (!(max_norm > 0.0f)) return MKQ_ERR_SCALE;
     int status = check_tensors(n, grads_host, outs_host, counts_host, dtypes_host, workspace, workspace_bytes);
+    if (status == MKQ_OK) status = check_results_apart(n, grads_host, outs_host, counts_host, dtypes_host);
     if (status != MKQ_OK) return status;
     const hipStream_t st = as_stream(stream);
     double *partials = static_cast<double *>(workspace);

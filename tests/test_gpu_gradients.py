@@ -187,3 +187,27 @@ def test_factors_below_the_normal_numbers(mkq, max_norm, in_place):
         if o.dtype != torch.float32:
             tol = tol + (y.abs() + tol) * torch.finfo(o.dtype).eps / 2 + torch.finfo(o.dtype).smallest_normal * torch.finfo(o.dtype).eps / 2
         assert bool(((o.double() - y).abs() <= tol).all())
+
+
+def test_results_beside_and_over_other_tensors(mkq):
+    """Neighbours without a gap, one gradient read twice and results that nobody overlaps are clipped; results over another tensor are
+    refused before anything is written"""
+    flat = torch.randn(400, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    a, b, c, d = flat.split(100)
+    before = flat.clone()
+    norm = mkq.mkq_clip_gradients([a, c], 1.0, outs=[b, d])
+    want = true_norm([before[:100], before[200:300]])
+    assert abs(float(norm) - want) <= want * (2.0 ** -24 + 1e-12)
+    assert torch.equal(a, before[:100]) and torch.equal(c, before[200:300])
+    assert abs(true_norm([b, d]) - 1.0) < 1e-5
+    mkq.mkq_clip_gradients([a, a], 1.0, outs=[b, d])
+    assert torch.equal(b, d) and abs(true_norm([b, d]) - 1.0) < 1e-5
+    many = torch.ones(700, 3, device="cuda")
+    mkq.mkq_clip_gradients(many.unbind(), 1.0)
+    assert abs(true_norm([many]) - 1.0) < 1e-5 and bool((many == many[0, 0]).all())
+    before = flat.clone()
+    for grads, outs in (([a, b], [b, a]), ([a, b], [c, a]), ([a, b], [c, c]), ([a], [flat[1:101]]), ([a, b], [a, flat[99:199]]),
+                        ([a, flat[99:199]], None), ([a, b, c], [a, c, d])):
+        with pytest.raises(ValueError):
+            mkq.mkq_clip_gradients(grads, 1.0, outs=outs)
+    assert torch.equal(flat, before)

@@ -154,3 +154,27 @@ def test_binding_names_types_that_it_does_not_take(lib):
                  lambda: mkq.mkq_pack_weights_int4_group(d)):
         with pytest.raises(ValueError, match="float32, float16 or bfloat16"):
             call()
+
+
+def test_clip_refuses_results_over_other_tensors(lib):
+    """A result written where another tensor is read or written: whole tensors in another order, one twice, parts, between many and
+    between types.  (Every call here is refused: the addresses are nobody's.)"""
+    def clip(ats, outs, counts, dtypes=None):
+        n = len(ats)
+        a, o = (C.c_void_p * n)(*ats), (C.c_void_p * n)(*outs)
+        c, d = (C.c_int64 * n)(*counts), (C.c_int32 * n)(*(dtypes or [F32] * n))
+        return lib.mkq_clip_gradients(n, a, o, c, d, 1.0, P, P, lib.mkq_gradient_norm_workspace_bytes(n), None)
+    A, B, D = 0x100000, 0x200000, 0x300000
+    for call in (lambda: clip([A, B], [B, A], [8, 8]),                                   # permuted
+                 lambda: clip([A, B], [D, A], [8, 8]),
+                 lambda: clip([A, A], [A, A], [8, 8]),                                   # twice, in place and not
+                 lambda: clip([A, B], [D, D], [8, 8]),
+                 lambda: clip([A, A], [A, B], [8, 8]),                                   # in place where another reads
+                 lambda: clip([A], [A + 16], [8]),                                       # over a part of itself
+                 lambda: clip([A, B], [D, D + 28], [8, 8]),                              # the last value of a result
+                 lambda: clip([A, A + 28], [A, A + 28], [8, 8]),
+                 lambda: clip([A, D], [A, B], [0x100001 // 4 + 1, 8]),
+                 lambda: clip([A, B], [D, D + 8], [8, 8], [F16, F32]),
+                 lambda: clip([A + 64 * i for i in range(700)], [A + 64 * (i ^ (i > 600)) for i in range(700)], [16] * 700),
+                 lambda: clip([A, 0, B], [B, 0, A], [8, 0, 8])):
+        assert call() == mkq.MKQ_ERR_UNSUPPORTED
