@@ -715,6 +715,11 @@ def _stream_on(dev: int, stream):
     return _stream(stream)
 
 
+def _workspace(workspace):
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous")
+
+
 def _new(shape, dtype, device, stream):
     """A tensor that belongs to the stream of the call, so that its memory is not handed on before the call is done."""
     torch = _torch()
@@ -841,6 +846,7 @@ def mkq_embedding_gradient(tokens, dy, V: int, scale: float = 1.0, grad_dtype: i
     ld_dy, dy_dtype, dtype = _rows(dy, "dy"), _float_code(dy, "dy"), _float_dtype(grad_dtype, "grad_dtype")
     M, D = dy.shape
     _need(tokens.numel() == M, "dy: a row for every token")
+    _workspace(workspace)
     dev = _same_device(tokens, dy, grad, workspace)
     _need(grad is not None or not accumulate, "accumulate: needs the gradient to add to")
     if grad is None:
@@ -895,6 +901,7 @@ def _norm_buffers(n: int, device, norm_out, workspace, stream):
 def mkq_gradient_norm(grads, norm_out=None, workspace=None, stream=None):
     """Norm over all values of a list of contiguous tensors (float32 / float16 / bfloat16, mixed) -> float32 tensor [1]."""
     grads = list(grads)
+    _workspace(workspace)
     codes = _float_codes([t.dtype for t in grads], "grads")
     counts, at = _tensor_list(grads, "grads")
     dev = _same_device(grads[0], norm_out, workspace)
@@ -909,6 +916,7 @@ def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, work
     """Scales a list of gradients (float32 / float16 / bfloat16, mixed; the float64 sums of mkq_scale_gradients are to be cast) to a
     norm of at most max_norm, in place or into ``outs`` (same types and sizes); returns the norm before, float32 tensor [1]."""
     grads = list(grads)
+    _workspace(workspace)
     dtypes = [t.dtype for t in grads]
     codes = _float_codes(dtypes, "grads")
     counts, at = _tensor_list(grads, "grads")

@@ -178,3 +178,14 @@ def test_clip_refuses_results_over_other_tensors(lib):
                  lambda: clip([A + 64 * i for i in range(700)], [A + 64 * (i ^ (i > 600)) for i in range(700)], [16] * 700),
                  lambda: clip([A, 0, B], [B, 0, A], [8, 0, 8])):
         assert call() == mkq.MKQ_ERR_UNSUPPORTED
+
+
+def test_binding_refuses_workspaces_with_gaps(lib):
+    """A view that counts more bytes than lie behind its address, or others' bytes between its own"""
+    x, t = torch.zeros(4, 64), torch.zeros(4, dtype=torch.int32)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 21, dtype=torch.uint8)[::2]):
+        for call in (lambda: mkq.mkq_embedding_gradient(t, x, 100, workspace=ws),
+                     lambda: mkq.mkq_gradient_norm([x], workspace=ws),
+                     lambda: mkq.mkq_clip_gradients([x], 1.0, workspace=ws)):
+            with pytest.raises(ValueError, match="workspace"):
+                call()
