@@ -428,13 +428,15 @@ int mkq_pack_weights_int4_group(const void *W, int w_dtype, int64_t N, int64_t K
 /* Linear of few tokens on group-scaled 4-bit weights, activations in floats (the head over the vocabulary, single linears
  * of decoding or of a classifier):
  *     y[m,n] = sum_g s_w[n,g] ( sum_{k in g} x[m,k] c[n,k] ) + bias[n],  + residual, act, narrowed once to out_dtype
- * Activations and codes enter the products exactly (binary32 ones too), all sums are binary32.  Infinities and NaN in a row
+ * Activations and codes enter the products exactly, all sums are binary32.  (A binary32 activation is a sum of three bfloat16 numbers:
+ * exactly from 2^-110 up, off by less than 2^-133 below.  A group's sum of |x c| reaches 2^128 only with activations near the end of
+ * binary32's or bfloat16's range, and is then an infinity or a NaN before its step is applied.)  Infinities and NaN in a row
  * of x reach that row of y, as in IEEE arithmetic on the dequantized weights (GELU as x Phi(x): +infinity stays one, -infinity gives a NaN).
  *   x     [M, K] of x_dtype (F32, F16, BF16), row stride ldx (any; K a multiple of 8 in rows of a multiple of 16 bytes is faster)
  *   Wq, s_w  from mkq_pack_weights_int4_group with the same group;  bias [N] binary32 or NULL
  *   out   [M, N] of out_dtype (F32, F16, BF16)
  *   epi   NULL, or act and residual (residual_dtype F32, F16 or BF16); its code and accumulator outputs: UNSUPPORTED
- * Any M (made for up to 128 tokens), N and K; M == 0 is a no-op.  No workspace.
+ * Any M (made for up to 128 tokens), N and K, up to about 2^34 results (UNSUPPORTED); M == 0 is a no-op.  No workspace.
  * Errors: NULL, SHAPE (group, ldx < K, ...), ALIGN, DTYPE, UNSUPPORTED, HIP. */
 int mkq_linear_int4_group(const void *x, int x_dtype, int64_t ldx, const uint8_t *Wq, const float *s_w, int group,
                           const float *bias, int64_t M, int64_t N, int64_t K, void *out, int out_dtype,

@@ -144,8 +144,8 @@ struct Product<ElemBF16> {
     __device__ static __forceinline__ v4f mul(V x, V c, v4f s) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, c, s, 0, 0, 0); }
     __device__ static __forceinline__ v16f mul(V x, V c, v16f s) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, c, s, 0, 0, 0); }
 };
-// x = hi + mid + lo: each part is the upper half of what is left (its first 8 bits), and what is left is exact, down to the
-// smallest normal number; nothing is left of an infinity, and a NaN stays one.  The smallest part is multiplied first.
+// x = hi + mid + lo: each part is the upper half of what is left (its first 8 bits), and what is left is exact, down to multiples of
+// 2^-133, bfloat16's smallest number (the matrix instruction takes those below its normal ones as they are); nothing is left of an infinity, and a NaN stays one.  The smallest part is multiplied first.
 template <>
 struct Product<ElemF32> : Product<ElemBF16> {
     static constexpr int PARTS = 3;

@@ -332,3 +332,22 @@ def test_gelu_of_infinities_and_nan(mkq, M, out):
     assert bool((got[:, 3] == math.inf).all()) and float(got[2, 5]) == math.inf
     got[:, 3], got[2, 5] = clean[:, 3], clean[2, 5]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("M,N", [(3, 40), (50, 6000)])
+def test_binary32_activations_down_to_the_smallest(mkq, M, N):
+    """Three bfloat16 parts hold what is a multiple of 2^-133, all 24 bits from 2^-110 up: a smaller activation is off by less than
+    2^-133, and the sum of K products, which steps of 1 leave alone, by K 2^-23 of their sizes and half a step of 2^-149 each."""
+    K = 40
+    g = torch.Generator().manual_seed(M)
+    codes = torch.randint(-8, 8, (N, K), generator=g)
+    s = torch.ones(N, 2)
+    for low, high in ((-149, -140), (-140, -126), (-126, -118), (-118, -110), (-110, -100)):
+        x = torch.ldexp(torch.rand(M, K, generator=g, dtype=torch.float64) + 0.5, torch.randint(low, high, (M, K), generator=g)).float()
+        got = mkq.mkq_linear_int4_group(x.cuda(), pack_codes(codes).cuda(), s.cuda(), None, N, K, 32, mkq.MKQ_F32).cpu()
+        xd, c = x.double(), codes.double()
+        S = xd @ c.abs().T
+        lost = (xd < 2.0 ** -110).double() * 2.0 ** -133 @ c.abs().T
+        tol = lost + (3 * K + 4) * 2.0 ** -23 * (S + lost) + (3 * K + 4) * 2.0 ** -149
+        off = (got.double() - xd @ c.T).abs()
+        assert bool((off <= tol).all()), (low, float((off / tol).max()))
