@@ -354,3 +354,117 @@ def test_a_tied_table_from_lookup_to_update(mkq):
     master -= 0.1 * grad
     Wq2, s2 = mkq.mkq_pack_weights_int4_group(master, group, s)
     assert not torch.equal(Wq2, Wq) and torch.equal(s2, s)
+
+
+# ---- long batches, where a thread has four rows, and long runs -------------------------------------------------------------
+def four_rows_from(D):
+    """Tokens from which a thread has four rows, and rows of a workgroup at a time"""
+    rows = 256 // min(256, -(-D // 8))
+    return rows * 4 * 2048, rows
+
+
+def lengths_around(D):
+    at, rows = four_rows_from(D)
+    return [at - 1, at, at + 1, at + rows, at + 4 * rows - 1]
+
+
+def batch_with_unknown_tokens(M, V, seed, dtype):
+    g = torch.Generator("cuda").manual_seed(seed)
+    t = torch.randint(0, V, (M,), generator=g, device="cuda", dtype=dtype)
+    t[torch.rand(M, generator=g, device="cuda") < 0.2] = V
+    t[torch.rand(M, generator=g, device="cuda") < 0.1] = -7
+    t[-1] = V - 1
+    return t
+
+
+@pytest.mark.parametrize("D,gap", [(1024, 0), (1024, 8), (2056, 0), (312, 5), (1001, 0), (1001, 7), (2051, 0)])
+def test_lookup_of_long_batches(mkq, D, gap):
+    """Bits of torch's, at every remainder of four rows a thread; rows with gaps and what lies behind the last one are left alone"""
+    V = 300
+    for i, M in enumerate(lengths_around(D)):
+        kinds = [("f16", "f16"), ("f32", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f16", "f32")][i:] + [("bf16", "bf16")]
+        for tt, out in kinds[:2]:
+            table = torch.randn(V, D, generator=torch.Generator("cuda").manual_seed(D), device="cuda").to(T[tt])
+            for dtype, scale in ((torch.int32, 1.0), (torch.int64, 1.7)):
+                t = batch_with_unknown_tokens(M, V, M, dtype)
+                known = ((t >= 0) & (t < V))[:, None]
+                want = torch.where(known, table[t.long().clamp(0, V - 1)].float() * torch.tensor(scale, device="cuda"), 0.0).to(T[out])
+                room = torch.full((M + 3, D + gap), -5.0, dtype=T[out], device="cuda")
+                got = mkq.mkq_embedding(t, table, scale, code(mkq, out), out=room[:M, :D])
+                assert torch.equal(got, want), (M, tt, out)
+                assert bool((room[:M, D:] == -5).all()) and bool((room[M:] == -5).all())
+
+
+@pytest.mark.parametrize("D,gap,group", [(1024, 0, 64), (1024, 8, 128), (2056, 0, 32), (312, 5, 32), (1001, 0, 64), (2051, 0, 128)])
+def test_lookup_int4_of_long_batches(mkq, D, gap, group):
+    V = 300
+    g = torch.Generator("cuda").manual_seed(D)
+    codes = torch.randint(-8, 8, (V, -(-D // 32) * 32), generator=g, device="cuda")
+    Wq = ((codes[:, 0::2] % 16) + 16 * (codes[:, 1::2] % 16)).to(torch.uint8)
+    s = torch.rand(V, -(-D // group), generator=g, device="cuda") * 0.01
+    rows = codes[:, :D].float() * s.repeat_interleave(group, 1)[:, :D]
+    for i, M in enumerate(lengths_around(D)):
+        out, dtype = ["f16", "f32", "bf16"][i % 3], [torch.int32, torch.int64][i % 2]
+        t = batch_with_unknown_tokens(M, V, M, dtype)
+        known = ((t >= 0) & (t < V))[:, None]
+        want = torch.where(known, rows[t.long().clamp(0, V - 1)] * torch.tensor(1.7, device="cuda"), 0.0).to(T[out])
+        room = torch.full((M + 3, D + gap), -5.0, dtype=T[out], device="cuda")
+        got = mkq.mkq_embedding_int4_group(t, Wq, s, V, D, group, 1.7, code(mkq, out), out=room[:M, :D])
+        assert torch.equal(got, want), (M, out)
+        assert bool((room[:M, D:] == -5).all()) and bool((room[M:] == -5).all())
+
+
+def check_exact_gradient(mkq, t, V, D, dt, gt, seed):
+    """Whole numbers whose sums stay below 2^24: every order of the additions gives them exactly, so a position that is lost or counted
+    twice shows, however long its run is"""
+    g = torch.Generator("cuda").manual_seed(seed)
+    dy = torch.randint(-9, 10, (len(t), D), generator=g, device="cuda").to(T[dt])
+    known = (t >= 0) & (t < V)
+    at = "cpu" if V <= 2 ** 20 else "cuda"  # (long runs take seconds there, tables of 2^27 rows here)
+    want = torch.zeros(V, D, dtype=torch.float64, device=at).index_add_(0, t[known].long().to(at), dy[known].double().to(at)).cuda()
+    assert not bool(known.any()) or int(torch.bincount(t[known].long()).max()) * 9 < 2 ** 24
+    assert torch.equal(mkq.mkq_embedding_gradient(t, dy, V, 1.0, code(mkq, gt)), want.to(T[gt]))
+    start = torch.randint(-9, 10, (V, D), generator=g, device="cuda").to(T[gt])
+    want = want + start.double()
+    assert torch.equal(mkq.mkq_embedding_gradient(t, dy, V, 1.0, code(mkq, gt), grad=start, accumulate=True), want.to(T[gt]))
+
+
+@pytest.mark.parametrize("tokens", ["same", "two", "blocks", "long_and_short", "all_outside", "ascending"])
+@pytest.mark.parametrize("M", [1, 8, 9, 63, 65, 1000, 4097, 9000, 12289, 70000, 70001])
+@pytest.mark.parametrize("D", [16, 5])
+def test_exact_gradient_of_extreme_batches(mkq, M, D, tokens):
+    V = 40000
+    i = torch.arange(M, device="cuda")
+    t = {"same": torch.full_like(i, 777), "two": i % 2 + 39998, "blocks": i // 997, "long_and_short": torch.where(i % 3 == 0, i // 3 % V, 5),
+         "all_outside": torch.full_like(i, V), "ascending": i % V}[tokens]
+    check_exact_gradient(mkq, t, V, D, "f32", "f32", M)
+
+
+@pytest.mark.parametrize("dt,gt", [("f32", "f32"), ("bf16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("M,V,D", [(300000, 1000, 8), (300000, 200000, 4), (65536, 30522, 32), (12288, 5000, 24), (12289, 5000, 7), (1200000, 90, 8),
+                                   (1200000, 90, 3), (20000, 2 ** 18, 8), (100000, 2 ** 18 - 1, 8), (13000, 2 ** 27, 1)])
+def test_exact_gradient_of_long_batches(mkq, M, V, D, dt, gt):
+    """One digit to four, and runs of up to 180000 positions"""
+    t = some_tokens(M, V, 1, torch.int32) if V <= 2 ** 20 else torch.randint(0, V, (M,), generator=torch.Generator().manual_seed(1)).repeat_interleave(3)[:M]
+    check_exact_gradient(mkq, t.cuda(), V, D, dt, gt, M + D)
+
+
+@pytest.mark.parametrize("chunks", [2, 3, 15, 16, 17, 18, 31, 32, 33, 48, 64, 272, 273, 300])
+@pytest.mark.parametrize("begin", [0, 1, 8 * 15, 8 * 16 - 1, 8 * 17])
+def test_exact_gradient_of_runs_over_any_number_of_chunks(mkq, chunks, begin):
+    """A run of one token in a sorted batch that begins and ends at, before and behind the borders of chunks and of their sixteens"""
+    for end in (-1, 0, 1):
+        n = 8 * chunks + end
+        t = torch.cat([torch.arange(begin), torch.full((n,), 5000), 5001 + torch.arange(40)]).int()
+        check_exact_gradient(mkq, t.cuda(), 6000, 8, "f32", "f32", chunks)
+
+
+@pytest.mark.parametrize("dt,gt", [("f32", "f16"), ("f32", "bf16"), ("f16", "bf16"), ("bf16", "f16")])
+@pytest.mark.parametrize("M,V,D", [(700, 100, 24), (700, 100, 21), (13000, 500, 16)])
+def test_gradient_between_types(mkq, M, V, D, dt, gt):
+    g = torch.Generator().manual_seed(M + D)
+    t, dy = some_tokens(M, V, M), torch.randn(M, D, generator=g).to(T[dt])
+    check_gradient(mkq.mkq_embedding_gradient(t.cuda(), dy.cuda(), V, -1.5, code(mkq, gt)), t, dy, V, -1.5)
+    start = torch.randn(V, D, generator=g).to(T[gt])
+    got = mkq.mkq_embedding_gradient(t.cuda(), dy.cuda(), V, -1.5, code(mkq, gt), grad=start.cuda(), accumulate=True)
+    check_gradient(got, t, dy, V, -1.5, start=start)

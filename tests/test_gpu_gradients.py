@@ -211,3 +211,11 @@ def test_results_beside_and_over_other_tensors(mkq):
         with pytest.raises(ValueError):
             mkq.mkq_clip_gradients(grads, 1.0, outs=outs)
     assert torch.equal(flat, before)
+
+
+def test_norm_of_a_hundred_and_more_tensors_and_their_clipping_in_place(mkq):
+    """The tensors of twelve layers with a table: more than a launch's arguments hold, so two lists of partial sums and of results"""
+    h, f = 96, 384
+    layer = [3 * h * h, 3 * h, h * h, h, f * h, f, h * f, h, h, h, h, h]
+    ts = tensors([5000 * h, 5000] + 12 * layer, 13, [torch.float32])
+    check(mkq, ts, 0.25 * true_norm(ts), True)
