@@ -417,7 +417,7 @@ int mkq_attention_int8(const void *qkv, int64_t batch, int64_t seq, int64_t hidd
  *   rows    ceil(K / 32) * 16 bytes: the canonical nibble packing, zero codes from K up to the next multiple of 32; any K > 0
  *   steps   s_w [N, ceil(K / group)] binary32, step g of a row for its codes g * group .. ; the last group may be short
  * mkq_pack_weights_int4_group: W [N, K] of w_dtype (F32, F16, BF16), row stride ldw; every group's step is its abs-max / 7
- * (all zeros -> 1) unless s_w_in gives them (then > 0 and below 2^120, a precondition), its codes are Eq. 1 of section 3.1
+ * (all zeros -> 1) unless s_w_in gives them (then > 0 and below 2^120, a precondition; for weights below 2^122 its own are), its codes are Eq. 1 of section 3.1
  * under that step; s_w_out may alias s_w_in.  N == 0 is a no-op.  Steps and biases of what follows need only the alignment of
  * a binary32 value, so that rows of a table can be passed on their own.
  * Errors: NULL, SHAPE (N < 0, K <= 0, ldw < K, group), ALIGN, DTYPE, UNSUPPORTED (N or K from about 2^31 on), HIP. */

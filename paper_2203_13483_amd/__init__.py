@@ -647,7 +647,9 @@ def mkq_attention_varlen(qkv, cu_seqlens, max_seq: int, hidden: int, heads: int,
 
 
 # The two ends of an encoder and the training of its table.  These take tensors as programs have them, so what would be read
-# wrongly is refused here: strides that the call cannot express, tensors of another device, sizes that do not agree.
+# wrongly is refused here: strides that the call cannot express, tensors of another device, sizes that do not agree.  Nothing is
+# recorded by autograd, whatever requires a gradient: results have no graph, and what is written in place or into ``out`` keeps its
+# version.  A training program joins lookup and gradient itself, in a torch.autograd.Function or a step of its own.
 
 def _need(ok, what: str):
     if not ok:
@@ -808,7 +810,8 @@ def _token_rows(tokens, D: int, out, dtype, stream):
 
 
 def mkq_embedding(tokens, table, scale: float = 1.0, out_dtype: int | None = None, *, out=None, stream=None):
-    """Rows of table [V,D] for tokens (int32 / int64, any shape, M of them) times scale -> [M,D] of out_dtype (None: the table's)."""
+    """Rows of table [V,D] for tokens (int32 / int64, any shape, M of them) times scale -> [M,D] of out_dtype (None: the table's).
+    Autograd does not see it: the table's gradient is mkq_embedding_gradient."""
     bits = _tokens(tokens)
     ld_table, table_dtype = _rows(table, "table"), _float_code(table, "table")
     V, D = table.shape
@@ -840,7 +843,8 @@ def mkq_embedding_gradient_workspace_bytes(M: int, D: int) -> int:
 
 def mkq_embedding_gradient(tokens, dy, V: int, scale: float = 1.0, grad_dtype: int = MKQ_F32, *, padding_token: int = -1,
                            grad=None, accumulate: bool = False, workspace=None, stream=None):
-    """Gradient [V,D] of mkq_embedding's table from dy [M,D].  ``accumulate``: added to the ``grad`` that is passed in."""
+    """Gradient [V,D] of mkq_embedding's table from dy [M,D] (outside autograd).  ``accumulate``: added to the ``grad`` that is
+    passed in."""
     torch = _torch()
     bits = _tokens(tokens)
     ld_dy, dy_dtype, dtype = _rows(dy, "dy"), _float_code(dy, "dy"), _float_dtype(grad_dtype, "grad_dtype")

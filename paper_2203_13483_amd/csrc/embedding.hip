@@ -3,9 +3,9 @@
 //     out[i,:] = scale * table[t_i,:]              dT[v,:] = scale * sum_{i: t_i = v} dy[i,:]
 //
 // All are bound by bytes: the rows read and written, and for the gradient the whole of dT, whose rows without a token are
-// zeros.  A lookup is one multiplication in binary32 and one rounding per value.  Gradients, us: 4096 binary16 tokens of 768 into
-// binary32 [30522, 768] 28 (18 sorting beside the zeros, 5 sums, 7 joining), 65536 bfloat16 tokens of 1024 into [30522, 1024] 94 (35
-// sorting beside the zeros, 49 sums: 4.6 TB/s, 8 joining).
+// zeros.  A lookup is one multiplication in binary32 and one rounding per value.  Gradients, us, a call among others (and its kernels, each
+// traced by itself): 4096 binary16 tokens of 768 into binary32 [30522, 768] 28.5 (18 sorting beside the zeros, 5 sums, 6 joining),
+// 65536 bfloat16 tokens of 1024 into [30522, 1024] 95 (35 in four launches that sort beside the zeros, 45 to 50 sums: 4.6 TB/s, 8 joining).
 #include "elements.h"
 
 namespace mkq {
@@ -632,7 +632,10 @@ static int launch_lookup(LookupParams p, bool table_vec, int out_dtype, hipStrea
     const int64_t units = ceil_div(p.D, 8);
     p.threads_per_row = (int)(units < 256 ? units : 256);
     const int rows = 256 / p.threads_per_row;
-    // four rows a thread where that still leaves a workgroup for every place on the chip, eight a CU
+    // Four rows a thread where that still leaves a workgroup for every place on the chip, eight a CU.  One | four, us, binary16 rows of 768 from
+    // as many: 2048 tokens 3.5 | 3.9, 4096 4.7 | 4.6, 8192 7.8 | 6.6, 16384 (from where four are taken) 12.0 | 9.3, 65536 47.6 | 38.1; from
+    // nibbles 3.0 | 4.0, 3.9 | 4.5, 6.0 | 5.9, 9.6 | 8.1, 38.1 | 31.2; rows of 1001 8192 11.4 | 15.7, 16384 19.9 | 17.5, 65536 101 | 97.  binary32 rows
+    // lose a little by it: of 768 16384 16.6 | 16.9, 65536 73.9 | 76.9, of 2056 32768 97 | 110, but from nibbles 60.5 | 57.4 and 84 | 80.
     const bool four = p.M >= (int64_t)rows * 4 * 2048;
     int64_t workgroups = ceil_div(p.M, rows * (four ? 4 : 1));
     if (workgroups > 1 << 20) workgroups = 1 << 20;

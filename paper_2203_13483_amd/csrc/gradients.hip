@@ -178,7 +178,8 @@ __device__ __forceinline__ void scale_values_small(const void *p, void *q, int64
     for (int i = threadIdx.x; i < values; i += 256) out[i] = E::put((float)((double)E::get(g[i]) * c));
 }
 
-// Every workgroup adds up the partial sums itself (16 KB out of the L2), which spares a launch between the two passes.
+// Every workgroup adds up the partial sums itself (up to 16 KB out of the L2 for every hundred tensors), which spares a launch between
+// the two passes.
 // Last pieces first: they were read last, and what the memory-side cache still holds of them need not come from HBM again.
 // A factor of 1 leaves gradients that are clipped in place as they are.  Without a limit (max_norm = infinity) it is 1 whatever the
 // norm: infinity over an infinite norm would make every finite gradient a NaN.

@@ -8,10 +8,12 @@
 // Activations enter exactly too: binary16 and bfloat16 ones as they are, binary32 ones as the sum of three bfloat16 parts
 // (8 + 8 + 8 bits).
 //
-// Bound: the weights' bytes for few tokens, by the instructions that turn codes into operands from about 30 on.  Measured, us:
-// one token, K = 768, N = 30522, groups of 64 6.2 (2.1 TB/s); K = 8192, N = 28672, groups of 128: 1 token 26 (4.8 TB/s; the same loads
-// with the arithmetic left out 23.5), 16 tokens 33 (3.8), 32 tokens 43, 64 tokens 53 (566 TFLOP/s); 120 tokens, K = 1024,
-// N = 30522 14.5 (516 TFLOP/s).
+// Bound: the weights' bytes for few tokens; from about ten on by waits between the loads, the barriers of the chunks and the
+// instructions that turn codes into operands, none of which is busy all the time.  Of the SIMDs' cycles, vector issue and the matrix
+// pipe take 58 % and 10 % for 16 bfloat16 tokens, K = 8192, N = 28672, 46 % and 25 % for 120 binary16 tokens, K = 1024, N = 30522, and
+// waves wait 47 % and 43 % of theirs.  Measured in a graph, binary16, us: one token, K = 768, N = 30522, groups of 64 6.3 (2.1 TB/s; 7.0 under
+// a trace, by itself); K = 8192, N = 28672, groups of 128: 1 token 27 (4.6 TB/s; the same loads with the arithmetic left out 23.5),
+// 16 tokens 32 (4.0), 32 tokens 43, 64 tokens 54 (557 TFLOP/s); 120 tokens, K = 1024, N = 30522 15.3 (490 TFLOP/s).
 #include <type_traits>
 
 #include "elements.h"
@@ -145,7 +147,8 @@ struct Product<ElemBF16> {
     __device__ static __forceinline__ v16f mul(V x, V c, v16f s) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, c, s, 0, 0, 0); }
 };
 // x = hi + mid + lo: each part is the upper half of what is left (its first 8 bits), and what is left is exact, down to multiples of
-// 2^-133, bfloat16's smallest number (the matrix instruction takes those below its normal ones as they are); nothing is left of an infinity, and a NaN stays one.  The smallest part is multiplied first.
+// 2^-133, bfloat16's smallest number (the matrix instruction takes those below its normal ones as they are); nothing is left of an
+// infinity, and a NaN stays one.  The smallest part is multiplied first.
 template <>
 struct Product<ElemF32> : Product<ElemBF16> {
     static constexpr int PARTS = 3;
@@ -292,7 +295,10 @@ __device__ __forceinline__ void store_tile(const Group4Params &p, typename Tile<
     else write(ElemBF16());
 }
 
-// Steps of 128 codes between two hand-overs of activations: what 64 KB of LDS and eight vectors a thread allow
+// Steps of 128 codes between two hand-overs of activations: four where the workgroup's x then takes 64 KiB of LDS, else two, at most
+// eight vectors a thread.  Two steps take more than that in <32, 2, 8, 2>, <32, 1, 8, 4> and <16, 1, 16, 8> (135 to 141 KiB with the weights'
+// steps) and in binary32's <16, 1, 8, 2> (101 to 104): one workgroup a CU there and in <16, 1, 16, 2> with groups of 32 (82), two with
+// the others (51 to 75).  A call of fewer tokens than a tile's takes less.
 template <class E, int G, int TN, int MT, int WAVES, int KS>
 struct Shape {
     static constexpr int PARTS = Product<E>::PARTS, ROWS = TN * MT;
@@ -532,15 +538,19 @@ static int launch_group4(Group4Params p, hipStream_t st)
 
 // Which tile, and how many of a workgroup's waves (eight) share its k loop: the largest tile whose workgroups fill the chip, since a tile
 // of more tokens converts a code for more of them, and channels that share a workgroup read x once.  us, binary16, tokens of a tile and
-// sharing waves: 120 tokens, K = 1024, N = 30522 14.5 (64, 1), 19.5 (64, 2), 20.8 (32, 2); 64 tokens, K = 8192, N = 28672 77.6 (64, 1), 53.1
-// (64, 2), 67.6 (32, 2), 94.9 (16, 2); 128 tokens, K = 4096, N = 8192 26.7 (64, 2), 19.5 (32, 2), 25.9 (32, 4), 35.6 (16, 4), K = 1024, N = 4096
-// 11.3, 8.8, 7.4, 10.0; 64 tokens, K = N = 4096 25.7 (64, 2), 13.3 (32, 4), 11.2 (16, 2), 10.9 (16, 4); one token, K = 768, N = 30522 6.2
-// (16, 2), 7.5 (16, 4), K = 4096, N = 16384 11.1 and 9.6.  Sixteen waves where x is much of what is read: K = 8192, N = 28672 16 tokens 33.5
-// instead of 35.2, 8 tokens 32.0 instead of 32.8, but one token 28.5 instead of 27.6; and eight of them on one k loop where that is
-// long: one token, K = 28672, N = 8192 30.7 instead of 37.8, K = N = 8192 10.3 instead of 11.3, but K = 4096, N = 16384 12.1 instead of 9.6.
-// Workgroups of four waves where even the last leave CUs idle: 16 tokens,
-// K = N = 4096 7.5 instead of 7.8, one token, K = N = 768 3.3 instead of 3.6.  binary32 has 16 tokens a tile: its three parts leave larger tiles
-// short chunks; 48 tokens, K = 768, N = 30522 17.0 (16, 1), 31.7 (16, 2), 16 tokens, K = 4096, N = 8192 27.8 and 19.8.
+// sharing waves: 120 tokens, K = 1024, N = 30522 15.3 (64, 1), 19.9 (64, 2), 21.3 (32, 2); 64 tokens, K = 8192, N = 28672 77.4 (64, 1), 54.8
+// (64, 2), 68.7 (32, 2), 99.5 (16, 2); 128 tokens, K = 4096, N = 8192 25.9 (64, 2), 19.5 (32, 2), 25.0 (32, 4), K = 1024, N = 4096
+// 9.1, 7.2, 6.2; 64 tokens, K = N = 4096 23.9 (64, 2), 12.6 (32, 4), 10.6 (16, 2), 11.2 (16, 4); one token, K = 768, N = 30522 6.3
+// (16, 2), 7.6 (16, 4), K = 4096, N = 16384 10.2 and 9.7.  Sixteen waves where x is much of what is read: K = 8192, N = 28672 16 tokens 32.3
+// instead of 34.1, 8 tokens 29.7 instead of 30.5, but one token 28.4 instead of 26.5; and eight of them on one k loop where that is
+// long: one token, K = 28672, N = 8192 30.8 instead of 37.9, K = N = 8192 10.4 instead of 11.3, but K = 4096, N = 16384 12.2 instead of 9.7.
+// Workgroups of four waves where even the last leave CUs idle, whatever K is; four | eight | sixteen with eight on a k loop, N = 768, one
+// token, groups of 64: K = 768 3.4 | 3.7 | 4.2, 1200 4.2 | 4.3 | 4.1, 4096 6.1 | 6.4 | 6.1, 8192 9.9 | 10.2 | 8.9, 16384 17.7 | 17.8 | 14.6; 16
+// tokens: 3.8 | 3.9 | 4.4, 4.8 | 4.7 | 4.5, 7.0 | 7.2 | 6.8, 11.4 | 11.6 | 10.3, 20.4 | 20.7 | 17.3: from K = 8192 on the sixteen would be better here, too.
+// binary32 has 16 tokens a tile: its three parts leave larger tiles short chunks.  One | two waves on a k loop, groups of 64: 48 tokens,
+// N = 30522, K = 768 16.4 | 32.0, K = 8192 147 | 209; 16 tokens, N = 8192, K = 768 7.2 | 6.3, K = 8192 53.5 | 34.8; between those, where two share
+// a loop but take more than one round of the CUs, one would be better: 16 tokens, N = 30522, K = 768 8.0 | 11.9, K = 8192 56 | 71, 48 tokens,
+// N = 16384, K = 768 10.6 | 16.3, N = 8192 7.5 | 11.2.
 template <class E, int G>
 static int choose_group4(const Group4Params &p, hipStream_t st)
 {
