@@ -468,3 +468,27 @@ def test_gradient_between_types(mkq, M, V, D, dt, gt):
     start = torch.randn(V, D, generator=g).to(T[gt])
     got = mkq.mkq_embedding_gradient(t.cuda(), dy.cuda(), V, -1.5, code(mkq, gt), grad=start.cuda(), accumulate=True)
     check_gradient(got, t, dy, V, -1.5, start=start)
+
+
+@pytest.mark.parametrize("M,D", [(300, 5000), (300, 5001), (2000, 20000), (2000, 20003)])
+def test_exact_gradient_of_long_rows(mkq, M, D):
+    """Columns in several rounds of a workgroup, and long runs whose shares of the columns are more than one round"""
+    check_exact_gradient(mkq, torch.where(torch.arange(M) % 5 == 0, torch.arange(M) % 7, 2).cuda(), 9, D, "f32", "f32", M + D)
+
+
+def test_lookups_and_gradient_on_other_streams_at_once(mkq):
+    """All three on streams of their own at the same time, inputs made on the current one"""
+    M, V, D = 6000, 2000, 320
+    table = torch.randn(V, D, generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    Wq, s = mkq.mkq_pack_weights_int4_group(table, 32)
+    t = torch.randint(0, V, (M,), generator=torch.Generator("cuda").manual_seed(2), device="cuda")
+    dy = torch.randint(-9, 10, (M, D), generator=torch.Generator("cuda").manual_seed(3), device="cuda").float()
+    calls = [lambda **kw: mkq.mkq_embedding(t, table, 0.3, **kw), lambda **kw: mkq.mkq_embedding_int4_group(t, Wq, s, V, D, 32, 0.3, **kw),
+             lambda **kw: mkq.mkq_embedding_gradient(t, dy, V, **kw)]
+    want = [f() for f in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        got = [f(stream=st) for f, st in zip(calls, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))

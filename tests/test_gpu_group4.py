@@ -351,3 +351,19 @@ def test_binary32_activations_down_to_the_smallest(mkq, M, N):
         tol = lost + (3 * K + 4) * 2.0 ** -23 * (S + lost) + (3 * K + 4) * 2.0 ** -149
         off = (got.double() - xd @ c.T).abs()
         assert bool((off <= tol).all()), (low, float((off / tol).max()))
+
+
+@pytest.mark.parametrize("xt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1030, 333, 264), (4097, 40, 96), (515, 5000, 520)])
+def test_many_tokens_are_exact_on_whole_numbers(mkq, M, N, K, xt):
+    """Scores of every position of a batch: many tiles of tokens, the last one short"""
+    g = torch.Generator("cuda").manual_seed(M)
+    codes = torch.randint(-8, 8, (N, -(-K // 32) * 32), generator=g, device="cuda")
+    codes[:, K:] = 0
+    s = 2.0 ** torch.randint(-3, 4, (N, -(-K // 64)), generator=g, device="cuda").float()
+    x = torch.randint(-15, 16, (M, K), generator=g, device="cuda").to(T[xt])
+    Wq = ((codes[:, 0::2] % 16) + 16 * (codes[:, 1::2] % 16)).to(torch.uint8)
+    room = torch.full((M * N + 64,), -77.25, device="cuda")
+    got = mkq.mkq_linear_int4_group(x, Wq, s, None, N, K, 64, mkq.MKQ_F32, out=room[:M * N].view(M, N))
+    w = codes[:, :K].double() * s.double().repeat_interleave(64, 1)[:, :K]
+    assert torch.equal(got.double(), x.double() @ w.T.contiguous()) and bool((room[M * N:] == -77.25).all())
