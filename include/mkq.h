@@ -494,6 +494,53 @@ int mkq_clip_gradients(int64_t n, const void *const *grads_host, void *const *ou
                        const int32_t *dtypes_host, float max_norm, float *norm_out, void *workspace, size_t workspace_bytes,
                        void *stream);
 
+/* Log probabilities of given tokens under rows of scores (of mkq_linear_int4_group as a head, or any other), entropies and the most
+ * probable alternatives, in one pass over the scores; and the gradient of the first two.  With z = scale * logits[m,:]:
+ *     normalizers[m] = (max_j logits[m,j],  L = log sum_j exp(z_j - max z)),    log p_j = z_j - max z - L
+ *     log_probs[m]   = log p_t, t = tokens[m];  0 for a token outside [0, V)
+ *     entropies[m]   = -sum_j p_j log p_j
+ *     top_tokens[m]  = the `top` tokens with the largest scores, equal scores (0 and -0 too) by the lower token, with their log p
+ *     grad[m,j]      = scale ( d_log_probs[m] (delta_jt - p_j)  -  d_entropies[m] p_j (log p_j + entropies[m]) )
+ * -infinity forbids a token: p = 0, its gradient is 0.  A row of nothing else has no distribution: log probabilities and L are -infinity,
+ * the entropy is 0, its gradient zeros.  A NaN or +infinity makes its row's results NaN (a NaN is ordered as -infinity).  A row whose d_log_probs
+ * (or whose token is outside) and d_entropies are 0 has zeros for a gradient, whatever its scores are.  top_log_probs have no gradient here.
+ *   logits  [M, V] of dtype (F32, F16, BF16), row stride ld: any, rows are read in aligned pieces of 16 bytes
+ *   scale   1 / temperature, 2^-100 .. 2^100;  tokens [M] of token_bits (32 or 64) bits, aligned to their own size
+ *   normalizers [M, 2] (8-byte aligned), log_probs [M], entropies [M], top_tokens and top_log_probs [M, top] (NULL if top == 0): binary32, int32
+ *   top     0 .. min(V, 64)
+ *   workspace  at least mkq_token_log_probs_workspace_bytes(M, V, top) bytes (0: may be NULL), 16-byte aligned; no preparation.  Two calls
+ *              that may run at the same time need two.
+ *   grad    [M, V] of grad_dtype (F32, F16, BF16), row stride ld_grad (what lies between the rows is left as it is); the logits themselves if type
+ *           and stride are theirs, otherwise apart from them (else UNSUPPORTED).  Strides that differ by no multiple of 8 are slower.
+ *   d_log_probs [M];  d_entropies [M], or NULL (then entropies may be NULL)
+ * Exponents and sums are binary32, log probabilities are off by about 1e-7 plus as much of their own size.  Equal calls give equal bits.
+ * M == 0 is a no-op.  Errors: NULL, SHAPE (top > V too), ALIGN, SCALE, DTYPE (token_bits too), WORKSPACE, UNSUPPORTED (top > 64), HIP. */
+size_t mkq_token_log_probs_workspace_bytes(int64_t M, int64_t V, int top);
+int mkq_token_log_probs(const void *logits, int dtype, int64_t ld, int64_t M, int64_t V, float scale, const void *tokens, int token_bits,
+                        float *normalizers, float *log_probs, float *entropies, int top, int32_t *top_tokens, float *top_log_probs,
+                        void *workspace, size_t workspace_bytes, void *stream);
+int mkq_token_log_probs_gradient(const void *logits, int dtype, int64_t ld, int64_t M, int64_t V, float scale, const void *tokens,
+                                 int token_bits, const float *normalizers, const float *entropies, const float *d_log_probs,
+                                 const float *d_entropies, void *grad, int grad_dtype, int64_t ld_grad, void *stream);
+
+/* Activations kept in 8 bits from the forward pass to the backward, with a step for every `group` (32, 64 or 128) neighbours of a row.
+ *   step  = max|x| / 127 of the group (binary32, between 2^-126 and the largest of which 127 are finite; all zeros -> 1);  a group with an infinity or a NaN: step NaN, codes 0
+ *   code  = x / step rounded to the nearest whole number, ties to even, decided exactly
+ *   codes mkq_checkpoint_bytes(M, K): rows of ceil(K / 32) * 32 bytes, zero codes past K;  steps [M, ceil(K / group)] binary32
+ * mkq_checkpoint_int8           x [M, K] of x_dtype (F32, F16, BF16), row stride ldx -> codes, steps
+ * mkq_checkpoint_restore        out = act(code * step) of out_dtype (MKQ_ACT_NONE, or MKQ_ACT_GELU: what stood behind it), row stride ld_out
+ * mkq_checkpoint_gelu_gradient  dx = dy (Phi(x) + x phi(x)), x = code * step; dx may be dy if type and stride are its own, otherwise it is apart
+ *                               from it (else UNSUPPORTED)
+ * What lies between rows of out and dx is left as it is.  Any K; multiples of 8 in rows that are multiples of 16 bytes are faster.
+ * mkq_low_rank_adapters_gradient reads such rows in the place of x.  M == 0 is a no-op.
+ * Errors: NULL, SHAPE (group too), ALIGN, DTYPE (act too), UNSUPPORTED, HIP. */
+size_t mkq_checkpoint_bytes(int64_t M, int64_t K);
+int mkq_checkpoint_int8(const void *x, int x_dtype, int64_t M, int64_t K, int64_t ldx, int group, int8_t *codes, float *steps, void *stream);
+int mkq_checkpoint_restore(const int8_t *codes, const float *steps, int group, int64_t M, int64_t K, int act, void *out, int out_dtype,
+                           int64_t ld_out, void *stream);
+int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int group, int64_t M, int64_t K, const void *dy, int dy_dtype,
+                                 int64_t ld_dy, void *dx, int dx_dtype, int64_t ld_dx, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

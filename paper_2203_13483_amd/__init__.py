@@ -37,6 +37,8 @@ EXPORTS = [
     "mkq_group_weight_bytes", "mkq_pack_weights_int4_group", "mkq_linear_int4_group",
     "mkq_embedding", "mkq_embedding_int4_group", "mkq_embedding_gradient_workspace_bytes", "mkq_embedding_gradient",
     "mkq_gradient_norm_workspace_bytes", "mkq_gradient_norm", "mkq_clip_gradients",
+    "mkq_token_log_probs_workspace_bytes", "mkq_token_log_probs", "mkq_token_log_probs_gradient",
+    "mkq_checkpoint_bytes", "mkq_checkpoint_int8", "mkq_checkpoint_restore", "mkq_checkpoint_gelu_gradient",
     "mkq_measure_stream", "mkq_measure_mfma_i8_operand_bytes", "mkq_measure_mfma_i8_ops", "mkq_measure_mfma_i8",
 ]
 
@@ -158,6 +160,15 @@ def load() -> C.CDLL:
         "mkq_gradient_norm": (ci, [i64, vp, vp, vp, vp, vp, sz, vp]),
         "mkq_clip_gradients": (ci, [i64, vp, vp, vp, vp, f32, vp, vp, sz, vp]),
     }
+    sig.update({
+        "mkq_token_log_probs_workspace_bytes": (sz, [i64, i64, ci]),
+        "mkq_token_log_probs": (ci, [vp, ci, i64, i64, i64, f32, vp, ci, vp, vp, vp, ci, vp, vp, vp, sz, vp]),
+        "mkq_token_log_probs_gradient": (ci, [vp, ci, i64, i64, i64, f32, vp, ci, vp, vp, vp, vp, vp, ci, i64, vp]),
+        "mkq_checkpoint_bytes": (sz, [i64, i64]),
+        "mkq_checkpoint_int8": (ci, [vp, ci, i64, i64, i64, ci, vp, vp, vp]),
+        "mkq_checkpoint_restore": (ci, [vp, vp, ci, i64, i64, ci, vp, ci, i64, vp]),
+        "mkq_checkpoint_gelu_gradient": (ci, [vp, vp, ci, i64, i64, vp, ci, i64, vp, ci, i64, vp]),
+    })
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
@@ -940,6 +951,135 @@ def mkq_clip_gradients(grads, max_norm: float, *, outs=None, norm_out=None, work
         raise ValueError("no result over another one or over another gradient: it would be scaled twice")
     _check(status, "mkq_clip_gradients")
     return norm_out
+
+
+class TokenLogProbs:
+    """What mkq_token_log_probs gives: float32 ``log_probs`` [M], ``entropies`` [M], ``normalizers`` [M,2] (largest score, logarithm of the sum
+    of the exponentials relative to it), ``top_tokens`` int32 [M,top] with ``top_log_probs``."""
+    __slots__ = ("log_probs", "entropies", "normalizers", "top_tokens", "top_log_probs")
+
+
+def mkq_token_log_probs_workspace_bytes(M: int, V: int, top: int = 0) -> int:
+    return int(load().mkq_token_log_probs_workspace_bytes(M, V, top))
+
+
+def _vector(t, n: int, what: str):
+    """A contiguous float32 vector of n values."""
+    _need(t.dtype == _torch().float32 and t.is_contiguous() and t.numel() == n, f"{what}: contiguous float32 [{n}]")
+
+
+def mkq_token_log_probs(logits, tokens, scale: float = 1.0, top: int = 0, *, workspace=None, stream=None) -> TokenLogProbs:
+    """Log probabilities of tokens [M] (int32 / int64; outside the vocabulary: 0) under scale * logits [M,V], entropies, and the ``top`` most
+    probable tokens of every row."""
+    torch = _torch()
+    ld, dtype, bits = _rows(logits, "logits"), _float_code(logits, "logits"), _tokens(tokens)
+    M, V = logits.shape
+    top = int(top)
+    _need(tokens.numel() == M, "tokens: one for every row")
+    _need(0 <= top <= V, "top: at most the vocabulary")
+    _workspace(workspace)
+    dev = _same_device(logits, tokens, workspace)
+    r, device = TokenLogProbs(), logits.device
+    r.log_probs, r.entropies = _new(M, torch.float32, device, stream), _new(M, torch.float32, device, stream)
+    r.normalizers = _new((M, 2), torch.float32, device, stream)
+    r.top_tokens, r.top_log_probs = _new((M, top), torch.int32, device, stream), _new((M, top), torch.float32, device, stream)
+    if workspace is None:
+        need = mkq_token_log_probs_workspace_bytes(M, V, top)
+        workspace = _new(need, torch.uint8, device, stream) if need else None
+    _check(load().mkq_token_log_probs(_ptr(logits), dtype, ld, M, V, float(scale), _ptr(tokens), bits, _ptr(r.normalizers), _ptr(r.log_probs),
+                                      _ptr(r.entropies), top, _ptr(r.top_tokens), _ptr(r.top_log_probs), _ptr(workspace),
+                                      0 if workspace is None else workspace.nbytes, _stream_on(dev, stream)), "mkq_token_log_probs")
+    return r
+
+
+def mkq_token_log_probs_gradient(logits, tokens, result: TokenLogProbs, d_log_probs, scale: float = 1.0, grad_dtype: int | None = None, *,
+                                 d_entropies=None, grad=None, stream=None):
+    """Gradient [M,V] of grad_dtype (None: the logits') of what mkq_token_log_probs gave for the same logits, tokens and scale, from the
+    gradients of its log probabilities and, optionally, entropies.  ``grad``: where it goes, the logits themselves too."""
+    ld, dtype, bits = _rows(logits, "logits"), _float_code(logits, "logits"), _tokens(tokens)
+    M, V = logits.shape
+    _need(tokens.numel() == M, "tokens: one for every row")
+    normalizers, entropies = result.normalizers, result.entropies
+    _vector(normalizers, 2 * M, "normalizers")
+    _vector(entropies, M, "entropies")
+    _vector(d_log_probs, M, "d_log_probs")
+    if d_entropies is not None:
+        _vector(d_entropies, M, "d_entropies")
+    if grad_dtype is None:
+        grad_dtype = dtype
+    to = _float_dtype(grad_dtype, "grad_dtype")
+    dev = _same_device(logits, tokens, normalizers, entropies, d_log_probs, d_entropies, grad)
+    if grad is None:
+        grad, ld_grad = _new_matrix(M, V, to, logits.device, stream), V
+    else:
+        ld_grad = _rows(grad, "grad")
+        _need(grad.dtype == to and tuple(grad.shape) == (M, V), "grad: [M, V] of grad_dtype")
+    _check(load().mkq_token_log_probs_gradient(_ptr(logits), dtype, ld, M, V, float(scale), _ptr(tokens), bits, _ptr(normalizers),
+                                               _ptr(entropies), _ptr(d_log_probs), _ptr(d_entropies), _ptr(grad), int(grad_dtype),
+                                               ld_grad, _stream_on(dev, stream)), "mkq_token_log_probs_gradient")
+    return grad
+
+
+def mkq_checkpoint_int8(x, group: int = 128, *, stream=None):
+    """x [M,K] float32/float16/bfloat16 kept in 8 bits -> (codes int8 [M, ceil(K/32)*32], steps float32 [M, ceil(K/group)])."""
+    torch = _torch()
+    ldx, dtype = _rows(x, "x"), _float_code(x, "x")
+    M, K = x.shape
+    _need(group in (32, 64, 128), "group: 32, 64 or 128")
+    dev = _same_device(x)
+    codes = _new_matrix(M, -(-K // 32) * 32, torch.int8, x.device, stream)
+    steps = _new_matrix(M, -(-K // group), torch.float32, x.device, stream)
+    _check(load().mkq_checkpoint_int8(_ptr(x), dtype, M, K, ldx, group, _ptr(codes), _ptr(steps), _stream_on(dev, stream)),
+           "mkq_checkpoint_int8")
+    return codes, steps
+
+
+def _checkpoint(codes, steps, K: int, group: int, what: str = "codes") -> int:
+    """Rows of a checkpoint of K columns."""
+    torch = _torch()
+    _need(group in (32, 64, 128), "group: 32, 64 or 128")
+    _need(codes.dtype == torch.int8 and codes.is_contiguous() and codes.dim() == 2 and codes.size(1) == -(-K // 32) * 32,
+          f"{what}: contiguous int8 [M, ceil(K/32)*32]")
+    M = codes.size(0)
+    _need(steps.dtype == torch.float32 and steps.is_contiguous() and tuple(steps.shape) == (M, -(-K // group)),
+          "steps: contiguous float32 [M, ceil(K/group)]")
+    return M
+
+
+def _out_rows(out, M: int, K: int, dtype, device, stream, what: str):
+    """The caller's [M, K] rows, or new ones, and their stride."""
+    if out is None:
+        return _new_matrix(M, K, dtype, device, stream), K
+    ld = _rows(out, what)
+    _need(out.dtype == dtype and tuple(out.shape) == (M, K), f"{what}: [{M}, {K}] of its type")
+    return out, ld
+
+
+def mkq_checkpoint_restore(codes, steps, K: int, group: int = 128, out_dtype: int = MKQ_F32, *, act: int = MKQ_ACT_NONE, out=None,
+                           stream=None):
+    """The [M,K] activations of mkq_checkpoint_int8 again, or their GELU."""
+    M, dtype = _checkpoint(codes, steps, K, group), _float_dtype(out_dtype, "out_dtype")
+    dev = _same_device(codes, steps, out)
+    out, ld_out = _out_rows(out, M, K, dtype, codes.device, stream, "out")
+    _check(load().mkq_checkpoint_restore(_ptr(codes), _ptr(steps), group, M, K, int(act), _ptr(out), int(out_dtype), ld_out,
+                                         _stream_on(dev, stream)), "mkq_checkpoint_restore")
+    return out
+
+
+def mkq_checkpoint_gelu_gradient(codes, steps, dy, group: int = 128, dx_dtype: int | None = None, *, dx=None, stream=None):
+    """dy [M,K] times the GELU's derivative at the activations that mkq_checkpoint_int8 kept -> [M,K] of dx_dtype (None: dy's).  ``dx``: where it
+    goes, dy itself too."""
+    ld_dy, dy_dtype = _rows(dy, "dy"), _float_code(dy, "dy")
+    M, K = dy.shape
+    _need(_checkpoint(codes, steps, K, group) == M, "dy: a row for every row kept")
+    if dx_dtype is None:
+        dx_dtype = dy_dtype
+    dtype = _float_dtype(dx_dtype, "dx_dtype")
+    dev = _same_device(codes, steps, dy, dx)
+    dx, ld_dx = _out_rows(dx, M, K, dtype, dy.device, stream, "dx")
+    _check(load().mkq_checkpoint_gelu_gradient(_ptr(codes), _ptr(steps), group, M, K, _ptr(dy), dy_dtype, ld_dy, _ptr(dx), int(dx_dtype),
+                                               ld_dx, _stream_on(dev, stream)), "mkq_checkpoint_gelu_gradient")
+    return dx
 
 
 class BertLayerInt4:

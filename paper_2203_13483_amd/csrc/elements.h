@@ -36,6 +36,13 @@ __device__ __forceinline__ float product(float a, float b)
     return r;
 }
 
+// A result as it is in binary32, kept from being fused with its narrowing for the same reason
+__device__ __forceinline__ float in_binary32(float v)
+{
+    asm("" : "+v"(v));
+    return v;
+}
+
 // Eight neighbours as binary32, from an address that is a multiple of 16
 template <class E>
 __device__ __forceinline__ void get8(const typename E::raw *p, float (&v)[8])
@@ -96,6 +103,15 @@ inline void with_elem(int dtype, F &&f)
 inline bool rows_aligned16(const void *p, int64_t ld, int dtype) { return aligned16(p) && (ld * dtype_bytes(dtype)) % 16 == 0; }
 
 inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Whether results [M, K] lie apart from what they are computed from, value by value, or exactly over it
+inline bool in_place_or_apart(const void *in, int in_dtype, int64_t ld_in, const void *out, int out_dtype, int64_t ld_out, int64_t M, int64_t K)
+{
+    if (in == out && in_dtype == out_dtype && (ld_in == ld_out || M <= 1)) return true;
+    auto extent = [&](int64_t ld, int dtype) { return (uintptr_t)(((unsigned __int128)(M - 1) * (uint64_t)ld + (uint64_t)K) * (uint64_t)dtype_bytes(dtype)); };
+    const uintptr_t i = reinterpret_cast<uintptr_t>(in), o = reinterpret_cast<uintptr_t>(out);
+    return i + extent(ld_in, in_dtype) <= o || o + extent(ld_out, out_dtype) <= i;
+}
 
 // Workgroups of a launch: the grid's work items are counted in 32 bits
 inline bool grid_ok(int64_t workgroups, int threads) { return workgroups > 0 && workgroups * threads < ((int64_t)1 << 32); }
