@@ -541,6 +541,38 @@ int mkq_checkpoint_restore(const int8_t *codes, const float *steps, int group, i
 int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int group, int64_t M, int64_t K, const void *dy, int dy_dtype,
                                  int64_t ld_dy, void *dx, int dx_dtype, int64_t ld_dx, void *stream);
 
+/* Low-rank adapters of many requests beside a shared projection.  Row m of a batch has the adapter a = adapter[m]; outside [0, R): none.
+ *     hidden[m] = down_a x[m]                 out[m] = base[m] + s_a up_a^T hidden[m]
+ * and their gradients, of the same rows, with u[m] = s_a up_a dy[m]:
+ *     dx[m] = dx_base[m] + down_a^T u[m]      d_down_a = sum_m u[m] x[m]^T      d_up_a = s_a sum_m hidden[m] dy[m]^T
+ * base is what the projection gave (mkq_linear_int4_group or any other: out itself will do), or NULL; out without a base may be the `residual` of a
+ * linear whose epilogue follows.  A row without an adapter has hidden 0 and out = base (0 without one); an adapter without a row has gradients 0.
+ *   x, dy       [M, K], [M, N] of their dtype (F32, F16, BF16), row strides ldx, ld_dy (any; multiples of 16 bytes are faster)
+ *               x of the gradient also MKQ_I8: what mkq_checkpoint_int8 kept of it, with its steps and group (ldx is not read)
+ *   adapter     [M] int32.  Rows of one adapter are best side by side; a tile of rows is gone through once for each of its adapters
+ *   down, up    [R, rank, K], [R, rank, N] of w_dtype: the long side in rows, of both;  scales [R] binary32, or NULL: 1.  A smaller adapter
+ *               has zeros in its last rows
+ *   base, out   [M, N] of out_dtype;  dx_base, dx [M, K] of dx_dtype; their row strides.  A base is its result if the strides are the same, otherwise
+ *               apart from it; dx is apart from dy and x (else UNSUPPORTED).  What lies between the rows is left as it is
+ *   hidden      [M, rank] binary32: an output of the first, or NULL; needed for d_up
+ *   d_down, d_up  [R, rank, K], [R, rank, N] of grad_dtype (F32, F16, BF16); accumulate: added to what is there, with one rounding.  dx, d_down and
+ *               d_up may be NULL, but not all of them; what only they need may be NULL then
+ *   workspace   at least the *_workspace_bytes bytes, 16-byte aligned; no preparation.  Two calls that may run at the same time need two
+ * Products are exact, all sums and hidden are binary32 (sums of products with 16-bit results may leave out 2^-16 of a product); equal calls give
+ * equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
+ * rank 1 .. 256, R up to about 4e6 (UNSUPPORTED).  M == 0: the first does nothing, the second writes its zeros.
+ * Errors: NULL, SHAPE (x_group too), ALIGN, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
+size_t mkq_low_rank_adapters_workspace_bytes(int64_t M, int64_t K, int64_t N, int rank, int64_t R);
+int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, const int32_t *adapter, int64_t M, int64_t K, int64_t N, int rank, int64_t R,
+                          const void *down, const void *up, int w_dtype, const float *scales, const void *base, int64_t ld_base, void *out,
+                          int out_dtype, int64_t ld_out, float *hidden, void *workspace, size_t workspace_bytes, void *stream);
+size_t mkq_low_rank_adapters_gradient_workspace_bytes(int64_t M, int64_t K, int64_t N, int rank, int64_t R);
+int mkq_low_rank_adapters_gradient(const void *dy, int dy_dtype, int64_t ld_dy, const void *x, int x_dtype, int64_t ldx, const float *x_steps,
+                                   int x_group, const int32_t *adapter, const float *hidden, int64_t M, int64_t K, int64_t N, int rank, int64_t R,
+                                   const void *down, const void *up, int w_dtype, const float *scales, const void *dx_base, int64_t ld_dx_base,
+                                   void *dx, int dx_dtype, int64_t ld_dx, void *d_down, void *d_up, int grad_dtype, int accumulate,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

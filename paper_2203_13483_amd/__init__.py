@@ -39,6 +39,8 @@ EXPORTS = [
     "mkq_gradient_norm_workspace_bytes", "mkq_gradient_norm", "mkq_clip_gradients",
     "mkq_token_log_probs_workspace_bytes", "mkq_token_log_probs", "mkq_token_log_probs_gradient",
     "mkq_checkpoint_bytes", "mkq_checkpoint_int8", "mkq_checkpoint_restore", "mkq_checkpoint_gelu_gradient",
+    "mkq_low_rank_adapters_workspace_bytes", "mkq_low_rank_adapters", "mkq_low_rank_adapters_gradient_workspace_bytes",
+    "mkq_low_rank_adapters_gradient",
     "mkq_measure_stream", "mkq_measure_mfma_i8_operand_bytes", "mkq_measure_mfma_i8_ops", "mkq_measure_mfma_i8",
 ]
 
@@ -168,6 +170,11 @@ def load() -> C.CDLL:
         "mkq_checkpoint_int8": (ci, [vp, ci, i64, i64, i64, ci, vp, vp, vp]),
         "mkq_checkpoint_restore": (ci, [vp, vp, ci, i64, i64, ci, vp, ci, i64, vp]),
         "mkq_checkpoint_gelu_gradient": (ci, [vp, vp, ci, i64, i64, vp, ci, i64, vp, ci, i64, vp]),
+        "mkq_low_rank_adapters_workspace_bytes": (sz, [i64, i64, i64, ci, i64]),
+        "mkq_low_rank_adapters": (ci, [vp, ci, i64, vp, i64, i64, i64, ci, i64, vp, vp, ci, vp, vp, i64, vp, ci, i64, vp, vp, sz, vp]),
+        "mkq_low_rank_adapters_gradient_workspace_bytes": (sz, [i64, i64, i64, ci, i64]),
+        "mkq_low_rank_adapters_gradient": (ci, [vp, ci, i64, vp, ci, i64, vp, ci, vp, vp, i64, i64, i64, ci, i64, vp, vp, ci, vp, vp, i64,
+                                                vp, ci, i64, vp, vp, ci, ci, vp, sz, vp]),
     })
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -1080,6 +1087,103 @@ def mkq_checkpoint_gelu_gradient(codes, steps, dy, group: int = 128, dx_dtype: i
     _check(load().mkq_checkpoint_gelu_gradient(_ptr(codes), _ptr(steps), group, M, K, _ptr(dy), dy_dtype, ld_dy, _ptr(dx), int(dx_dtype),
                                                ld_dx, _stream_on(dev, stream)), "mkq_checkpoint_gelu_gradient")
     return dx
+
+
+def mkq_low_rank_adapters_workspace_bytes(M: int, K: int, N: int, rank: int, R: int) -> int:
+    return int(load().mkq_low_rank_adapters_workspace_bytes(M, K, N, rank, R))
+
+
+def mkq_low_rank_adapters_gradient_workspace_bytes(M: int, K: int, N: int, rank: int, R: int) -> int:
+    return int(load().mkq_low_rank_adapters_gradient_workspace_bytes(M, K, N, rank, R))
+
+
+def _adapters(adapter, down, up, scales, M: int):
+    """R, rank, K, N and the type of the adapters' matrices."""
+    torch = _torch()
+    w_dtype = _float_code(down, "down")
+    _need(adapter.dtype == torch.int32 and adapter.is_contiguous() and adapter.numel() == M, "adapter: contiguous int32, one for every row")
+    _need(down.dim() == 3 and up.dim() == 3 and down.is_contiguous() and up.is_contiguous() and up.dtype == down.dtype
+          and down.shape[:2] == up.shape[:2], "down, up: contiguous [R, rank, K] and [R, rank, N] of one type")
+    R, rank, K = down.shape
+    if scales is not None:
+        _vector(scales, R, "scales")
+    return R, rank, K, up.size(2), w_dtype
+
+
+def mkq_low_rank_adapters(x, adapter, down, up, scales=None, out_dtype: int | None = None, *, base=None, out=None, hidden=None, workspace=None,
+                          stream=None):
+    """base + scales[a] * (x down_a^T) up_a for every row's adapter a (int32 [M]; outside: none) -> [M,N] of out_dtype (None: x's).  down [R,rank,K],
+    up [R,rank,N]; ``base`` [M,N] of out_dtype, ``out`` too if need be; ``hidden`` float32 [M,rank]: x down_a^T for the gradient."""
+    torch = _torch()
+    ldx, x_dtype = _rows(x, "x"), _float_code(x, "x")
+    M = x.size(0)
+    R, rank, K, N, w_dtype = _adapters(adapter, down, up, scales, M)
+    _need(x.size(1) == K, "x: [M, K]")
+    if out_dtype is None:
+        out_dtype = x_dtype
+    dtype = _float_dtype(out_dtype, "out_dtype")
+    _workspace(workspace)
+    dev = _same_device(x, adapter, down, up, scales, base, out, hidden, workspace)
+    ld_base = 0
+    if base is not None:
+        ld_base = _rows(base, "base")
+        _need(base.dtype == dtype and tuple(base.shape) == (M, N), "base: [M, N] of out_dtype")
+    if hidden is not None:
+        _vector(hidden, M * rank, "hidden")
+    out, ld_out = _out_rows(out, M, N, dtype, x.device, stream, "out")
+    if workspace is None:
+        workspace = _new(mkq_low_rank_adapters_workspace_bytes(M, K, N, rank, R), torch.uint8, x.device, stream)
+    _check(load().mkq_low_rank_adapters(_ptr(x), x_dtype, ldx, _ptr(adapter), M, K, N, rank, R, _ptr(down), _ptr(up), w_dtype, _ptr(scales),
+                                        _ptr(base), ld_base, _ptr(out), int(out_dtype), ld_out, _ptr(hidden), _ptr(workspace),
+                                        workspace.nbytes, _stream_on(dev, stream)), "mkq_low_rank_adapters")
+    return out
+
+
+def mkq_low_rank_adapters_gradient(dy, x, adapter, hidden, down, up, scales=None, dx_dtype: int | None = None, grad_dtype: int = MKQ_F32, *,
+                                   steps=None, group: int = 0, base=None, dx=None, d_down=None, d_up=None, accumulate: bool = False,
+                                   want_dx: bool = True, workspace=None, stream=None):
+    """Gradients (dx [M,K] of dx_dtype (None: dy's), d_down [R,rank,K], d_up [R,rank,N] of grad_dtype) of mkq_low_rank_adapters from dy [M,N], its x and
+    the ``hidden`` that it gave.  ``steps``, ``group``: x is the codes of mkq_checkpoint_int8.  ``base`` is added to dx; ``accumulate``: added to the
+    ``d_down`` and ``d_up`` that are passed in; ``want_dx`` False: none."""
+    torch = _torch()
+    ld_dy, dy_dtype = _rows(dy, "dy"), _float_code(dy, "dy")
+    M = dy.size(0)
+    R, rank, K, N, w_dtype = _adapters(adapter, down, up, scales, M)
+    _need(dy.size(1) == N, "dy: [M, N]")
+    _vector(hidden, M * rank, "hidden")
+    if steps is not None:
+        _need(_checkpoint(x, steps, K, group, "x") == M, "x: a row for every row of dy")
+        x_dtype, ldx = MKQ_I8, x.size(1)
+    else:
+        x_dtype, ldx = _float_code(x, "x"), _rows(x, "x")
+        _need(tuple(x.shape) == (M, K), "x: [M, K]")
+    if dx_dtype is None:
+        dx_dtype = dy_dtype
+    dtype, grad = _float_dtype(dx_dtype, "dx_dtype"), _float_dtype(grad_dtype, "grad_dtype")
+    _workspace(workspace)
+    dev = _same_device(dy, x, adapter, hidden, down, up, scales, steps, base, dx, d_down, d_up, workspace)
+    ld_base = ld_dx = 0
+    _need(want_dx or (dx is None and base is None), "dx: wanted")
+    if want_dx:
+        if base is not None:
+            ld_base = _rows(base, "base")
+            _need(base.dtype == dtype and tuple(base.shape) == (M, K), "base: [M, K] of dx_dtype")
+        dx, ld_dx = _out_rows(dx, M, K, dtype, dy.device, stream, "dx")
+    _need(not accumulate or (d_down is not None and d_up is not None), "accumulate: needs the gradients to add to")
+    if d_down is None:
+        d_down = _new((R, rank, K), grad, dy.device, stream)
+    if d_up is None:
+        d_up = _new((R, rank, N), grad, dy.device, stream)
+    _need(d_down.dtype == d_up.dtype == grad and d_down.is_contiguous() and d_up.is_contiguous() and d_down.shape == down.shape
+          and d_up.shape == up.shape, "d_down, d_up: contiguous, of the adapters' sizes and grad_dtype")
+    if workspace is None:
+        workspace = _new(mkq_low_rank_adapters_gradient_workspace_bytes(M, K, N, rank, R), torch.uint8, dy.device, stream)
+    _check(load().mkq_low_rank_adapters_gradient(_ptr(dy), dy_dtype, ld_dy, _ptr(x), x_dtype, ldx, _ptr(steps), int(group), _ptr(adapter),
+                                                 _ptr(hidden), M, K, N, rank, R, _ptr(down), _ptr(up), w_dtype, _ptr(scales), _ptr(base), ld_base,
+                                                 _ptr(dx), int(dx_dtype), ld_dx, _ptr(d_down), _ptr(d_up), int(grad_dtype), int(accumulate),
+                                                 _ptr(workspace), workspace.nbytes, _stream_on(dev, stream)),
+           "mkq_low_rank_adapters_gradient")
+    return dx, d_down, d_up
 
 
 class BertLayerInt4:

@@ -104,13 +104,20 @@ inline bool rows_aligned16(const void *p, int64_t ld, int dtype) { return aligne
 
 inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
+// Whether two matrices of M rows do not touch (a dtype that is none of floats: bytes)
+inline bool apart(const void *a, int a_dtype, int64_t ld_a, int64_t cols_a, const void *b, int b_dtype, int64_t ld_b, int64_t cols_b, int64_t M)
+{
+    auto extent = [&](int64_t ld, int64_t cols, int dtype) {
+        return (uintptr_t)(((unsigned __int128)(M - 1) * (uint64_t)ld + (uint64_t)cols) * (uint64_t)(is_float_dtype(dtype) ? dtype_bytes(dtype) : 1));
+    };
+    const uintptr_t i = reinterpret_cast<uintptr_t>(a), o = reinterpret_cast<uintptr_t>(b);
+    return i + extent(ld_a, cols_a, a_dtype) <= o || o + extent(ld_b, cols_b, b_dtype) <= i;
+}
 // Whether results [M, K] lie apart from what they are computed from, value by value, or exactly over it
 inline bool in_place_or_apart(const void *in, int in_dtype, int64_t ld_in, const void *out, int out_dtype, int64_t ld_out, int64_t M, int64_t K)
 {
     if (in == out && in_dtype == out_dtype && (ld_in == ld_out || M <= 1)) return true;
-    auto extent = [&](int64_t ld, int dtype) { return (uintptr_t)(((unsigned __int128)(M - 1) * (uint64_t)ld + (uint64_t)K) * (uint64_t)dtype_bytes(dtype)); };
-    const uintptr_t i = reinterpret_cast<uintptr_t>(in), o = reinterpret_cast<uintptr_t>(out);
-    return i + extent(ld_in, in_dtype) <= o || o + extent(ld_out, out_dtype) <= i;
+    return apart(in, in_dtype, ld_in, K, out, out_dtype, ld_out, K, M);
 }
 
 // Workgroups of a launch: the grid's work items are counted in 32 bits

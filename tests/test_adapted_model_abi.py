@@ -74,12 +74,51 @@ def test_checkpoint_refusals(lib):
         assert f(M=0) == mkq.MKQ_OK
         assert f(c=None) == f(s=None) == mkq.MKQ_ERR_NULL
         assert f(c=ODD) == f(s=VERY_ODD) == mkq.MKQ_ERR_ALIGN
-        assert f(M=2 ** 31) == f(K=2 ** 31, ld=2 ** 31) == mkq.MKQ_ERR_UNSUPPORTED
+        assert f(M=2 ** 31) == f(K=2 ** 31, ld=2 ** 31, **({"ldo": 2 ** 31} if f is slope else {})) == mkq.MKQ_ERR_UNSUPPORTED
     assert slope(ldo=99) == mkq.MKQ_ERR_SHAPE
     assert keep(x=None) == back(o=None) == slope(dy=None) == slope(dx=None) == mkq.MKQ_ERR_NULL
     assert keep(x=ODD) == back(o=ODD) == slope(dy=ODD) == slope(dx=ODD) == mkq.MKQ_ERR_ALIGN
     assert slope(dx=P, odt=F32) == slope(dx=P, ldo=104) == slope(dx=C.c_void_p(0x1010)) == mkq.MKQ_ERR_UNSUPPORTED
     assert lib.mkq_checkpoint_bytes(3, 33) == 3 * 64 and lib.mkq_checkpoint_bytes(-1, 3) == lib.mkq_checkpoint_bytes(1, 0) == 0
+
+
+def test_adapter_refusals(lib):
+    def fwd(x=P, dt=F16, ldx=64, a=P, M=4, K=64, N=32, rank=8, R=2, down=P, up=P, w=F16, scales=None, base=None, ldb=32, out=Q, odt=F16, ldo=32,
+            hidden=None, ws=P, n=1 << 20):
+        return lib.mkq_low_rank_adapters(x, dt, ldx, a, M, K, N, rank, R, down, up, w, scales, base, ldb, out, odt, ldo, hidden, ws, n, None)
+    assert fwd(dt=mkq.MKQ_I8) == fwd(w=mkq.MKQ_I4) == fwd(odt=-1) == mkq.MKQ_ERR_DTYPE
+    for bad in (dict(M=-1), dict(K=0), dict(N=0), dict(rank=0), dict(R=0), dict(ldx=63), dict(ldo=31), dict(base=P, ldb=31)):
+        assert fwd(**bad) == mkq.MKQ_ERR_SHAPE, bad
+    assert fwd(rank=257) == fwd(R=2 ** 23) == fwd(M=2 ** 31) == fwd(K=2 ** 31, ldx=2 ** 31) == fwd(N=2 ** 31, ldo=2 ** 31) == mkq.MKQ_ERR_UNSUPPORTED
+    assert fwd(x=None) == fwd(a=None) == fwd(down=None) == fwd(up=None) == fwd(out=None) == mkq.MKQ_ERR_NULL
+    for bad in (dict(x=ODD), dict(a=VERY_ODD), dict(down=ODD), dict(up=ODD), dict(scales=VERY_ODD), dict(base=ODD), dict(out=ODD), dict(hidden=VERY_ODD), dict(ws=ODD)):
+        assert fwd(**bad) == mkq.MKQ_ERR_ALIGN, bad
+    assert fwd(base=Q, ldb=40) == fwd(base=C.c_void_p(0x10000010)) == mkq.MKQ_ERR_UNSUPPORTED
+    need = lib.mkq_low_rank_adapters_workspace_bytes(4, 64, 32, 8, 2)
+    assert need >= 4 * 8 * 4 and fwd(ws=None) == fwd(n=need - 1) == mkq.MKQ_ERR_WORKSPACE
+    assert fwd(M=0, x=None, ws=None) == mkq.MKQ_OK
+    assert lib.mkq_low_rank_adapters_workspace_bytes(4, 64, 32, 300, 2) == lib.mkq_low_rank_adapters_workspace_bytes(-4, 64, 32, 3, 2) == 0
+
+    X, DX = C.c_void_p(0x20000000), C.c_void_p(0x30000000)
+
+    def bwd(dy=Q, dt=F16, ldy=32, x=X, xt=F16, ldx=64, steps=None, group=0, a=P, hidden=P, M=4, K=64, N=32, rank=8, R=2, down=P, up=P, w=F16, scales=None,
+            base=None, ldb=64, dx=DX, dxt=F16, ldd=64, dd=P, du=P, g=F32, acc=0, ws=P, n=1 << 20):
+        return lib.mkq_low_rank_adapters_gradient(dy, dt, ldy, x, xt, ldx, steps, group, a, hidden, M, K, N, rank, R, down, up, w, scales, base, ldb, dx, dxt,
+                                                  ldd, dd, du, g, acc, ws, n, None)
+    assert bwd(dt=mkq.MKQ_I8) == bwd(xt=mkq.MKQ_I4) == bwd(w=9) == bwd(dxt=mkq.MKQ_I8) == bwd(g=mkq.MKQ_I8) == mkq.MKQ_ERR_DTYPE
+    for bad in (dict(M=-1), dict(rank=0), dict(R=0), dict(ldy=31), dict(ldx=63), dict(ldd=63), dict(base=P, ldb=63), dict(xt=mkq.MKQ_I8, steps=P, group=16)):
+        assert bwd(**bad) == mkq.MKQ_ERR_SHAPE, bad
+    for bad in (dict(dy=None), dict(x=None), dict(a=None), dict(hidden=None), dict(down=None), dict(up=None), dict(xt=mkq.MKQ_I8, group=32),
+                dict(dx=None, dd=None, du=None)):
+        assert bwd(**bad) == mkq.MKQ_ERR_NULL, bad
+    for bad in (dict(dy=ODD), dict(x=ODD), dict(a=VERY_ODD), dict(hidden=VERY_ODD), dict(dx=ODD), dict(dd=ODD), dict(du=ODD), dict(base=ODD), dict(ws=ODD),
+                dict(steps=VERY_ODD, xt=mkq.MKQ_I8, group=32)):
+        assert bwd(**bad) == mkq.MKQ_ERR_ALIGN, bad
+    # dx over what is read behind it
+    assert bwd(dx=Q) == bwd(dx=X) == bwd(base=DX, ldb=72) == bwd(rank=257) == mkq.MKQ_ERR_UNSUPPORTED
+    need = lib.mkq_low_rank_adapters_gradient_workspace_bytes(4, 64, 32, 8, 2)
+    assert lib.mkq_low_rank_adapters_gradient_workspace_bytes(0, 64, 32, 8, 2) > 0 and bwd(M=0, ws=None) == mkq.MKQ_ERR_WORKSPACE
+    assert need > 0 and bwd(ws=None) == bwd(n=need - 1) == mkq.MKQ_ERR_WORKSPACE
 
 
 def test_binding_refuses_what_it_would_read_wrongly():
@@ -99,3 +138,17 @@ def test_binding_refuses_what_it_would_read_wrongly():
                dict(d=torch.zeros(4), d_entropies=torch.zeros(5)), dict(d=torch.zeros(4))):
         with pytest.raises(ValueError):
             mkq.mkq_token_log_probs_gradient(x, t, r, kw.pop("d"), **kw)
+    ids, down, up = torch.zeros(4, dtype=torch.int32), torch.zeros(2, 3, 10), torch.zeros(2, 3, 12)
+    dy, hidden = torch.zeros(4, 12), torch.zeros(4, 3)
+    for call in (lambda: mkq.mkq_low_rank_adapters(x, ids.long(), down, up), lambda: mkq.mkq_low_rank_adapters(x, ids[:3], down, up),
+                 lambda: mkq.mkq_low_rank_adapters(x, ids, down, up.half()), lambda: mkq.mkq_low_rank_adapters(x, ids, down, up[:1]),
+                 lambda: mkq.mkq_low_rank_adapters(x, ids, down[:, :, :9], up), lambda: mkq.mkq_low_rank_adapters(x, ids, down, up, torch.ones(3)),
+                 lambda: mkq.mkq_low_rank_adapters(x, ids, down, up),
+                 lambda: mkq.mkq_low_rank_adapters_gradient(dy, x, ids, hidden[:3], down, up),
+                 lambda: mkq.mkq_low_rank_adapters_gradient(dy, x[:3], ids, hidden, down, up),
+                 lambda: mkq.mkq_low_rank_adapters_gradient(dy, x, ids, hidden, down, up, accumulate=True),
+                 lambda: mkq.mkq_low_rank_adapters_gradient(dy, x, ids, hidden, down, up, want_dx=False, dx=x),
+                 lambda: mkq.mkq_low_rank_adapters_gradient(dy, x, ids, hidden, down, up, steps=torch.ones(4, 1), group=32),
+                 lambda: mkq.mkq_low_rank_adapters_gradient(dy, x, ids, hidden, down, up)):
+        with pytest.raises(ValueError):
+            call()
