@@ -34,7 +34,7 @@ struct AdapterParams {
     const int32_t *adapter;
     const float *scales;  // [R], or NULL: 1
     int64_t M;
-    int R, rank, splits;
+    int R, rank, pitch, splits;  // pitch: rank rounded up to eight
 };
 __device__ __forceinline__ float scale_of(const AdapterParams &p, int a) { return p.scales ? p.scales[a] : 1.0f; }
 // The adapter of a row, -1 for none
@@ -111,45 +111,67 @@ __device__ __forceinline__ v4f multiply(const uint4 (&a)[PA], const uint4 (&b)[P
     return c;
 }
 
-// Eight neighbours of a row from place k on, as fetched; zeros from place `end` on
+// Eight neighbours of a row from place k on, as fetched.  Whole vectors only, and no branch that lanes of a wave take apart: where the row
+// ends among a wave's places (`edge`), its last eight elements are fetched instead and moved down, zeros behind them.  A row of fewer than
+// eight is fetched one by one.  (Rows kept in 8 bits have zeros behind them.)
 template <class E>
 struct Neighbours {
     u32x4 w[E::BYTES == 4 ? 2 : 1];
-    __device__ __forceinline__ void clear()
+    __device__ __forceinline__ void without_first(int n)
     {
-#pragma unroll
-        for (auto &v : w) v = u32x4{0, 0, 0, 0};
-    }
-    __device__ __forceinline__ void fetch(const typename E::raw *row, int64_t k, int64_t end)
-    {
-        const typename E::raw *at = row + k;
-        if (k + 8 <= end) {
-            if constexpr (E::BYTES == 1) {
-                const uint2 v = *reinterpret_cast<const uint2 *>(at);
-                w[0] = u32x4{v.x, v.y, 0, 0};
-            } else {
-                w[0] = reinterpret_cast<const Loose<E::BYTES> *>(at)->v;
-                if constexpr (E::BYTES == 4) w[1] = reinterpret_cast<const Loose<4> *>(at + 4)->v;
-            }
+        if constexpr (E::BYTES == 2) {
+            u32x4 &v = w[0];
+            if (n & 1)
+                v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16), v[3] >> 16};
+            if (n & 2) v = u32x4{v[1], v[2], v[3], 0};
+            if (n & 4) v = u32x4{v[2], v[3], 0, 0};
+            if (n >= 8) v = u32x4{0, 0, 0, 0};
         } else {
-            typename E::raw v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k + i < end ? at[i] : typename E::raw(0);
-            if constexpr (E::BYTES == 4) {
-                w[0] = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-                w[1] = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-            } else if constexpr (E::BYTES == 2) {
-                w[0] = u32x4{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16};
-            } else {
-                uint32_t lo = 0, hi = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    lo |= (uint32_t)(uint8_t)v[i] << (8 * i);
-                    hi |= (uint32_t)(uint8_t)v[4 + i] << (8 * i);
-                }
-                w[0] = u32x4{lo, hi, 0, 0};
+            u32x4 &v = w[0], &x = w[E::BYTES / 4];
+            if (n & 1) {
+                v = u32x4{v[1], v[2], v[3], x[0]};
+                x = u32x4{x[1], x[2], x[3], 0};
+            }
+            if (n & 2) {
+                v = u32x4{v[2], v[3], x[0], x[1]};
+                x = u32x4{x[2], x[3], 0, 0};
+            }
+            if (n >= 4) {
+                v = n >= 8 ? u32x4{0, 0, 0, 0} : x;
+                x = u32x4{0, 0, 0, 0};
             }
         }
+    }
+    // `row`: the bytes of a row, or a place that all lanes share with `off` bytes to a lane's row
+    __device__ __forceinline__ void fetch(const void *row, int k, int end, bool edge) { fetch(row, 0u, k, end, edge); }
+    __device__ __forceinline__ void fetch(const void *place, uint32_t off, int k, int end, bool edge)
+    {
+        const uint8_t *row = static_cast<const uint8_t *>(place);
+        if constexpr (E::BYTES == 1) {
+            if (edge) k = k < end ? k : (end - 1) & ~7;
+            const uint2 v = *reinterpret_cast<const uint2 *>(row + (off + (uint32_t)k));
+            w[0] = u32x4{v.x, v.y, 0, 0};
+        } else {
+            if (end < 8) return fetch_short(row, off, k, end);
+            const int from = edge && k + 8 > end ? end - 8 : k;
+            const uint8_t *at = row + (off + (uint32_t)from * E::BYTES);
+            w[0] = reinterpret_cast<const Loose<E::BYTES> *>(at)->v;
+            if constexpr (E::BYTES == 4) w[1] = reinterpret_cast<const Loose<4> *>(at + 16)->v;
+            if (edge) without_first(k - from < 8 ? k - from : 8);
+        }
+    }
+    __device__ __forceinline__ void fetch_short(const uint8_t *row, uint32_t off, int k, int end)
+    {
+        w[0] = u32x4{0, 0, 0, 0};
+        if constexpr (E::BYTES == 4) w[1] = u32x4{0, 0, 0, 0};
+        if (k != 0) return;
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < end) {
+                const typename E::raw v = *reinterpret_cast<const typename E::raw *>(row + (off + i * E::BYTES));
+                if constexpr (E::BYTES == 4) w[i / 4][i % 4] = __float_as_uint(v);
+                else w[0][i / 2] |= (uint32_t)v << (16 * (i % 2));
+            }
     }
     __device__ __forceinline__ float get(int i) const
     {
@@ -159,25 +181,107 @@ struct Neighbours {
     }
 };
 
-// Eight neighbours of a row from place k on, those before `end`
+// Eight neighbours of a row from place k on, those before `end`; place and off as above
 template <class O>
-__device__ __forceinline__ void put_neighbours(typename O::raw *row, int64_t k, int64_t end, const float (&y)[8])
+__device__ __forceinline__ void put_neighbours(void *place, uint32_t off, int k, int end, bool edge, const float (&y)[8])
 {
-    typename O::raw *to = row + k;
-    if (k + 8 > end) {
+    uint8_t *to = static_cast<uint8_t *>(place) + (off + (uint32_t)k * O::BYTES);
+    uint32_t w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (k + e < end) to[e] = O::put(in_binary32(y[e]));
-    } else if constexpr (O::BYTES == 4) {
-#pragma unroll
-        for (int e = 0; e < 8; e += 4)
-            reinterpret_cast<Loose<4> *>(to + e)->v = u32x4{__float_as_uint(y[e]), __float_as_uint(y[e + 1]), __float_as_uint(y[e + 2]), __float_as_uint(y[e + 3])};
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (O::BYTES == 4) {
+            w[e] = __float_as_uint(y[e]);
+            w[4 + e] = __float_as_uint(y[4 + e]);
+        } else {
             w[e] = std::is_same<O, ElemF16>::value ? pack2_f16(in_binary32(y[2 * e]), in_binary32(y[2 * e + 1])) : pack2_bf16(y[2 * e], y[2 * e + 1]);
-        reinterpret_cast<Loose<2> *>(to)->v = u32x4{w[0], w[1], w[2], w[3]};
+        }
+    }
+    if (edge && k + 8 > end) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (k + e < end) {
+                if constexpr (O::BYTES == 4) reinterpret_cast<uint32_t *>(to)[e] = w[e];
+                else reinterpret_cast<uint16_t *>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
+            }
+    } else {
+        reinterpret_cast<Loose<O::BYTES> *>(to)->v = u32x4{w[0], w[1], w[2], w[3]};
+        if constexpr (O::BYTES == 4) reinterpret_cast<Loose<4> *>(to + 16)->v = u32x4{w[4], w[5], w[6], w[7]};
+    }
+}
+// A number that the compiler takes for new where it stands: what follows from it is computed there again, not kept in registers around a loop
+__device__ __forceinline__ int fresh(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// ---- the batch's rows by adapter -------------------------------------------------------------------------------------------
+// order: rows with an adapter, sorted by it, in the batch's order; starts [R + 1].  An adapter's rows are summed in pieces of
+// `piece` rows: task starts[a] / piece + a + j has the j-th (no two adapters' tasks meet, as starts grow by an adapter's rows).
+struct PlanParams {
+    int piece, tasks_most;
+    int32_t *order, *starts;
+    int4 *tasks;  // [tasks_most] adapter (-1: nothing to do), first and last place in order, pieces of the adapter
+};
+__device__ __forceinline__ int task_of(int start, int a, int piece) { return start / piece + a; }
+
+// A workgroup of 256 has an adapter: each thread looks through neighbouring rows for those of the adapter and those of smaller ones
+__device__ void plan(const AdapterParams &p, const PlanParams &plan, int a)
+{
+    __shared__ int equal_before[4], less_before[4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t each = (p.M + 1023) / 1024 * 4;
+    const int64_t from = threadIdx.x * each < p.M ? threadIdx.x * each : p.M, to = from + each < p.M ? from + each : p.M;
+    auto rows = [&](auto &&f) {
+        int64_t m = from;
+        for (; m + 16 <= to; m += 16) {
+            u32x4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = reinterpret_cast<const Loose<4> *>(p.adapter + m + 4 * i)->v;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f(m + i, (int)v[i / 4][i % 4]);
+        }
+        for (; m < to; ++m) f(m, p.adapter[m]);
+    };
+    int equal = 0, less = 0;
+    rows([&](int64_t, int b) {
+        equal += b == a;
+        less += b >= 0 && b < a;
+    });
+    int before = equal, all_less = less;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int v = __shfl_up(before, off, 64);
+        if (lane >= off) before += v;
+        all_less += __shfl_xor(all_less, off, 64);
+    }
+    if (lane == 63) {
+        equal_before[wave] = before;
+        less_before[wave] = all_less;
+    }
+    __syncthreads();
+    int start = 0, waves_before = 0, count = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        start += less_before[w];
+        if (w < wave) waves_before += equal_before[w];
+        count += equal_before[w];
+    }
+    int at = start + waves_before + before - equal;
+    if (equal)
+        rows([&](int64_t m, int b) {
+            if (b == a) plan.order[at++] = (int32_t)m;
+        });
+    if (threadIdx.x == 0) {
+        plan.starts[a] = start;
+        if (a == p.R - 1) plan.starts[p.R] = start + count;
+    }
+    // (behind the last adapter's: fewer rows than the batch's may have an adapter)
+    const int first = task_of(start, a, plan.piece), next = a + 1 < p.R ? task_of(start + count, a + 1, plan.piece) : plan.tasks_most;
+    const int pieces = count ? (count + plan.piece - 1) / plan.piece : 1;
+    for (int i = first + (int)threadIdx.x; i < next; i += 256) {
+        const int j = i - first, last = (j + 1) * plan.piece < count ? (j + 1) * plan.piece : count;
+        plan.tasks[i] = j < pieces ? make_int4(a, start + j * plan.piece, start + last, pieces) : make_int4(-1, 0, 0, 0);
     }
 }
 
@@ -190,7 +294,10 @@ struct ShrinkParams {
     int slots;          // workgroups that share a tile's adapters
     int rank_chunks, per_split;  // steps of 64 places of a split
     bool scaled;        // times the adapter's scale
-    float *t;           // [splits, M, rank]
+    float *t;           // [splits, M, pitch], zeros behind the rank
+    float *hidden;      // [M, rank], or NULL: the same
+    int plans;          // workgroups in front that put the rows in order
+    PlanParams plan;
 };
 constexpr int SHRINK_STEP = 64;
 
@@ -207,13 +314,15 @@ __device__ __forceinline__ void operand(const Neighbours<E> &n, uint4 (&out)[Par
     }
 }
 
-// Tiles of 16 rows and RT * 16 of the rank; the four waves of a workgroup take steps in turn and add up through LDS
+// Tiles of 16 rows and RT * 16 of the rank; the four waves of a workgroup take steps in turn, and UNROLL at a time, and add up through LDS
 template <class X, class W, int RT>
 __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
 {
+    constexpr int UNROLL = RT * (X::BYTES + W::BYTES) <= 4 ? 4 : RT * (X::BYTES + W::BYTES) <= 8 ? 2 : 1;
     __shared__ v4f sums[4][RT][64];
+    if (blockIdx.x < (unsigned)p.plans) return plan(p.a, p.plan, blockIdx.x);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
-    unsigned b = blockIdx.x;
+    unsigned b = blockIdx.x - p.plans;
     const int chunk = b % p.rank_chunks;
     b /= p.rank_chunks;
     const int split = b % p.a.splits;
@@ -225,7 +334,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
     const typename X::raw *x = static_cast<const typename X::raw *>(p.x) + row * p.ldx;
     const int steps = (p.K + SHRINK_STEP - 1) / SHRINK_STEP;
     const int from = split * p.per_split, to = from + p.per_split < steps ? from + p.per_split : steps;
-    float *t = p.t + (int64_t)split * p.a.M * p.a.rank;
+    float *t = p.t + (int64_t)split * p.a.M * p.a.pitch;
     Adapters adapters(mine, slot, p.slots, lane < 16 && m0 + lane < p.a.M && mine < 0);
     int a;
     uint64_t same;
@@ -233,50 +342,57 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
         if (a < 0) {  // rows without an adapter
             for (int i = 0; i < 16; ++i)
                 if (same >> i & 1)
-                    for (int r = chunk * RT * 16 + (int)threadIdx.x; r < p.a.rank && r < (chunk + 1) * RT * 16; r += 256) t[(m0 + i) * p.a.rank + r] = 0.0f;
+                    for (int r = chunk * RT * 16 + (int)threadIdx.x; r < p.a.pitch && r < (chunk + 1) * RT * 16; r += 256) {
+                        t[(m0 + i) * p.a.pitch + r] = 0.0f;
+                        if (p.hidden && r < p.a.rank) p.hidden[(m0 + i) * p.a.rank + r] = 0.0f;
+                    }
             continue;
         }
         v4f acc[RT];
         const typename W::raw *w[RT];
-        bool real[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const int at = (chunk * RT + r) * 16 + c;
             acc[r] = v4f{0, 0, 0, 0};
-            real[r] = at < p.a.rank;
-            w[r] = static_cast<const typename W::raw *>(p.w) + ((int64_t)a * p.a.rank + (real[r] ? at : 0)) * p.K;
+            w[r] = static_cast<const typename W::raw *>(p.w) + ((int64_t)a * p.a.rank + (at < p.a.rank ? at : p.a.rank - 1)) * p.K;
         }
-        for (int s = from + wave; s < to; s += 4) {
-            Neighbours<X> xs[2];
-            Neighbours<W> ws[2][RT];
+        auto take = [&](auto n, int s) {
+            constexpr int N = decltype(n)::value;
+            Neighbours<X> xs[N][2];
+            Neighbours<W> ws[N][2][RT];
+            const bool edge = (s + 4 * (N - 1) + 1) * SHRINK_STEP > p.K;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = s * SHRINK_STEP + h * 32 + q * 8;
-                xs[h].clear();
-                if (k < p.K) xs[h].fetch(x, k, p.K);
+            for (int u = 0; u < N; ++u)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    ws[h][r].clear();
-                    if (k < p.K && real[r]) ws[h][r].fetch(w[r], k, p.K);
+                for (int h = 0; h < 2; ++h) {
+                    const int k = (s + 4 * u) * SHRINK_STEP + h * 32 + q * 8;
+                    xs[u][h].fetch(x, k, p.K, edge);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) ws[u][h][r].fetch(w[r], k, p.K, edge);
                 }
-            }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if constexpr (std::is_same<X, ElemF16>::value && std::is_same<W, ElemF16>::value) {
+            for (int u = 0; u < N; ++u)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, xs[h].w[0]), __builtin_bit_cast(v8h, ws[h][r].w[0]), acc[r], 0, 0, 0);
-                } else {
-                    uint4 xp[Parts<X>::N], wp[Parts<W>::N];
-                    operand(xs[h], xp);
+                for (int h = 0; h < 2; ++h) {
+                    if constexpr (std::is_same<X, ElemF16>::value && std::is_same<W, ElemF16>::value) {
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        operand(ws[h][r], wp);
-                        acc[r] = multiply<3>(xp, wp, acc[r]);
+                        for (int r = 0; r < RT; ++r)
+                            acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, xs[u][h].w[0]), __builtin_bit_cast(v8h, ws[u][h][r].w[0]), acc[r], 0, 0, 0);
+                    } else {
+                        uint4 xp[Parts<X>::N], wp[Parts<W>::N];
+                        operand(xs[u][h], xp);
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) {
+                            operand(ws[u][h][r], wp);
+                            acc[r] = multiply<3>(xp, wp, acc[r]);
+                        }
                     }
                 }
-            }
-        }
+        };
+        int s = from + wave;
+        if constexpr (UNROLL > 1)
+            for (; s + 4 * (UNROLL - 1) < to; s += 4 * UNROLL) take(IntC<UNROLL>(), s);
+        for (; s < to; s += 4) take(IntC<1>(), s);
 #pragma unroll
         for (int r = 0; r < RT; ++r) sums[wave][r][lane] = acc[r];
         __syncthreads();
@@ -286,7 +402,11 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
             const int at = (chunk * RT + r) * 16 + c;
 #pragma unroll
             for (int v = 0; v < 4; ++v)
-                if (at < p.a.rank && (same >> (4 * q + v) & 1)) t[(m0 + 4 * q + v) * p.a.rank + at] = sum[v] * scale;
+                if (at < p.a.pitch && (same >> (4 * q + v) & 1)) {
+                    const float value = at < p.a.rank ? sum[v] * scale : 0.0f;
+                    t[(m0 + 4 * q + v) * p.a.pitch + at] = value;
+                    if (p.hidden && at < p.a.rank) p.hidden[(m0 + 4 * q + v) * p.a.rank + at] = value;
+                }
         }
         __syncthreads();
     }
@@ -300,10 +420,11 @@ struct ExpandParams {
     const void *base; // [M, N], or NULL
     void *out;
     int64_t ld_base, ld_out;
-    int N, column_blocks, slots, row_groups;
+    int N, column_blocks, slots, row_groups, tiles;
     bool scaled;      // t is still to be multiplied by the adapter's scale
     bool keep_scaled; // ... as it is kept
-    float *keep;      // [M, rank], or NULL: what the splits add up to
+    float *keep;      // [M, keep_pitch], or NULL: what the splits add up to
+    int keep_pitch;
 };
 
 // Columns of eight rows as the matrix unit takes them: of eight rows' neighbours in lanes (c, q), tile i has the columns 8 c + i
@@ -329,238 +450,174 @@ struct Block {
     }
 };
 
-// t of a row from place r on, eight values, added up over the splits
-__device__ __forceinline__ void hidden_values(const ExpandParams &p, int64_t row, int r, float (&v)[8])
+// t of row c from place r on, eight values, added up over the splits; t: that of the first row
+__device__ __forceinline__ void hidden_values(const ExpandParams &p, const float *t, int c, int r, float (&v)[8])
 {
+    const uint32_t off = (uint32_t)(c * p.a.pitch + (r < p.a.pitch ? r : 0)) * 4;
+    const int64_t split = p.a.M * p.a.pitch;
+    auto load = [&](int s, float (&to)[8]) { load8(reinterpret_cast<const float *>(reinterpret_cast<const uint8_t *>(t + s * split) + off), to); };
+    load(0, v);
+    for (int s = 1; s < p.a.splits; s += 3) {
+        float more[3][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-    if (r >= p.a.rank) return;
-    for (int s = 0; s < p.a.splits; ++s) {
-        Neighbours<ElemF32> n;
-        n.fetch(p.t + ((int64_t)s * p.a.M + row) * p.a.rank, r, p.a.rank);
+        for (int i = 0; i < 3; ++i) load(s + i < p.a.splits ? s + i : s, more[i]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += n.get(e);
+        for (int i = 0; i < 3; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += s + i < p.a.splits ? more[i][e] : 0.0f;
     }
+    if (r >= p.a.pitch)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
 }
 
-// A wave has 16 RB rows and 128 columns; lane (c, q) ends with columns 8 c .. 8 c + 7 of rows 4 q .. 4 q + 3 of every 16
-template <class W, class O, int RB>
-__global__ __launch_bounds__(256) void expand_kernel(const ExpandParams p)
+// A wave has 128 columns of `tiles` tiles of 16 rows; lane (c, q) has columns 8 c .. 8 c + 7 of rows 4 q .. 4 q + 3.  The adapter's rows are fetched
+// again for every tile (from the caches), 32 at a time.
+template <class W, class O>
+__global__ __launch_bounds__(256, W::BYTES == 4 || O::BYTES == 4 ? 2 : 3) void expand_kernel(const ExpandParams p)
 {
     constexpr int PT = O::BYTES == 4 ? 3 : 2;  // (2^-16 of a product is left out under results of 16 bits, which end at 2^-9 or 2^-12)
-    const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
-    int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = (int)(task % p.column_blocks);
-    task /= p.column_blocks;
-    const int slot = (int)(task / p.row_groups);
+    const int64_t rest = task / p.column_blocks;
+    const int slot = (int)(rest / p.row_groups), group = (int)(rest - (int64_t)slot * p.row_groups);
     if (slot >= p.slots) return;
-    const int64_t m0 = (task - (int64_t)slot * p.row_groups) * (16 * RB);
-    const int mine = adapter_of(p.a, lane < 16 * RB ? m0 + lane : p.a.M);
-    const int64_t n0 = (int64_t)block * 128 + 8 * c;
-    Adapters adapters(mine, slot, p.slots, lane < 16 * RB && m0 + lane < p.a.M && mine < 0);
-    int a;
-    uint64_t same;
-    while (adapters.next(a, same)) {
-        v4f acc[RB][8];
+    const bool edge = block * 128 + 128 > p.N;
+    for (int tile = 0; tile < p.tiles; ++tile) {
+        const int64_t m0 = ((int64_t)group * p.tiles + tile) * 16;
+        if (m0 >= p.a.M) break;
+        const int lane = fresh(threadIdx.x & 63), c = lane & 15, q = lane >> 4, n0 = block * 128 + 8 * c;
+        const int last_row = p.a.M - m0 < 16 ? (int)(p.a.M - m0) - 1 : 15;
+        const int mine = adapter_of(p.a, lane < 16 ? m0 + lane : p.a.M);
+        Neighbours<O> base[4];
+        if (p.base) {
+            const void *at = static_cast<const typename O::raw *>(p.base) + m0 * p.ld_base;
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[b][i] = v4f{0, 0, 0, 0};
-        const float scale = a < 0 ? 0.0f : scale_of(p.a, a), factor = p.scaled ? scale : 1.0f;
-        const typename W::raw *w = static_cast<const typename W::raw *>(p.w) + (int64_t)(a < 0 ? 0 : a) * p.a.rank * p.N;
-        if (a < 0) {  // rows without an adapter
-            if (p.keep && block == 0)
-                for (int i = 0; i < 16 * RB; ++i)
-                    if (same >> i & 1)
-                        for (int r = lane; r < p.a.rank; r += 64) p.keep[(m0 + i) * p.a.rank + r] = 0.0f;
-            if (p.base == p.out) continue;
+            for (int v = 0; v < 4; ++v)
+                base[v].fetch(at, (uint32_t)(4 * q + v < last_row ? 4 * q + v : last_row) * ((uint32_t)p.ld_base * O::BYTES), n0, p.N, edge);
         }
-        for (int r0 = 0; a >= 0 && r0 < p.a.rank; r0 += 32) {
-            const int r = r0 + 8 * q;
-            Block<W> block_w;
+        typename O::raw *out = static_cast<typename O::raw *>(p.out) + m0 * p.ld_out;
+        const float *t = p.t + m0 * p.a.pitch;
+        Adapters adapters(mine, slot, p.slots, lane < 16 && m0 + lane < p.a.M && mine < 0);
+        int a;
+        uint64_t same;
+        while (adapters.next(a, same)) {
+            v4f acc[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                block_w.rows[e].clear();
-                if (r + e < p.a.rank && n0 < p.N) block_w.rows[e].fetch(w + (int64_t)(r + e) * p.N, n0, p.N);
-            }
-            uint4 tp[RB][PT];
+            for (int i = 0; i < 8; ++i) acc[i] = v4f{0, 0, 0, 0};
+            if (a < 0) {  // rows without an adapter
+                if (p.keep && block == 0)
+                    for (int i = 0; i < 16; ++i)
+                        if (same >> i & 1)
+                            for (int r = lane; r < p.a.rank; r += 64) p.keep[(m0 + i) * p.keep_pitch + r] = 0.0f;
+                if (p.base == p.out) continue;
+            } else {
+                const float scale = scale_of(p.a, a), factor = p.scaled ? scale : 1.0f;
+                const typename W::raw *w = static_cast<const typename W::raw *>(p.w) + (int64_t)a * p.a.rank * p.N;
+                for (int r0 = 0; r0 < p.a.rank; r0 += 32) {
+                    const int r = r0 + 8 * q;
+                    Block<W> rows;  // (behind the rank its last row again: t is 0 there)
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int64_t row = m0 + 16 * b + c < p.a.M ? m0 + 16 * b + c : p.a.M - 1;
-                float v[8];
-                hidden_values(p, row, r, v);
-                const bool kept = p.keep && block == 0 && (same >> (16 * b + c) & 1);
+                    for (int e = 0; e < 8; ++e)
+                        rows.rows[e].fetch(w, (uint32_t)(r + e < p.a.rank ? r + e : p.a.rank - 1) * ((uint32_t)p.N * W::BYTES), n0, p.N, edge);
+                    uint4 tp[PT];
+                    float v[8];
+                    hidden_values(p, t, c < last_row ? c : last_row, r, v);
+                    if (p.keep && block == 0 && (same >> c & 1)) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float s = v[e] * factor;
-                    if (kept && r + e < p.a.rank) p.keep[row * p.a.rank + r + e] = p.keep_scaled ? s : v[e];
-                    v[e] = s;
+                        for (int e = 0; e < 8; ++e)
+                            if (r + e < p.a.rank) p.keep[(m0 + c) * p.keep_pitch + r + e] = p.keep_scaled ? v[e] * factor : v[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= factor;
+                    parts_of(v, tp);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint4 wp[Parts<W>::N];
+                        rows.column(i, wp);
+                        acc[i] = multiply<PT>(tp, wp, acc[i]);
+                    }
                 }
-                parts_of(v, tp[b]);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                uint4 wp[Parts<W>::N];
-                block_w.column(i, wp);
-#pragma unroll
-                for (int b = 0; b < RB; ++b) acc[b][i] = multiply<PT>(tp[b], wp, acc[b][i]);
-            }
-        }
-        if (n0 >= p.N) continue;
-#pragma unroll
-        for (int b = 0; b < RB; ++b)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int i = 16 * b + 4 * q + v;
-                if (same >> i & 1) {
+            for (int v = 0; v < 4; ++v)
+                if (same >> (4 * q + v) & 1 && n0 < p.N) {
                     float y[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = acc[b][e][v];
-                    if (p.base) {
-                        Neighbours<O> n;
-                        n.fetch(static_cast<const typename O::raw *>(p.base) + (m0 + i) * p.ld_base, n0, p.N);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] += n.get(e);
-                    }
-                    put_neighbours<O>(static_cast<typename O::raw *>(p.out) + (m0 + i) * p.ld_out, n0, p.N, y);
+                    for (int e = 0; e < 8; ++e) y[e] = p.base ? acc[e][v] + base[v].get(e) : acc[e][v];
+                    put_neighbours<O>(out, (uint32_t)(4 * q + v) * ((uint32_t)p.ld_out * O::BYTES), n0, p.N, edge, y);
                 }
-            }
-    }
-}
-
-// ---- the batch's rows by adapter -------------------------------------------------------------------------------------------
-// order: rows with an adapter, sorted by it, in the batch's order; starts [R + 1].  An adapter's rows are summed in pieces of
-// `piece` rows: task starts[a] / piece + a + j has the j-th (no two adapters' tasks meet, as starts grow by an adapter's rows).
-struct PlanParams {
-    AdapterParams a;
-    int piece;
-    int32_t *order, *starts;
-    int4 *tasks;  // [tasks_most] adapter (-1: nothing to do), first and last place in order, pieces of the adapter
-    int tasks_most;
-};
-__device__ __forceinline__ int task_of(int start, int a, int piece) { return start / piece + a; }
-
-// A workgroup has an adapter: each thread looks through neighbouring rows for those of the adapter and those of smaller ones
-__global__ __launch_bounds__(1024) void plan_kernel(const PlanParams p)
-{
-    __shared__ int equal_before[16], less_before[16];
-    const int a = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int each = (int)((p.a.M + 1023) / 1024);
-    const int64_t from = (int64_t)threadIdx.x * each, to = from + each < p.a.M ? from + each : p.a.M;
-    int equal = 0, less = 0;
-    for (int64_t m = from; m < to; ++m) {
-        const int b = p.a.adapter[m];
-        equal += b == a;
-        less += b >= 0 && b < a;
-    }
-    int before = equal, all_less = less;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int v = __shfl_up(before, off, 64);
-        if (lane >= off) before += v;
-        all_less += __shfl_xor(all_less, off, 64);
-    }
-    if (lane == 63) {
-        equal_before[wave] = before;
-        less_before[wave] = all_less;
-    }
-    __syncthreads();
-    int start = 0, waves_before = 0, count = 0;
-    for (int w = 0; w < 16; ++w) {
-        start += less_before[w];
-        if (w < wave) waves_before += equal_before[w];
-        count += equal_before[w];
-    }
-    int at = start + waves_before + before - equal;
-    for (int64_t m = from; m < to; ++m)
-        if (p.a.adapter[m] == a) p.order[at++] = (int32_t)m;
-    if (threadIdx.x == 0) {
-        p.starts[a] = start;
-        if (a == p.a.R - 1) p.starts[p.a.R] = start + count;
-    }
-    // (behind the last adapter's: fewer rows than the batch's may have an adapter)
-    const int first = task_of(start, a, p.piece), next = a + 1 < p.a.R ? task_of(start + count, a + 1, p.piece) : p.tasks_most;
-    const int pieces = count ? (count + p.piece - 1) / p.piece : 1;
-    for (int i = first + (int)threadIdx.x; i < next; i += 1024) {
-        const int j = i - first, last = (j + 1) * p.piece < count ? (j + 1) * p.piece : count;
-        p.tasks[i] = j < pieces ? make_int4(a, start + j * p.piece, start + last, pieces) : make_int4(-1, 0, 0, 0);
+        }
     }
 }
 
 // ---- outer ----------------------------------------------------------------------------------------------------------------
-struct OuterParams {
-    AdapterParams a;
-    const float *coeff;  // [M, rank]
+struct OuterSide {
+    const float *coeff;  // [M, coeff_pitch]
     const void *y;       // [M, N] of stride ld
     const float *steps;  // of rows kept in 8 bits: [M, groups]
     int64_t ld;
-    int N, column_blocks, rank_chunks, groups, group_shift, piece;
+    int coeff_pitch, N, column_blocks, groups, group_shift;
     bool scaled;         // the result is multiplied by the adapter's scale
-    bool accumulate;
-    const int32_t *order, *starts;
-    const int4 *tasks;
-    int tasks_most;
     float *partials;     // [parts, rank, N]
     void *grad;          // [R, rank, N]
 };
+struct OuterParams {
+    AdapterParams a;
+    OuterSide side[2];  // d_down's and d_up's, without columns if not wanted
+    int rank_chunks, grad_dtype;
+    bool accumulate;
+    PlanParams plan;
+};
 template <> struct Parts<Codes> { static constexpr int N = 3; };
 
-template <class O>
-__device__ __forceinline__ void write_grad(const OuterParams &p, int a, int r, int64_t n, float v)
+__device__ __forceinline__ void write_grad(const OuterParams &p, const OuterSide &side, int a, int64_t at, float v)
 {
-    typename O::raw *at = static_cast<typename O::raw *>(p.grad) + ((int64_t)a * p.a.rank + r) * p.N + n;
-    v *= p.scaled ? scale_of(p.a, a) : 1.0f;
-    if (p.accumulate) v += O::get(*at);
-    *at = O::put(in_binary32(v));
+    v *= side.scaled ? scale_of(p.a, a) : 1.0f;
+    at += (int64_t)a * p.a.rank * side.N;
+    auto write = [&](auto o) {
+        using O = decltype(o);
+        typename O::raw *to = static_cast<typename O::raw *>(side.grad) + at;
+        if (p.accumulate) v += O::get(*to);
+        *to = O::put(in_binary32(v));
+    };
+    if (p.grad_dtype == MKQ_F32) write(ElemF32());
+    else if (p.grad_dtype == MKQ_F16) write(ElemF16());
+    else write(ElemBF16());
 }
 
-// A wave has a piece of an adapter's rows, 128 columns and RT * 16 of the rank: 32 rows a step, lane (c, q) fetches eight neighbouring columns
-// of eight of them
-template <class Y, class O, int RT>
-__global__ __launch_bounds__(256) void outer_kernel(const OuterParams p)
-{
-    const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
-    int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int block = (int)(task % p.column_blocks);
-    task /= p.column_blocks;
-    const int chunk = (int)(task % p.rank_chunks);
-    task /= p.rank_chunks;
-    if (task >= p.tasks_most) return;
-    const int4 what = p.tasks[task];
-    const int a = __builtin_amdgcn_readfirstlane(what.x), first = __builtin_amdgcn_readfirstlane(what.y), last = __builtin_amdgcn_readfirstlane(what.z);
-    const int pieces = __builtin_amdgcn_readfirstlane(what.w);
-    if (a < 0) return;
-    if (first == last && p.accumulate) return;
-    const int64_t n0 = (int64_t)block * 128 + 8 * c;
-    v4f acc[RT][8];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[r][i] = v4f{0, 0, 0, 0};
-    for (int s = first; s < last; s += 32) {
-        Block<Y> y;
-        float step[8], coeff[RT][8];
+// 32 rows of a piece on their way: lane (c, q) has eight neighbouring columns of rows 8 q .. 8 q + 7, and their coefficients for place c of the rank
+template <class Y, int RT>
+struct OuterStage {
+    Block<Y> y;
+    float coeff[RT][8], step[Y::BYTES == 1 ? 8 : 1];
+    // rows: in lanes from `first` on, the piece's
+    __device__ __forceinline__ void fetch(const OuterParams &p, const OuterSide &side, int chunk, int n0, bool edge, int rows, int first)
+    {
+        const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            // behind the last row: that row again, times 0
-            const int place = s + 8 * q + e;
-            const int64_t row = p.order[place < last ? place : last - 1];
-            y.rows[e].clear();
-            if (n0 < p.N) {
-                y.rows[e].fetch(static_cast<const typename Y::raw *>(p.y) + row * p.ld, n0, p.N);
-                if constexpr (Y::BYTES == 1) step[e] = p.steps[row * p.groups + (n0 >> p.group_shift)];
-            } else {
-                step[e] = 0.0f;
-            }
+            const int64_t row = __shfl(rows, first + 8 * q + e, 64);
+            y.rows[e].fetch(static_cast<const typename Y::raw *>(side.y) + row * side.ld, n0, side.N, edge);
+            if constexpr (Y::BYTES == 1) step[e] = side.steps[row * side.groups + ((n0 < side.N ? n0 : 0) >> side.group_shift)];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const int at = (chunk * RT + r) * 16 + c;
-                coeff[r][e] = place < last && at < p.a.rank ? p.coeff[row * p.a.rank + at] : 0.0f;
+                coeff[r][e] = side.coeff[row * side.coeff_pitch + (at < p.a.rank ? at : 0)];
             }
         }
+    }
+    // left: how many of the rows are the piece's; the others are its last row again, times 0
+    __device__ __forceinline__ void add(v4f (&acc)[RT][8], int left)
+    {
+        const int q = (threadIdx.x & 63) >> 4;
         uint4 cp[RT][3];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) parts_of(coeff[r], cp[r]);
+        for (int r = 0; r < RT; ++r) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) coeff[r][e] = 8 * q + e < left ? coeff[r][e] : 0.0f;
+            parts_of(coeff[r], cp[r]);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             uint4 yp[Parts<Y>::N];
@@ -576,47 +633,111 @@ __global__ __launch_bounds__(256) void outer_kernel(const OuterParams p)
             for (int r = 0; r < RT; ++r) acc[r][i] = multiply<3>(cp[r], yp, acc[r][i]);
         }
     }
-    const int start = p.starts[a], part = 2 * (start / p.piece) + (first - start) / p.piece;
+};
+
+// A piece of an adapter's rows, 128 columns and RT * 16 of the rank.  The rows of the next step are asked for before those at hand are used.
+template <class Y, int RT>
+__device__ __forceinline__ void outer(const OuterParams &p, const OuterSide &side, int block, int chunk, int a, int first, int last, int pieces)
+{
+    const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4, n0 = block * 128 + 8 * c, n = last - first;
+    const bool edge = block * 128 + 128 > side.N;
+    v4f acc[RT][8];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[r][i] = v4f{0, 0, 0, 0};
+    const int32_t *order = p.plan.order + first;
+    auto places = [&](int s) { return (int)order[s + lane < n ? s + lane : n - 1]; };
+    if (n > 0) {
+        OuterStage<Y, RT> even, odd;
+        int rows = places(0);
+        even.fetch(p, side, chunk, n0, edge, rows, 0);
+        for (int s = 0; s < n; s += 64) {
+            int next = rows;
+            if (s + 64 < n) next = places(s + 64);
+            if (s + 32 < n) odd.fetch(p, side, chunk, n0, edge, rows, 32);
+            even.add(acc, n - s);
+            rows = next;
+            if (s + 64 < n) even.fetch(p, side, chunk, n0, edge, rows, 0);
+            if (s + 32 < n) odd.add(acc, n - s - 32);
+        }
+    }
+    const int start = p.plan.starts[a], part = 2 * (start / p.plan.piece) + (first - start) / p.plan.piece;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int at = (chunk * RT + r) * 16 + 4 * q + v;
             if (at >= p.a.rank) continue;
+            if (pieces > 1 && n0 + 8 <= side.N) {
+                float *to = side.partials + ((int64_t)part * p.a.rank + at) * side.N + n0;
+#pragma unroll
+                for (int i = 0; i < 8; i += 4)
+                    reinterpret_cast<Loose<4> *>(to + i)->v = u32x4{__float_as_uint(acc[r][i][v]), __float_as_uint(acc[r][i + 1][v]),
+                                                                    __float_as_uint(acc[r][i + 2][v]), __float_as_uint(acc[r][i + 3][v])};
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (n0 + i >= p.N) continue;
-                if (pieces > 1) p.partials[((int64_t)part * p.a.rank + at) * p.N + n0 + i] = acc[r][i][v];
-                else write_grad<O>(p, a, at, n0 + i, acc[r][i][v]);
+                if (n0 + i >= side.N) continue;
+                if (pieces > 1) side.partials[((int64_t)part * p.a.rank + at) * side.N + n0 + i] = acc[r][i][v];
+                else write_grad(p, side, a, (int64_t)at * side.N + n0 + i, acc[r][i][v]);
             }
         }
 }
 
+template <class X, class D, int RT>
+__global__ __launch_bounds__(256, (X::BYTES < 4 && D::BYTES < 4 ? 4 : 3) - RT) void outer_kernel(const OuterParams p)
+{
+    const int blocks = p.side[0].column_blocks + p.side[1].column_blocks;
+    int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = (int)(task % blocks);
+    task /= blocks;
+    const int chunk = (int)(task % p.rank_chunks);
+    task /= p.rank_chunks;
+    if (task >= p.plan.tasks_most) return;
+    const int4 what = p.plan.tasks[task];
+    const int a = __builtin_amdgcn_readfirstlane(what.x), first = __builtin_amdgcn_readfirstlane(what.y), last = __builtin_amdgcn_readfirstlane(what.z);
+    const int pieces = __builtin_amdgcn_readfirstlane(what.w);
+    if (a < 0 || (first == last && p.accumulate)) return;
+    if (block < p.side[0].column_blocks) outer<X, RT>(p, p.side[0], block, chunk, a, first, last, pieces);
+    else outer<D, RT>(p, p.side[1], block - p.side[0].column_blocks, chunk, a, first, last, pieces);
+}
+
 // Adds up the pieces of the adapters that have several, in their order
-template <class O>
 __global__ __launch_bounds__(256) void outer_join_kernel(const OuterParams p)
 {
-    const int64_t values = (int64_t)p.a.rank * p.N;
-    const unsigned blocks = (unsigned)((values + 1023) / 1024);
+    const int columns = p.side[0].column_blocks ? p.side[0].N : 0;
+    const int64_t values0 = (int64_t)p.a.rank * columns, values = values0 + (p.side[1].column_blocks ? (int64_t)p.a.rank * p.side[1].N : 0);
+    const unsigned blocks = (unsigned)((values + 255) / 256);
     const int a = (int)(blockIdx.x / blocks);
-    const int start = p.starts[a], count = p.starts[a + 1] - start;
-    if (count <= p.piece) return;
-    const int pieces = (count + p.piece - 1) / p.piece;
-    const float *from = p.partials + (int64_t)(2 * (start / p.piece)) * values;
-    const int64_t first = (int64_t)(blockIdx.x - (unsigned)a * blocks) * 1024 + threadIdx.x;
-    for (int u = 0; u < 4; ++u) {
-        const int64_t i = first + u * 256;
-        if (i >= values) return;
-        float sum = 0.0f;
-        for (int j = 0; j < pieces; ++j) sum += from[j * values + i];
-        const int r = (int)(i / p.N);
-        write_grad<O>(p, a, r, i - (int64_t)r * p.N, sum);
+    const int start = p.plan.starts[a], count = p.plan.starts[a + 1] - start;
+    if (count <= p.plan.piece) return;
+    const int pieces = (count + p.plan.piece - 1) / p.plan.piece;
+    int64_t i = (int64_t)(blockIdx.x - (unsigned)a * blocks) * 256 + threadIdx.x;
+    if (i >= values) return;
+    const bool second = i >= values0;
+    const OuterSide &side = p.side[second];
+    i -= second ? values0 : 0;
+    const int64_t step = (int64_t)p.a.rank * side.N;
+    const float *from = side.partials + (int64_t)(2 * (start / p.plan.piece)) * step + i;
+    float sum = 0.0f;
+    int j = 0;
+    for (; j + 8 <= pieces; j += 8) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = from[(j + k) * step];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += v[k];
     }
+    for (; j < pieces; ++j) sum += from[j * step];
+    write_grad(p, side, a, i, sum);
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
 constexpr int64_t ADAPTERS_MOST = 0x3FFFFF, SIDES_MOST = 0x7FFFFF00;
 constexpr int RANK_MOST = 256;
+constexpr int64_t STRIDE_MOST = (int64_t)1 << 25;  // elements between rows: 16 of them are addressed in 32 bits
 constexpr int FEW_ROWS = 512;  // up to here a tile's adapters are shared out among workgroups
 
 struct AdapterShape {
@@ -626,7 +747,9 @@ struct AdapterShape {
 static int check_shape(const AdapterShape &d)
 {
     if (d.M < 0 || d.K <= 0 || d.N <= 0 || d.R <= 0 || d.rank <= 0) return MKQ_ERR_SHAPE;
-    if (d.M > SIDES_MOST || d.K > SIDES_MOST || d.N > SIDES_MOST || d.R > ADAPTERS_MOST || d.rank > RANK_MOST) return MKQ_ERR_UNSUPPORTED;
+    if (d.M > SIDES_MOST || d.K > SIDES_MOST || d.N > SIDES_MOST || d.R > ADAPTERS_MOST || d.rank > RANK_MOST || d.K * d.rank >= (int64_t)1 << 29 || d.N * d.rank >= (int64_t)1 << 29 ||
+        d.K > STRIDE_MOST || d.N > STRIDE_MOST)
+        return MKQ_ERR_UNSUPPORTED;
     return MKQ_OK;
 }
 
@@ -651,16 +774,30 @@ static void with_tiles(int tiles, F &&f)
     else f(std::integral_constant<int, 4>());
 }
 
-static int launch_shrink(const AdapterShape &d, const AdapterParams &a, const void *x, int x_dtype, int64_t ldx, const void *w, int w_dtype, int64_t side,
-                         bool scaled, float *t, hipStream_t st)
+static ShrinkParams shrink_params(const AdapterShape &d, const AdapterParams &a, const void *x, int64_t ldx, const void *w, int64_t side, bool scaled, float *t,
+                                  float *hidden)
 {
-    const int tiles = rank_tiles(d.rank);
-    const ShrinkParams p = {a, x, w, ldx, (int)side, slots_of(d), (int)ceil_div(d.rank, 16 * tiles), (int)ceil_div(ceil_div(side, SHRINK_STEP), a.splits), scaled, t};
-    const int64_t workgroups = ceil_div(d.M, 16) * p.slots * a.splits * p.rank_chunks;
+    ShrinkParams p = {};
+    p.a = a;
+    p.x = x;
+    p.w = w;
+    p.ldx = ldx;
+    p.K = (int)side;
+    p.slots = slots_of(d);
+    p.rank_chunks = (int)ceil_div(d.rank, 16 * rank_tiles(d.rank));
+    p.per_split = (int)ceil_div(ceil_div(side, SHRINK_STEP), a.splits);
+    p.scaled = scaled;
+    p.t = t;
+    p.hidden = hidden;
+    return p;
+}
+static int launch_shrink(const AdapterShape &d, const ShrinkParams &p, int x_dtype, int w_dtype, hipStream_t st)
+{
+    const int64_t workgroups = (p.x ? ceil_div(d.M, 16) * p.slots * p.a.splits * p.rank_chunks : 0) + p.plans;
     if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
     with_elem(x_dtype, [&](auto x_e) {
         with_elem(w_dtype, [&](auto w_e) {
-            with_tiles(tiles, [&](auto n) { shrink_kernel<decltype(x_e), decltype(w_e), decltype(n)::value><<<(unsigned)workgroups, 256, 0, st>>>(p); });
+            with_tiles(rank_tiles(d.rank), [&](auto n) { shrink_kernel<decltype(x_e), decltype(w_e), decltype(n)::value><<<(unsigned)workgroups, 256, 0, st>>>(p); });
         });
     });
     return launch_status();
@@ -668,27 +805,30 @@ static int launch_shrink(const AdapterShape &d, const AdapterParams &a, const vo
 
 static int launch_expand(const AdapterShape &d, ExpandParams p, int w_dtype, int out_dtype, hipStream_t st)
 {
-    const int rows = d.M <= FEW_ROWS * 4 ? 16 : 64;
     p.column_blocks = (int)ceil_div(p.N, 128);
-    p.row_groups = (int)ceil_div(d.M, rows);
     p.slots = slots_of(d);
+    // tiles of a wave: four, if 4096 waves are left then
+    const int64_t all = ceil_div(d.M, 16), fill = all * p.column_blocks / 4096;
+    p.tiles = (int)(fill < 1 ? 1 : fill > 4 ? 4 : fill);
+    p.row_groups = (int)ceil_div(all, p.tiles);
     const int64_t workgroups = ceil_div((int64_t)p.column_blocks * p.row_groups * p.slots, 4);
     if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
     with_elem(w_dtype, [&](auto w) {
         with_elem(out_dtype, [&](auto o) {
-            if (rows == 16) expand_kernel<decltype(w), decltype(o), 1><<<(unsigned)workgroups, 256, 0, st>>>(p);
-            else expand_kernel<decltype(w), decltype(o), 4><<<(unsigned)workgroups, 256, 0, st>>>(p);
+            expand_kernel<decltype(w), decltype(o)><<<(unsigned)workgroups, 256, 0, st>>>(p);
         });
     });
     return launch_status();
 }
 
-// Rows of a piece: about 1280 waves in all
+// Rows of a piece: about 2000 waves in all
 static int piece_rows(const AdapterShape &d)
 {
-    const int64_t columns = ceil_div(d.K, 128) + ceil_div(d.N, 128), n = ceil_div(ceil_div(d.M * columns, 1280), 32) * 32;
+    const int64_t columns = ceil_div(d.K, 128) + ceil_div(d.N, 128), n = ceil_div(ceil_div(d.M * columns, 2048), 64) * 64;
     return (int)(n < 64 ? 64 : n > 2048 ? 2048 : n);
 }
+
+static int pitch_of(int rank) { return (rank + 7) / 8 * 8; }
 
 struct AdapterWorkspace {
     size_t t, u, order, starts, tasks, down, up, total;
@@ -699,7 +839,7 @@ static AdapterWorkspace forward_workspace(const AdapterShape &d)
 {
     AdapterWorkspace w = {};
     w.splits = splits_of(d, d.K);
-    w.total = (size_t)w.splits * d.M * d.rank * sizeof(float);
+    w.total = (size_t)w.splits * d.M * pitch_of(d.rank) * sizeof(float);
     return w;
 }
 static AdapterWorkspace gradient_workspace(const AdapterShape &d)
@@ -713,7 +853,7 @@ static AdapterWorkspace gradient_workspace(const AdapterShape &d)
     w.splits = splits_of(d, d.N);
     w.piece = piece_rows(d);
     w.tasks_most = d.M / w.piece + d.R;
-    const size_t hidden = (size_t)d.M * d.rank * sizeof(float), parts = d.M > w.piece ? 2 * (size_t)(d.M / w.piece) + 2 : 0;
+    const size_t hidden = (size_t)d.M * pitch_of(d.rank) * sizeof(float), parts = d.M > w.piece ? 2 * (size_t)(d.M / w.piece) + 2 : 0;
     w.t = take(w.splits > 1 ? hidden * w.splits : 0);
     w.u = take(hidden);
     w.order = take((size_t)d.M * sizeof(int32_t));
@@ -731,21 +871,20 @@ static void with_rows(int dtype, F &&f)
     else with_elem(dtype, f);
 }
 
-static int launch_outer(const AdapterShape &d, OuterParams p, int y_dtype, int grad_dtype, hipStream_t st)
+static int launch_outer(const AdapterShape &d, OuterParams p, int x_dtype, int dy_dtype, hipStream_t st)
 {
-    p.column_blocks = (int)ceil_div(p.N, 128);
     const int tiles = d.rank <= 16 ? 1 : 2;
     p.rank_chunks = (int)ceil_div(d.rank, 16 * tiles);
-    const int64_t workgroups = ceil_div((int64_t)p.tasks_most * p.column_blocks * p.rank_chunks, 4);
-    const int64_t joins = d.R * ceil_div((int64_t)d.rank * p.N, 1024);
+    const int64_t workgroups = ceil_div((int64_t)p.plan.tasks_most * (p.side[0].column_blocks + p.side[1].column_blocks) * p.rank_chunks, 4);
+    const int64_t joins = d.R * ceil_div((int64_t)d.rank * ((p.side[0].column_blocks ? d.K : 0) + (p.side[1].column_blocks ? d.N : 0)), 256);
     if (!grid_ok(workgroups, 256) || !grid_ok(joins, 256)) return MKQ_ERR_UNSUPPORTED;
-    with_rows(y_dtype, [&](auto y) {
-        with_elem(grad_dtype, [&](auto o) {
-            if (tiles == 1) outer_kernel<decltype(y), decltype(o), 1><<<(unsigned)workgroups, 256, 0, st>>>(p);
-            else outer_kernel<decltype(y), decltype(o), 2><<<(unsigned)workgroups, 256, 0, st>>>(p);
-            if (d.M > p.piece) outer_join_kernel<decltype(o)><<<(unsigned)joins, 256, 0, st>>>(p);
+    with_rows(x_dtype, [&](auto x) {
+        with_elem(dy_dtype, [&](auto y) {
+            if (tiles == 1) outer_kernel<decltype(x), decltype(y), 1><<<(unsigned)workgroups, 256, 0, st>>>(p);
+            else outer_kernel<decltype(x), decltype(y), 2><<<(unsigned)workgroups, 256, 0, st>>>(p);
         });
     });
+    if (d.M > p.plan.piece) outer_join_kernel<<<(unsigned)joins, 256, 0, st>>>(p);
     return launch_status();
 }
 
@@ -772,16 +911,28 @@ extern "C" int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, co
     if (!aligned16(x) || !aligned4(adapter) || !aligned16(down) || !aligned16(up) || !aligned4(scales) || !aligned16(base) || !aligned16(out) || !aligned4(hidden))
         return MKQ_ERR_ALIGN;
     if (status != MKQ_OK) return status;
+    if (ld_out > STRIDE_MOST || (base && ld_base > STRIDE_MOST)) return MKQ_ERR_UNSUPPORTED;
     if (base && !in_place_or_apart(base, out_dtype, ld_base, out, out_dtype, ld_out, M, N)) return MKQ_ERR_UNSUPPORTED;
     const AdapterWorkspace w = forward_workspace(d);
     if (!workspace || workspace_bytes < w.total) return MKQ_ERR_WORKSPACE;
     if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
     const hipStream_t st = as_stream(stream);
-    const AdapterParams a = {adapter, scales, M, (int)R, rank, w.splits};
-    float *t = w.splits == 1 && hidden ? hidden : static_cast<float *>(workspace);
-    status = launch_shrink(d, a, x, x_dtype, ldx, down, w_dtype, K, false, t, st);
+    const AdapterParams a = {adapter, scales, M, (int)R, rank, pitch_of(rank), w.splits};
+    float *t = static_cast<float *>(workspace);
+    status = launch_shrink(d, shrink_params(d, a, x, ldx, down, K, false, t, w.splits == 1 ? hidden : nullptr), x_dtype, w_dtype, st);
     if (status != MKQ_OK) return status;
-    ExpandParams e = {a, t, up, base, out, ld_base, ld_out, (int)N, 0, 0, 0, true, false, w.splits > 1 ? hidden : nullptr};
+    ExpandParams e = {};
+    e.a = a;
+    e.t = t;
+    e.w = up;
+    e.base = base;
+    e.out = out;
+    e.ld_base = ld_base;
+    e.ld_out = ld_out;
+    e.N = (int)N;
+    e.scaled = true;
+    e.keep = w.splits > 1 ? hidden : nullptr;
+    e.keep_pitch = rank;
     return launch_expand(d, e, w_dtype, out_dtype, st);
 }
 
@@ -816,6 +967,7 @@ extern "C" int mkq_low_rank_adapters_gradient(const void *dy, int dy_dtype, int6
     if (status != MKQ_OK) return status;
     const int64_t pitch = kept ? ceil_div(K, 32) * 32 : ldx;
     if (dx && M > 0) {
+        if (ld_dx > STRIDE_MOST || (dx_base && ld_dx_base > STRIDE_MOST)) return MKQ_ERR_UNSUPPORTED;
         if (dx_base && !in_place_or_apart(dx_base, dx_dtype, ld_dx_base, dx, dx_dtype, ld_dx, M, K)) return MKQ_ERR_UNSUPPORTED;
         // the batch's rows are read again behind dx
         if (!apart(dy, dy_dtype, ld_dy, N, dx, dx_dtype, ld_dx, K, M) || (d_down && !apart(x, x_dtype, pitch, K, dx, dx_dtype, ld_dx, K, M))) return MKQ_ERR_UNSUPPORTED;
@@ -825,51 +977,66 @@ extern "C" int mkq_low_rank_adapters_gradient(const void *dy, int dy_dtype, int6
     if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     const hipStream_t st = as_stream(stream);
-    AdapterParams a = {adapter, scales, M, (int)R, rank, dx && M > 0 ? w.splits : 1};
-    float *u = reinterpret_cast<float *>(ws + w.u);
-    if (M > 0 && (dx || d_down)) {
-        float *t = a.splits > 1 ? reinterpret_cast<float *>(ws + w.t) : u;
-        status = launch_shrink(d, a, dy, dy_dtype, ld_dy, up, w_dtype, N, a.splits == 1, t, st);
+    const AdapterParams a = {adapter, scales, M, (int)R, rank, pitch_of(rank), dx && M > 0 ? w.splits : 1};
+    float *u = reinterpret_cast<float *>(ws + w.u), *t = a.splits > 1 ? reinterpret_cast<float *>(ws + w.t) : u;
+    const PlanParams plan = {w.piece, (int)w.tasks_most, reinterpret_cast<int32_t *>(ws + w.order), reinterpret_cast<int32_t *>(ws + w.starts),
+                             reinterpret_cast<int4 *>(ws + w.tasks)};
+    // one launch puts the rows in order and makes u
+    const bool products = M > 0 && (dx || d_down);
+    ShrinkParams shrink = shrink_params(d, a, products ? dy : nullptr, ld_dy, up, N, a.splits == 1, t, nullptr);
+    shrink.plans = d_down || d_up ? (int)R : 0;
+    shrink.plan = plan;
+    if (products || shrink.plans) {
+        status = launch_shrink(d, shrink, dy_dtype, w_dtype, st);
         if (status != MKQ_OK) return status;
-        if (dx) {
-            ExpandParams e = {a, t, down, dx_base, dx, ld_dx_base, ld_dx, (int)K, 0, 0, 0, a.splits > 1, true, a.splits > 1 ? u : nullptr};
-            status = launch_expand(d, e, w_dtype, dx_dtype, st);
-            if (status != MKQ_OK) return status;
-        }
+    }
+    if (dx && M > 0) {
+        ExpandParams e = {};
+        e.a = a;
+        e.t = t;
+        e.w = down;
+        e.base = dx_base;
+        e.out = dx;
+        e.ld_base = ld_dx_base;
+        e.ld_out = ld_dx;
+        e.N = (int)K;
+        e.scaled = e.keep_scaled = a.splits > 1;
+        e.keep = a.splits > 1 ? u : nullptr;
+        e.keep_pitch = a.pitch;
+        status = launch_expand(d, e, w_dtype, dx_dtype, st);
+        if (status != MKQ_OK) return status;
     }
     if (!d_down && !d_up) return MKQ_OK;
-    PlanParams plan = {a, w.piece, reinterpret_cast<int32_t *>(ws + w.order), reinterpret_cast<int32_t *>(ws + w.starts), reinterpret_cast<int4 *>(ws + w.tasks), (int)w.tasks_most};
-    plan_kernel<<<(unsigned)R, 1024, 0, st>>>(plan);
-    status = launch_status();
     OuterParams o = {};
     o.a = a;
-    o.piece = w.piece;
+    o.plan = plan;
+    o.grad_dtype = grad_dtype;
     o.accumulate = accumulate != 0;
-    o.order = plan.order;
-    o.starts = plan.starts;
-    o.tasks = plan.tasks;
-    o.tasks_most = (int)w.tasks_most;
-    if (status == MKQ_OK && d_down) {
-        o.coeff = u;
-        o.y = x;
-        o.steps = x_steps;
-        o.ld = pitch;
-        o.N = (int)K;
-        o.group_shift = x_group == 32 ? 5 : x_group == 64 ? 6 : 7;
-        o.groups = kept ? (int)ceil_div(K, x_group) : 0;
-        o.partials = reinterpret_cast<float *>(ws + w.down);
-        o.grad = d_down;
-        status = launch_outer(d, o, x_dtype, grad_dtype, st);
+    if (d_down) {
+        OuterSide &s = o.side[0];
+        s.coeff = u;
+        s.coeff_pitch = a.pitch;
+        s.y = x;
+        s.steps = x_steps;
+        s.ld = pitch;
+        s.N = (int)K;
+        s.column_blocks = (int)ceil_div(K, 128);
+        s.group_shift = x_group == 32 ? 5 : x_group == 64 ? 6 : 7;
+        s.groups = kept ? (int)ceil_div(K, x_group) : 0;
+        s.partials = reinterpret_cast<float *>(ws + w.down);
+        s.grad = d_down;
     }
-    if (status == MKQ_OK && d_up) {
-        o.coeff = hidden;
-        o.y = dy;
-        o.ld = ld_dy;
-        o.N = (int)N;
-        o.scaled = true;
-        o.partials = reinterpret_cast<float *>(ws + w.up);
-        o.grad = d_up;
-        status = launch_outer(d, o, dy_dtype, grad_dtype, st);
+    if (d_up) {
+        OuterSide &s = o.side[1];
+        s.coeff = hidden;
+        s.coeff_pitch = rank;
+        s.y = dy;
+        s.ld = ld_dy;
+        s.N = (int)N;
+        s.column_blocks = (int)ceil_div(N, 128);
+        s.scaled = true;
+        s.partials = reinterpret_cast<float *>(ws + w.up);
+        s.grad = d_up;
     }
-    return status;
+    return launch_outer(d, o, d_down ? x_dtype : MKQ_F32, dy_dtype, st);
 }
