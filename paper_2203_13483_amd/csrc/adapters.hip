@@ -12,23 +12,13 @@
 // one to three bfloat16 parts (binary32 three, binary16 two), and products of parts whose places add up to 2^-24 or less are left out.
 // Sums are binary32.  A tile of rows may hold any adapters: it is gone through once for each of them, results are taken for the rows
 // that have it, so a request's infinities and NaN stay in its rows.
-#include "elements.h"
 #include "gemm_common.h"
+#include "neighbours.h"
 
 namespace mkq {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
-
-// 16 bytes from an address that only fits their elements (the unit takes any)
-template <int BYTES>
-struct __attribute__((packed, aligned(BYTES))) Loose {
-    u32x4 v;
-};
-struct Codes {  // rows kept in 8 bits
-    using raw = int8_t;
-    static constexpr int BYTES = 1;
-};
 
 struct AdapterParams {
     const int32_t *adapter;
@@ -111,103 +101,6 @@ __device__ __forceinline__ v4f multiply(const uint4 (&a)[PA], const uint4 (&b)[P
     return c;
 }
 
-// Eight neighbours of a row from place k on, as fetched.  Whole vectors only, and no branch that lanes of a wave take apart: where the row
-// ends among a wave's places (`edge`), its last eight elements are fetched instead and moved down, zeros behind them.  A row of fewer than
-// eight is fetched one by one.  (Rows kept in 8 bits have zeros behind them.)
-template <class E>
-struct Neighbours {
-    u32x4 w[E::BYTES == 4 ? 2 : 1];
-    __device__ __forceinline__ void without_first(int n)
-    {
-        if constexpr (E::BYTES == 2) {
-            u32x4 &v = w[0];
-            if (n & 1)
-                v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16), v[3] >> 16};
-            if (n & 2) v = u32x4{v[1], v[2], v[3], 0};
-            if (n & 4) v = u32x4{v[2], v[3], 0, 0};
-            if (n >= 8) v = u32x4{0, 0, 0, 0};
-        } else {
-            u32x4 &v = w[0], &x = w[E::BYTES / 4];
-            if (n & 1) {
-                v = u32x4{v[1], v[2], v[3], x[0]};
-                x = u32x4{x[1], x[2], x[3], 0};
-            }
-            if (n & 2) {
-                v = u32x4{v[2], v[3], x[0], x[1]};
-                x = u32x4{x[2], x[3], 0, 0};
-            }
-            if (n >= 4) {
-                v = n >= 8 ? u32x4{0, 0, 0, 0} : x;
-                x = u32x4{0, 0, 0, 0};
-            }
-        }
-    }
-    // `row`: the bytes of a row, or a place that all lanes share with `off` bytes to a lane's row
-    __device__ __forceinline__ void fetch(const void *row, int k, int end, bool edge) { fetch(row, 0u, k, end, edge); }
-    __device__ __forceinline__ void fetch(const void *place, uint32_t off, int k, int end, bool edge)
-    {
-        const uint8_t *row = static_cast<const uint8_t *>(place);
-        if constexpr (E::BYTES == 1) {
-            if (edge) k = k < end ? k : (end - 1) & ~7;
-            const uint2 v = *reinterpret_cast<const uint2 *>(row + (off + (uint32_t)k));
-            w[0] = u32x4{v.x, v.y, 0, 0};
-        } else {
-            if (end < 8) return fetch_short(row, off, k, end);
-            const int from = edge && k + 8 > end ? end - 8 : k;
-            const uint8_t *at = row + (off + (uint32_t)from * E::BYTES);
-            w[0] = reinterpret_cast<const Loose<E::BYTES> *>(at)->v;
-            if constexpr (E::BYTES == 4) w[1] = reinterpret_cast<const Loose<4> *>(at + 16)->v;
-            if (edge) without_first(k - from < 8 ? k - from : 8);
-        }
-    }
-    __device__ __forceinline__ void fetch_short(const uint8_t *row, uint32_t off, int k, int end)
-    {
-        w[0] = u32x4{0, 0, 0, 0};
-        if constexpr (E::BYTES == 4) w[1] = u32x4{0, 0, 0, 0};
-        if (k != 0) return;
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < end) {
-                const typename E::raw v = *reinterpret_cast<const typename E::raw *>(row + (off + i * E::BYTES));
-                if constexpr (E::BYTES == 4) w[i / 4][i % 4] = __float_as_uint(v);
-                else w[0][i / 2] |= (uint32_t)v << (16 * (i % 2));
-            }
-    }
-    __device__ __forceinline__ float get(int i) const
-    {
-        if constexpr (E::BYTES == 4) return __uint_as_float(w[i / 4][i % 4]);
-        else if constexpr (E::BYTES == 1) return (float)(int8_t)(w[0][i / 4] >> (8 * (i % 4)));
-        else return E::get((uint16_t)(w[0][i / 2] >> (16 * (i % 2))));
-    }
-};
-
-// Eight neighbours of a row from place k on, those before `end`; place and off as above
-template <class O>
-__device__ __forceinline__ void put_neighbours(void *place, uint32_t off, int k, int end, bool edge, const float (&y)[8])
-{
-    uint8_t *to = static_cast<uint8_t *>(place) + (off + (uint32_t)k * O::BYTES);
-    uint32_t w[8];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (O::BYTES == 4) {
-            w[e] = __float_as_uint(y[e]);
-            w[4 + e] = __float_as_uint(y[4 + e]);
-        } else {
-            w[e] = std::is_same<O, ElemF16>::value ? pack2_f16(in_binary32(y[2 * e]), in_binary32(y[2 * e + 1])) : pack2_bf16(y[2 * e], y[2 * e + 1]);
-        }
-    }
-    if (edge && k + 8 > end) {
-#pragma unroll
-        for (int e = 0; e < 7; ++e)
-            if (k + e < end) {
-                if constexpr (O::BYTES == 4) reinterpret_cast<uint32_t *>(to)[e] = w[e];
-                else reinterpret_cast<uint16_t *>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
-            }
-    } else {
-        reinterpret_cast<Loose<O::BYTES> *>(to)->v = u32x4{w[0], w[1], w[2], w[3]};
-        if constexpr (O::BYTES == 4) reinterpret_cast<Loose<4> *>(to + 16)->v = u32x4{w[4], w[5], w[6], w[7]};
-    }
-}
 // A number that the compiler takes for new where it stands: what follows from it is computed there again, not kept in registers around a loop
 __device__ __forceinline__ int fresh(int v)
 {
@@ -334,6 +227,8 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
     const typename X::raw *x = static_cast<const typename X::raw *>(p.x) + row * p.ldx;
     const int steps = (p.K + SHRINK_STEP - 1) / SHRINK_STEP;
     const int from = split * p.per_split, to = from + p.per_split < steps ? from + p.per_split : steps;
+    // rows a power of two apart that all began at the same place would ask the same memory channels: tiles begin at places of their own
+    const int turn = from < to ? (int)((m0 / 16) % (unsigned)(to - from)) : 0;
     float *t = p.t + (int64_t)split * p.a.M * p.a.pitch;
     Adapters adapters(mine, slot, p.slots, lane < 16 && m0 + lane < p.a.M && mine < 0);
     int a;
@@ -360,12 +255,14 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
             constexpr int N = decltype(n)::value;
             Neighbours<X> xs[N][2];
             Neighbours<W> ws[N][2][RT];
-            const bool edge = (s + 4 * (N - 1) + 1) * SHRINK_STEP > p.K;
 #pragma unroll
             for (int u = 0; u < N; ++u)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int k = (s + 4 * u) * SHRINK_STEP + h * 32 + q * 8;
+                    int step = s + 4 * u + turn;
+                    step -= step >= to ? to - from : 0;
+                    const bool edge = (step + 1) * SHRINK_STEP > p.K;
+                    const int k = step * SHRINK_STEP + h * 32 + q * 8;
                     xs[u][h].fetch(x, k, p.K, edge);
 #pragma unroll
                     for (int r = 0; r < RT; ++r) ws[u][h][r].fetch(w[r], k, p.K, edge);
@@ -474,7 +371,7 @@ __device__ __forceinline__ void hidden_values(const ExpandParams &p, const float
 // A wave has 128 columns of `tiles` tiles of 16 rows; lane (c, q) has columns 8 c .. 8 c + 7 of rows 4 q .. 4 q + 3.  The adapter's rows are fetched
 // again for every tile (from the caches), 32 at a time.
 template <class W, class O>
-__global__ __launch_bounds__(256, W::BYTES == 4 || O::BYTES == 4 ? 2 : 3) void expand_kernel(const ExpandParams p)
+__global__ __launch_bounds__(256, 2) void expand_kernel(const ExpandParams p)
 {
     constexpr int PT = O::BYTES == 4 ? 3 : 2;  // (2^-16 of a product is left out under results of 16 bits, which end at 2^-9 or 2^-12)
     const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -483,22 +380,32 @@ __global__ __launch_bounds__(256, W::BYTES == 4 || O::BYTES == 4 ? 2 : 3) void e
     const int slot = (int)(rest / p.row_groups), group = (int)(rest - (int64_t)slot * p.row_groups);
     if (slot >= p.slots) return;
     const bool edge = block * 128 + 128 > p.N;
+    const int64_t first = (int64_t)group * p.tiles * 16;
+    // at most four tiles: a row of theirs a lane
+    const int all = adapter_of(p.a, (int)(threadIdx.x & 63) < 16 * p.tiles ? first + (threadIdx.x & 63) : p.a.M);
+    auto fetch_base = [&](Neighbours<O> (&to)[4], int64_t m0) {
+        if (!p.base || m0 >= p.a.M) return;
+        const int lane = fresh(threadIdx.x & 63), q = lane >> 4, n0 = block * 128 + 8 * (lane & 15);
+        const int last_row = p.a.M - m0 < 16 ? (int)(p.a.M - m0) - 1 : 15;
+        const void *at = static_cast<const typename O::raw *>(p.base) + m0 * p.ld_base;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            to[v].fetch(at, (uint32_t)(4 * q + v < last_row ? 4 * q + v : last_row) * ((uint32_t)p.ld_base * O::BYTES), n0, p.N, edge);
+    };
+    Neighbours<O> base[4], next_base[4];
+    fetch_base(next_base, first);
     for (int tile = 0; tile < p.tiles; ++tile) {
-        const int64_t m0 = ((int64_t)group * p.tiles + tile) * 16;
+        const int64_t m0 = first + 16 * tile;
         if (m0 >= p.a.M) break;
         const int lane = fresh(threadIdx.x & 63), c = lane & 15, q = lane >> 4, n0 = block * 128 + 8 * c;
         const int last_row = p.a.M - m0 < 16 ? (int)(p.a.M - m0) - 1 : 15;
-        const int mine = adapter_of(p.a, lane < 16 ? m0 + lane : p.a.M);
-        Neighbours<O> base[4];
-        if (p.base) {
-            const void *at = static_cast<const typename O::raw *>(p.base) + m0 * p.ld_base;
+        const int mine = __shfl(all, 16 * tile + c, 64), of_tile = lane < 16 ? mine : -1;
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-                base[v].fetch(at, (uint32_t)(4 * q + v < last_row ? 4 * q + v : last_row) * ((uint32_t)p.ld_base * O::BYTES), n0, p.N, edge);
-        }
+        for (int v = 0; v < 4; ++v) base[v] = next_base[v];
+        if (tile + 1 < p.tiles) fetch_base(next_base, m0 + 16);
         typename O::raw *out = static_cast<typename O::raw *>(p.out) + m0 * p.ld_out;
         const float *t = p.t + m0 * p.a.pitch;
-        Adapters adapters(mine, slot, p.slots, lane < 16 && m0 + lane < p.a.M && mine < 0);
+        Adapters adapters(of_tile, slot, p.slots, lane < 16 && m0 + lane < p.a.M && mine < 0);
         int a;
         uint64_t same;
         while (adapters.next(a, same)) {

@@ -199,6 +199,40 @@ __device__ __forceinline__ float most_of_eight(float v)
     return fmaxf(v, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x141, 0xF, 0xF, true)));
 }
 
+// Eight neighbouring scores as they are in memory
+template <class E>
+struct Eight {
+    uint4 w[E::BYTES == 4 ? 2 : 1];
+    __device__ __forceinline__ void fetch(const typename E::raw *at)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(w) / 16); ++i) w[i] = reinterpret_cast<const uint4 *>(at)[i];
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        const uint4 &v = w[E::BYTES == 4 ? i / 4 : 0];
+        const int at = E::BYTES == 4 ? i % 4 : i / 2;
+        const uint32_t x = at == 0 ? v.x : at == 1 ? v.y : at == 2 ? v.z : v.w;
+        if constexpr (E::BYTES == 4) return __uint_as_float(x);
+        else return E::get((uint16_t)(x >> (16 * (i % 2))));
+    }
+    // (binary16: two at a time, so that get() is only an operand of the fused product)
+    __device__ __forceinline__ float most() const
+    {
+        if constexpr (std::is_same<E, ElemF16>::value) {
+            auto larger = [](uint32_t a, uint32_t b) {
+                uint32_t r;
+                asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+                return r;
+            };
+            const uint32_t two = larger(larger(w[0].x, w[0].y), larger(w[0].z, w[0].w));
+            return fmaxf(ElemF16::get((uint16_t)two), ElemF16::get((uint16_t)(two >> 16)));
+        } else {
+            return fmaxf(fmaxf(fmaxf(get(0), get(1)), fmaxf(get(2), get(3))), fmaxf(fmaxf(get(4), get(5)), fmaxf(get(6), get(7))));
+        }
+    }
+};
+
 // A row, or a part of it, seen as vectors of eight from `shift` places before its first score
 template <class E>
 struct ScoreRow {
@@ -212,29 +246,44 @@ struct ScoreRow {
         end = p.V + shift;
     }
     __device__ __forceinline__ bool whole(int v) const { return v * 8 >= shift && v * 8 + 8 <= end; }
-    __device__ __forceinline__ float at(int place, float none) const { return place >= shift && place < end ? E::get(from[place]) : none; }
-    // places outside the row: -infinity
-    __device__ __forceinline__ void get(int v, float (&x)[8]) const
+    // places outside the row, and all if not `real`: -infinity
+    __device__ __forceinline__ void get(int v, bool real, Eight<E> &x) const
     {
-        if (whole(v)) return get8<E>(from + (int64_t)v * 8, x);
+        if (real && whole(v)) return x.fetch(from + (int64_t)v * 8);
+        constexpr uint32_t NONE = E::BYTES == 4 ? 0xFF800000u : std::is_same<E, ElemF16>::value ? 0xFC00u : 0xFF80u;
+        uint32_t u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = at(v * 8 + e, -__builtin_inff());
+        for (int e = 0; e < 8; ++e) {
+            u[e] = NONE;
+            if (real && v * 8 + e >= shift && v * 8 + e < end) {
+                if constexpr (E::BYTES == 4) u[e] = __float_as_uint(from[v * 8 + e]);
+                else u[e] = from[v * 8 + e];
+            }
+        }
+        if constexpr (E::BYTES == 4) {
+            x.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+            x.w[1] = make_uint4(u[4], u[5], u[6], u[7]);
+        } else {
+            x.w[0] = make_uint4(u[0] | u[1] << 16, u[2] | u[3] << 16, u[4] | u[5] << 16, u[6] | u[7] << 16);
+        }
     }
 };
 
 constexpr int SCORE_UNROLL = 4;
 
-template <class E, bool TOP, int THREADS>
-__device__ __forceinline__ void add_vectors(const ScoreParams &p, const float (&x)[SCORE_UNROLL][8], Mass &m, float *largest, const int (&at)[SCORE_UNROLL],
-                                            int pieces)
+// N vectors of each lane, 64 apart; the first lane's first is number `first` of the workgroup's
+template <class E, bool TOP, int N>
+__device__ __forceinline__ void add_vectors(const ScoreParams &p, const Eight<E> (&x)[N], Mass &m, float *largest, int first, int pieces)
 {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int u = 0; u < SCORE_UNROLL; ++u) {
-        float v = fmaxf(fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])), fmaxf(fmaxf(x[u][4], x[u][5]), fmaxf(x[u][6], x[u][7])));
+    for (int u = 0; u < N; ++u) {
+        float v = x[u].most();
         m.most = fmaxf(m.most, v);
         if constexpr (TOP) {
             v = fmaxf(most_of_eight(v), -__builtin_inff());
-            if ((threadIdx.x & 7) == 0 && at[u] < pieces) largest[at[u]] = v;
+            const int at = (first + u * 64 + lane) / (PIECE / 8);
+            if ((lane & 7) == 0 && at < pieces) largest[at] = v;
         }
     }
     const float up = m.most * p.c;
@@ -244,10 +293,10 @@ __device__ __forceinline__ void add_vectors(const ScoreParams &p, const float (&
         m.ref = ref;
     }
 #pragma unroll
-    for (int u = 0; u < SCORE_UNROLL; ++u)
+    for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float d = __builtin_fmaf(x[u][e], p.c, -m.ref), power = __builtin_amdgcn_exp2f(d);
+            const float d = __builtin_fmaf(x[u].get(e), p.c, -m.ref), power = __builtin_amdgcn_exp2f(d);
             m.sum += power;
             m.weighted = __builtin_fmaf(power, fmaxf(d, NO_MASS), m.weighted);
         }
@@ -319,25 +368,28 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
     const int pieces = all_pieces - piece0 < p.pieces_per_part ? all_pieces - piece0 : p.pieces_per_part;
     const int v0 = piece0 * (PIECE / 8), v1 = v0 + pieces * (PIECE / 8);
 
+    // A wave has SCORE_UNROLL * 64 neighbouring vectors at a time.  Only where the row begins or ends among them they are looked at one by one.
+    // (Rows a power of two apart that all began at the same place would ask the same memory channels: each begins at another.)
     Mass m = {-__builtin_inff(), -FAR, 0.0f, 0.0f};
-    for (int v = v0; v < v1; v += THREADS * SCORE_UNROLL) {
-        float x[SCORE_UNROLL][8];
-        int at[SCORE_UNROLL];
-        const bool inside = v * 8 >= r.shift && (v + THREADS * SCORE_UNROLL) * 8 <= r.end && v + THREADS * SCORE_UNROLL <= v1;
+    constexpr int STEP = 64 * SCORE_UNROLL;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int steps = (v1 - v0 + STEP - 1) / STEP, mine = (steps - wave + WAVES - 1) / WAVES;
+    int step = mine > 0 ? (int)(blockIdx.x % (unsigned)mine) : 0;
+    for (int i = 0; i < mine; ++i, step = step + 1 < mine ? step + 1 : 0) {
+        const int v = v0 + (step * WAVES + wave) * STEP;
+        if (v * 8 >= r.shift && (v + STEP) * 8 <= r.end && v + STEP <= v1) {
+            Eight<E> x[SCORE_UNROLL];
 #pragma unroll
-        for (int u = 0; u < SCORE_UNROLL; ++u) {
-            const int mine = v + u * THREADS + (int)threadIdx.x;
-            at[u] = (mine - v0) / (PIECE / 8);
-            if (inside) {
-                get8<E>(r.from + (int64_t)mine * 8, x[u]);
-            } else if (mine < v1) {
-                r.get(mine, x[u]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[u][e] = -__builtin_inff();
+            for (int u = 0; u < SCORE_UNROLL; ++u) x[u].fetch(r.from + (int64_t)(v + u * 64 + lane) * 8);
+            add_vectors<E, TOP>(p, x, m, largest, v - v0, pieces);
+        } else {
+#pragma unroll 1
+            for (int w = v; w < v + STEP && w < v1; w += 64) {
+                Eight<E> x[1];
+                r.get(w + lane, w + lane < v1, x[0]);
+                add_vectors<E, TOP>(p, x, m, largest, w - v0, pieces);
             }
         }
-        add_vectors<E, TOP, THREADS>(p, x, m, largest, at, pieces);
     }
     m = joined(m);
     if ((threadIdx.x & 63) == 0) masses[threadIdx.x >> 6] = m;
@@ -360,12 +412,12 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
     if (far) {  // relative to the largest; without any, only a NaN counts
         Mass f = {most, 0.0f, 0.0f, 0.0f};
         for (int v = v0 + (int)threadIdx.x; v < v1; v += THREADS) {
-            float x[8];
-            r.get(v, x);
+            Eight<E> x;
+            r.get(v, true, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool none = x[e] == -__builtin_inff();
-                const float d = none ? NO_MASS : (x[e] - most) * p.c, power = __builtin_amdgcn_exp2f(d);
+                const bool none = x.get(e) == -__builtin_inff();
+                const float d = none ? NO_MASS : (x.get(e) - most) * p.c, power = __builtin_amdgcn_exp2f(d);
                 f.sum += power;
                 f.weighted = __builtin_fmaf(power, fmaxf(d, NO_MASS), f.weighted);
             }
@@ -383,7 +435,6 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
         }
     }
     if (threadIdx.x >= 64) return;
-    const int lane = threadIdx.x;
     Key best = 0;
     if constexpr (TOP) {
         // The `top` pieces with the largest scores hold the `top` largest scores (ties: the lower piece has the lower places)
@@ -490,17 +541,17 @@ __global__ __launch_bounds__(256) void token_gradient_kernel(const ScoreGradPara
     };
     const int v0 = chunk * (GRAD_CHUNK / 8) + (int)threadIdx.x;
     if constexpr (VEC) {
-        float x[SCORE_UNROLL][8];
+        Eight<E> x[SCORE_UNROLL];
 #pragma unroll
         for (int u = 0; u < SCORE_UNROLL; ++u)
-            if (v0 + u * 256 < (r.end + 7) / 8) r.get(v0 + u * 256, x[u]);
+            if (v0 + u * 256 < (r.end + 7) / 8) r.get(v0 + u * 256, true, x[u]);
 #pragma unroll
         for (int u = 0; u < SCORE_UNROLL; ++u) {
             const int v = v0 + u * 256;
             if (v >= (r.end + 7) / 8) break;
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = value(x[u][e], v * 8 + e);
+            for (int e = 0; e < 8; ++e) y[e] = value(x[u].get(e), v * 8 + e);
             if (r.whole(v)) {
                 put8<O>(out + (int64_t)v * 8, y);
             } else {
