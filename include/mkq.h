@@ -560,7 +560,8 @@ int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int gr
  *   workspace   at least the *_workspace_bytes bytes, 16-byte aligned; no preparation.  Two calls that may run at the same time need two
  * Products are exact, all sums and hidden are binary32 (sums of products with 16-bit results may leave out 2^-16 of a product); equal calls give
  * equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
- * rank 1 .. 256, R up to about 4e6, rank K and rank N below 2^29, K, N and the strides of base, out, dx_base and dx up to 2^25 (UNSUPPORTED).  M == 0: the first does nothing, the second writes its zeros.
+ * rank 1 .. 256, R up to about 4e6, rank K and rank N below 2^29, K and N from 8 and, as
+ * the strides of base, out, dx_base and dx, up to 2^25 (UNSUPPORTED).  M == 0: the first does nothing, the second writes its zeros.
  * Errors: NULL, SHAPE (x_group too), ALIGN, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
 size_t mkq_low_rank_adapters_workspace_bytes(int64_t M, int64_t K, int64_t N, int rank, int64_t R);
 int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, const int32_t *adapter, int64_t M, int64_t K, int64_t N, int rank, int64_t R,

@@ -185,15 +185,13 @@ struct ShrinkParams {
     int64_t ldx;
     int K;
     int slots;          // workgroups that share a tile's adapters
-    int rank_chunks, per_split;  // steps of 64 places of a split
+    int rank_chunks;
     bool scaled;        // times the adapter's scale
     float *t;           // [splits, M, pitch], zeros behind the rank
     float *hidden;      // [M, rank], or NULL: the same
     int plans;          // workgroups in front that put the rows in order
     PlanParams plan;
 };
-constexpr int SHRINK_STEP = 64;
-
 template <class E>
 __device__ __forceinline__ void operand(const Neighbours<E> &n, uint4 (&out)[Parts<E>::N])
 {
@@ -207,14 +205,53 @@ __device__ __forceinline__ void operand(const Neighbours<E> &n, uint4 (&out)[Par
     }
 }
 
-// Tiles of 16 rows and RT * 16 of the rank; the four waves of a workgroup take steps in turn, and UNROLL at a time, and add up through LDS
+// Places of a row that a wave multiplies at a time: 256 bytes of the larger elements
+constexpr int shrink_step(int x_bytes, int w_bytes) { return x_bytes == 4 || w_bytes == 4 ? 64 : 128; }
+
+// Sixteen rows of a step on their way from memory to LDS: neighbouring lanes fetch neighbouring pieces of 16 bytes of a row.  (Fetched as
+// the matrix unit takes them, a row a lane, every lane asked for a line of its own: dy of 8192 x 4096 bfloat16 32 us.)  In LDS piece i of row r is
+// at i ^ r, so that sixteen rows' same pieces, and a row's sixteen pieces, are on different banks.
+template <class E, int STEP>
+struct ShrinkRows {
+    static constexpr int PIECES = STEP * E::BYTES / 16, N = PIECES / 4;  // of a row, of a lane
+    static constexpr int BYTES = 16 * STEP * E::BYTES;
+    u32x4 v[N];
+    __device__ static __forceinline__ int row_of(int i) { return (64 * i + (int)(threadIdx.x & 63)) / PIECES; }
+    __device__ static __forceinline__ int piece_of() { return (threadIdx.x & 63) % PIECES; }
+    __device__ __forceinline__ void put(uint8_t *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = row_of(i);
+            *reinterpret_cast<u32x4 *>(lds + (r * PIECES + (piece_of() ^ (r % PIECES))) * 16) = v[i];
+        }
+    }
+    // lane (c, q): eight places from 32 h + 8 q on of row c
+    __device__ static __forceinline__ Neighbours<E> get(const uint8_t *lds, int h)
+    {
+        const int c = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
+        Neighbours<E> n;
+#pragma unroll
+        for (int i = 0; i < E::BYTES / 2; ++i) {
+            const int piece = (4 * h + q) * (E::BYTES / 2) + i;
+            n.w[i] = *reinterpret_cast<const u32x4 *>(lds + (c * PIECES + (piece ^ (c % PIECES))) * 16);
+        }
+        return n;
+    }
+};
+
+// Tiles of 16 rows and RT * 16 of the rank; the four waves of a workgroup take steps in turn and add up through LDS
 template <class X, class W, int RT>
 __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
 {
-    constexpr int UNROLL = RT * (X::BYTES + W::BYTES) <= 4 ? 4 : RT * (X::BYTES + W::BYTES) <= 8 ? 2 : 1;
-    __shared__ v4f sums[4][RT][64];
+    constexpr int STEP = shrink_step(X::BYTES, W::BYTES);
+    using XRows = ShrinkRows<X, STEP>;
+    using WRows = ShrinkRows<W, STEP>;
+    constexpr int LDS = XRows::BYTES + RT * WRows::BYTES;  // of a wave; the sums have room in it
+    static_assert(LDS >= RT * 64 * 16, "sums");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * LDS];
     if (blockIdx.x < (unsigned)p.plans) return plan(p.a, p.plan, blockIdx.x);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
     unsigned b = blockIdx.x - p.plans;
     const int chunk = b % p.rank_chunks;
     b /= p.rank_chunks;
@@ -223,13 +260,17 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
     const int slot = b % p.slots;
     const int64_t m0 = (int64_t)(b / p.slots) * 16;
     const int mine = adapter_of(p.a, lane < 16 ? m0 + lane : p.a.M);
-    const int64_t row = m0 + c < p.a.M ? m0 + c : p.a.M - 1;
-    const typename X::raw *x = static_cast<const typename X::raw *>(p.x) + row * p.ldx;
-    const int steps = (p.K + SHRINK_STEP - 1) / SHRINK_STEP;
-    const int from = split * p.per_split, to = from + p.per_split < steps ? from + p.per_split : steps;
-    // rows a power of two apart that all began at the same place would ask the same memory channels: tiles begin at places of their own
-    const int turn = from < to ? (int)((m0 / 16) % (unsigned)(to - from)) : 0;
+    const int steps = (p.K + STEP - 1) / STEP, per_split = (steps + p.a.splits - 1) / p.a.splits;
+    const int from = split * per_split, to = from + per_split < steps ? from + per_split : steps;
     float *t = p.t + (int64_t)split * p.a.M * p.a.pitch;
+    uint8_t *lds_x = lds + wave * LDS, *lds_w = lds_x + XRows::BYTES;
+    v4f *sums = reinterpret_cast<v4f *>(lds);
+    const typename X::raw *x[XRows::N];
+#pragma unroll
+    for (int i = 0; i < XRows::N; ++i) {
+        const int64_t row = m0 + XRows::row_of(i);
+        x[i] = static_cast<const typename X::raw *>(p.x) + (row < p.a.M ? row : p.a.M - 1) * p.ldx;
+    }
     Adapters adapters(mine, slot, p.slots, lane < 16 && m0 + lane < p.a.M && mine < 0);
     int a;
     uint64_t same;
@@ -244,58 +285,58 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
             continue;
         }
         v4f acc[RT];
-        const typename W::raw *w[RT];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const int at = (chunk * RT + r) * 16 + c;
-            acc[r] = v4f{0, 0, 0, 0};
-            w[r] = static_cast<const typename W::raw *>(p.w) + ((int64_t)a * p.a.rank + (at < p.a.rank ? at : p.a.rank - 1)) * p.K;
-        }
-        auto take = [&](auto n, int s) {
-            constexpr int N = decltype(n)::value;
-            Neighbours<X> xs[N][2];
-            Neighbours<W> ws[N][2][RT];
+        for (int r = 0; r < RT; ++r) acc[r] = v4f{0, 0, 0, 0};
+        const typename W::raw *w = static_cast<const typename W::raw *>(p.w) + (int64_t)a * p.a.rank * p.K;
+        XRows xs;
+        WRows ws[RT];
+        auto fetch = [&](int s) {
+            const bool edge = (s + 1) * STEP > p.K;
 #pragma unroll
-            for (int u = 0; u < N; ++u)
+            for (int i = 0; i < XRows::N; ++i) xs.v[i] = fetch16<X, false>(x[i], 0, s * STEP + XRows::piece_of() * (16 / X::BYTES), p.K, edge);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    int step = s + 4 * u + turn;
-                    step -= step >= to ? to - from : 0;
-                    const bool edge = (step + 1) * SHRINK_STEP > p.K;
-                    const int k = step * SHRINK_STEP + h * 32 + q * 8;
-                    xs[u][h].fetch(x, k, p.K, edge);
+            for (int r = 0; r < RT; ++r)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) ws[u][h][r].fetch(w[r], k, p.K, edge);
-                }
-#pragma unroll
-            for (int u = 0; u < N; ++u)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if constexpr (std::is_same<X, ElemF16>::value && std::is_same<W, ElemF16>::value) {
-#pragma unroll
-                        for (int r = 0; r < RT; ++r)
-                            acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, xs[u][h].w[0]), __builtin_bit_cast(v8h, ws[u][h][r].w[0]), acc[r], 0, 0, 0);
-                    } else {
-                        uint4 xp[Parts<X>::N], wp[Parts<W>::N];
-                        operand(xs[u][h], xp);
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            operand(ws[u][h][r], wp);
-                            acc[r] = multiply<3>(xp, wp, acc[r]);
-                        }
-                    }
+                for (int i = 0; i < WRows::N; ++i) {
+                    const int at = (chunk * RT + r) * 16 + WRows::row_of(i);
+                    ws[r].v[i] = fetch16<W, false>(w, (uint32_t)(at < p.a.rank ? at : p.a.rank - 1) * ((uint32_t)p.K * W::BYTES),
+                                            s * STEP + WRows::piece_of() * (16 / W::BYTES), p.K, edge);
                 }
         };
-        int s = from + wave;
-        if constexpr (UNROLL > 1)
-            for (; s + 4 * (UNROLL - 1) < to; s += 4 * UNROLL) take(IntC<UNROLL>(), s);
-        for (; s < to; s += 4) take(IntC<1>(), s);
+        if (from + wave < to) fetch(from + wave);
+        for (int s = from + wave; s < to; s += 4) {
+            xs.put(lds_x);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) sums[wave][r][lane] = acc[r];
+            for (int r = 0; r < RT; ++r) ws[r].put(lds_w + r * WRows::BYTES);
+            if (s + 4 < to) fetch(s + 4);
+            wave_order();
+#pragma unroll
+            for (int h = 0; h < STEP / 32; ++h) {
+                const Neighbours<X> xn = XRows::get(lds_x, h);
+                if constexpr (std::is_same<X, ElemF16>::value && std::is_same<W, ElemF16>::value) {
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, xn.w[0]),
+                                                                        __builtin_bit_cast(v8h, WRows::get(lds_w + r * WRows::BYTES, h).w[0]), acc[r], 0, 0, 0);
+                } else {
+                    uint4 xp[Parts<X>::N], wp[Parts<W>::N];
+                    operand(xn, xp);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        operand(WRows::get(lds_w + r * WRows::BYTES, h), wp);
+                        acc[r] = multiply<3>(xp, wp, acc[r]);
+                    }
+                }
+            }
+            wave_order();
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RT; ++r) sums[(wave * RT + r) * 64 + lane] = acc[r];
         __syncthreads();
         const float scale = p.scaled ? scale_of(p.a, a) : 1.0f;
         for (int r = wave; r < RT; r += 4) {
-            const v4f sum = (sums[0][r][lane] + sums[1][r][lane]) + (sums[2][r][lane] + sums[3][r][lane]);
+            const v4f sum = (sums[r * 64 + lane] + sums[(RT + r) * 64 + lane]) + (sums[(2 * RT + r) * 64 + lane] + sums[(3 * RT + r) * 64 + lane]);
             const int at = (chunk * RT + r) * 16 + c;
 #pragma unroll
             for (int v = 0; v < 4; ++v)
@@ -368,18 +409,21 @@ __device__ __forceinline__ void hidden_values(const ExpandParams &p, const float
         for (int e = 0; e < 8; ++e) v[e] = 0.0f;
 }
 
-// A wave has 128 columns of `tiles` tiles of 16 rows; lane (c, q) has columns 8 c .. 8 c + 7 of rows 4 q .. 4 q + 3.  The adapter's rows are fetched
-// again for every tile (from the caches), 32 at a time.
-template <class W, class O>
+// A wave has 128 columns of `tiles` tiles of 16 rows; lane (c, q) has columns 8 c .. 8 c + 7 of rows 4 q .. 4 q + 3.  KEEP: the adapter's rows are
+// kept as operands in LDS while the adapter is the same, otherwise they are fetched again for every tile (from the caches), 32 at a time.
+template <class W, class O, bool KEEP>
 __global__ __launch_bounds__(256, 2) void expand_kernel(const ExpandParams p)
 {
-    constexpr int PT = O::BYTES == 4 ? 3 : 2;  // (2^-16 of a product is left out under results of 16 bits, which end at 2^-9 or 2^-12)
+    constexpr int PW = Parts<W>::N, PT = O::BYTES == 4 ? 3 : 2;  // (2^-16 of a product is left out under results of 16 bits, which end at 2^-9 or 2^-12)
     const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = (int)(task % p.column_blocks);
     const int64_t rest = task / p.column_blocks;
     const int slot = (int)(rest / p.row_groups), group = (int)(rest - (int64_t)slot * p.row_groups);
     if (slot >= p.slots) return;
     const bool edge = block * 128 + 128 > p.N;
+    extern __shared__ uint4 operands[];
+    uint4 *kept = operands + (KEEP ? (threadIdx.x >> 6) * ((p.a.rank + 31) / 32 * 8 * PW * 64) + (threadIdx.x & 63) : 0);
+    int have = -1;
     const int64_t first = (int64_t)group * p.tiles * 16;
     // at most four tiles: a row of theirs a lane
     const int all = adapter_of(p.a, (int)(threadIdx.x & 63) < 16 * p.tiles ? first + (threadIdx.x & 63) : p.a.M);
@@ -421,12 +465,30 @@ __global__ __launch_bounds__(256, 2) void expand_kernel(const ExpandParams p)
             } else {
                 const float scale = scale_of(p.a, a), factor = p.scaled ? scale : 1.0f;
                 const typename W::raw *w = static_cast<const typename W::raw *>(p.w) + (int64_t)a * p.a.rank * p.N;
-                for (int r0 = 0; r0 < p.a.rank; r0 += 32) {
+                auto fetch = [&](Block<W> &rows, int r0) {  // (behind the rank its last row again: t is 0 there)
                     const int r = r0 + 8 * q;
-                    Block<W> rows;  // (behind the rank its last row again: t is 0 there)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         rows.rows[e].fetch(w, (uint32_t)(r + e < p.a.rank ? r + e : p.a.rank - 1) * ((uint32_t)p.N * W::BYTES), n0, p.N, edge);
+                };
+                if (KEEP && a != have) {
+                    for (int r0 = 0; r0 < p.a.rank; r0 += 32) {
+                        Block<W> rows;
+                        fetch(rows, r0);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint4 wp[PW];
+                            rows.column(i, wp);
+#pragma unroll
+                            for (int k = 0; k < PW; ++k) kept[((r0 / 32 * 8 + i) * PW + k) * 64] = wp[k];
+                        }
+                    }
+                    have = a;
+                }
+                for (int r0 = 0; r0 < p.a.rank; r0 += 32) {
+                    const int r = r0 + 8 * q;
+                    Block<W> rows;
+                    if (!KEEP) fetch(rows, r0);
                     uint4 tp[PT];
                     float v[8];
                     hidden_values(p, t, c < last_row ? c : last_row, r, v);
@@ -440,8 +502,13 @@ __global__ __launch_bounds__(256, 2) void expand_kernel(const ExpandParams p)
                     parts_of(v, tp);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        uint4 wp[Parts<W>::N];
-                        rows.column(i, wp);
+                        uint4 wp[PW];
+                        if constexpr (KEEP) {
+#pragma unroll
+                            for (int k = 0; k < PW; ++k) wp[k] = kept[((r0 / 32 * 8 + i) * PW + k) * 64];
+                        } else {
+                            rows.column(i, wp);
+                        }
                         acc[i] = multiply<PT>(tp, wp, acc[i]);
                     }
                 }
@@ -655,7 +722,7 @@ static int check_shape(const AdapterShape &d)
 {
     if (d.M < 0 || d.K <= 0 || d.N <= 0 || d.R <= 0 || d.rank <= 0) return MKQ_ERR_SHAPE;
     if (d.M > SIDES_MOST || d.K > SIDES_MOST || d.N > SIDES_MOST || d.R > ADAPTERS_MOST || d.rank > RANK_MOST || d.K * d.rank >= (int64_t)1 << 29 || d.N * d.rank >= (int64_t)1 << 29 ||
-        d.K > STRIDE_MOST || d.N > STRIDE_MOST)
+        d.K > STRIDE_MOST || d.N > STRIDE_MOST || d.K < 8 || d.N < 8)
         return MKQ_ERR_UNSUPPORTED;
     return MKQ_OK;
 }
@@ -666,7 +733,7 @@ static int rank_tiles(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : 4; }
 // Workgroups that share the places of a row: about 512 of them in all, four steps each at least
 static int splits_of(const AdapterShape &d, int64_t side)
 {
-    const int64_t steps = ceil_div(side, SHRINK_STEP), groups = ceil_div(d.M, 16) * slots_of(d) * ceil_div(d.rank, 16 * rank_tiles(d.rank));
+    const int64_t steps = ceil_div(side, 64), groups = ceil_div(d.M, 16) * slots_of(d) * ceil_div(d.rank, 16 * rank_tiles(d.rank));
     int64_t n = groups == 0 || groups >= 512 ? 1 : 512 / groups;
     if (n > ceil_div(steps, 4)) n = ceil_div(steps, 4);
     if (n > 16) n = 16;
@@ -692,7 +759,6 @@ static ShrinkParams shrink_params(const AdapterShape &d, const AdapterParams &a,
     p.K = (int)side;
     p.slots = slots_of(d);
     p.rank_chunks = (int)ceil_div(d.rank, 16 * rank_tiles(d.rank));
-    p.per_split = (int)ceil_div(ceil_div(side, SHRINK_STEP), a.splits);
     p.scaled = scaled;
     p.t = t;
     p.hidden = hidden;
@@ -722,7 +788,11 @@ static int launch_expand(const AdapterShape &d, ExpandParams p, int w_dtype, int
     if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
     with_elem(w_dtype, [&](auto w) {
         with_elem(out_dtype, [&](auto o) {
-            expand_kernel<decltype(w), decltype(o)><<<(unsigned)workgroups, 256, 0, st>>>(p);
+            using W = decltype(w);
+            using O = decltype(o);
+            const int blocks = (int)ceil_div(d.rank, 32) * Parts<W>::N;  // of 8 KiB a wave
+            if (p.tiles > 1 && blocks <= 2) expand_kernel<W, O, true><<<(unsigned)workgroups, 256, blocks * 4 * 8192, st>>>(p);
+            else expand_kernel<W, O, false><<<(unsigned)workgroups, 256, 0, st>>>(p);
         });
     });
     return launch_status();

@@ -66,7 +66,7 @@ __device__ __forceinline__ uint2 codes_by_division(const float (&x)[8], float st
 // Binary32 values: fma(x, 1 / step, 128) is off by less than 5e-5 (its own rounding 2^-17, two of the quotient's 2^-24 times 127); where it
 // lies nearer than that to a boundary the eight are divided.
 template <class E>
-__device__ __forceinline__ uint2 checkpoint_codes(const Neighbours<E> &n, float step, float)
+__device__ __forceinline__ uint2 checkpoint_codes(const Neighbours<E, true> &n, float step, float)
 {
     float x[8];
 #pragma unroll
@@ -90,7 +90,7 @@ __device__ __forceinline__ uint2 checkpoint_codes(const Neighbours<E> &n, float 
 // factor 1 / step moved by 3e-7 against it rounds all values as they have to be (its own roundings are 1.2e-7), in one fused
 // addition of 1.5 * 2^23, which leaves the code in the low byte.  Steps that are exact, or not the quotient, divide.
 template <class E>
-__device__ __forceinline__ uint2 checkpoint_codes_16(const Neighbours<E> &n, float step, float most)
+__device__ __forceinline__ uint2 checkpoint_codes_16(const Neighbours<E, true> &n, float step, float most)
 {
     const float off = __builtin_fmaf(step, 127.0f, -most);  // the step's rounding, with its sign
     if (__builtin_expect(off == 0.0f || step <= 0x1p-126f || step >= STEP_MOST || most == 0.0f, 0)) {
@@ -111,7 +111,7 @@ __device__ __forceinline__ uint2 checkpoint_codes_16(const Neighbours<E> &n, flo
 
 // The largest |x| of eight as bits: those of infinities and NaN are above all others'
 template <class E>
-__device__ __forceinline__ uint32_t largest_bits(const Neighbours<E> &n)
+__device__ __forceinline__ uint32_t largest_bits(const Neighbours<E, true> &n)
 {
     uint32_t most = 0;
     if constexpr (E::BYTES == 4) {
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256) void checkpoint_kernel(const CheckpointParams 
 {
     const int64_t first = (int64_t)blockIdx.x * (256 * CHECKPOINT_UNROLL), row0 = first / p.chunks;
     const uint32_t chunk0 = (uint32_t)(first - row0 * p.chunks) + threadIdx.x;
-    Neighbours<E> x[CHECKPOINT_UNROLL];
+    Neighbours<E, true> x[CHECKPOINT_UNROLL];
 #pragma unroll
     for (int u = 0; u < CHECKPOINT_UNROLL; ++u) {
         const ChunkAt at(p, row0, chunk0, u);
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256) void checkpoint_use_kernel(const CheckpointPar
     const uint32_t chunk0 = (uint32_t)(first - row0 * p.chunks) + threadIdx.x;
     uint2 codes[CHECKPOINT_UNROLL];
     float step[CHECKPOINT_UNROLL];
-    Neighbours<D> dy[CHECKPOINT_UNROLL];
+    Neighbours<D, true> dy[CHECKPOINT_UNROLL];
 #pragma unroll
     for (int u = 0; u < CHECKPOINT_UNROLL; ++u) {
         const ChunkAt at(p, row0, chunk0, u);

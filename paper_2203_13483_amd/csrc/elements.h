@@ -27,6 +27,13 @@ struct ElemBF16 {
     __device__ static __forceinline__ raw put(float v) { return float_to_bf16_bits(v); }
 };
 
+// What lanes of a wave wrote to LDS before is there for its other lanes behind: a wave's accesses are done in their order
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A product rounded to binary32, also where it is narrowed next: the compiler would fuse a single value's product with its rounding
 // to 16 bits, but not those of a vector, and the same value would come out differently by where it lies.
 __device__ __forceinline__ float product(float a, float b)

@@ -16,10 +16,46 @@ struct Codes {  // rows kept in 8 bits
     static constexpr int BYTES = 1;
 };
 
-// Eight neighbours of a row from place k on, as fetched.  Whole vectors only, and no branch that lanes of a wave take apart: where the row
-// ends among a wave's places (`edge`), its last eight elements are fetched instead and moved down, zeros behind them.  A row of fewer than
-// eight is fetched one by one.  (Rows kept in 8 bits have zeros behind them.)
-template <class E>
+// Sixteen bytes without their first n elements, zeros behind them
+template <int BYTES>
+__device__ __forceinline__ u32x4 without_first(u32x4 v, int n)
+{
+    if constexpr (BYTES == 2) {
+        if (n & 1)
+            v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16), v[3] >> 16};
+        n >>= 1;
+    }
+    if (n & 1) v = u32x4{v[1], v[2], v[3], 0};
+    if (n & 2) v = u32x4{v[2], v[3], 0, 0};
+    return n >= 4 ? u32x4{0, 0, 0, 0} : v;
+}
+// The elements of sixteen bytes of a row from place k on, zeros from place `end` on.  Whole vectors only, and no branch that lanes of a wave take
+// apart: where the row ends among a wave's places (`edge`), its last sixteen bytes are fetched instead and moved down.  SHORT: rows may have fewer,
+// which are fetched one by one.  place: the bytes of the row, or a place that all lanes share with `off` bytes to a lane's row
+template <class E, bool SHORT>
+__device__ __forceinline__ u32x4 fetch16(const void *place, uint32_t off, int k, int end, bool edge)
+{
+    constexpr int N = 16 / E::BYTES;
+    const uint8_t *row = static_cast<const uint8_t *>(place);
+    if (SHORT && end < N) {
+        u32x4 v = {0, 0, 0, 0};
+        if (k != 0) return v;
+#pragma unroll
+        for (int i = 0; i < N - 1; ++i)
+            if (i < end) {
+                const typename E::raw x = *reinterpret_cast<const typename E::raw *>(row + (off + i * E::BYTES));
+                if constexpr (E::BYTES == 4) v[i] = __float_as_uint(x);
+                else v[i / 2] |= (uint32_t)x << (16 * (i % 2));
+            }
+        return v;
+    }
+    const int from = edge && k + N > end ? end - N : k;
+    const u32x4 v = reinterpret_cast<const Loose<E::BYTES> *>(row + (off + (uint32_t)from * E::BYTES))->v;
+    return edge ? without_first<E::BYTES>(v, k - from < N ? k - from : N) : v;
+}
+
+// Eight neighbours of a row from place k on.  (Rows kept in 8 bits have zeros behind them.)
+template <class E, bool SHORT = false>
 struct Neighbours {
     u32x4 w[E::BYTES == 4 ? 2 : 1];
     __device__ __forceinline__ void clear()
@@ -27,60 +63,17 @@ struct Neighbours {
         w[0] = u32x4{0, 0, 0, 0};
         if constexpr (E::BYTES == 4) w[1] = u32x4{0, 0, 0, 0};
     }
-    __device__ __forceinline__ void without_first(int n)
-    {
-        if constexpr (E::BYTES == 2) {
-            u32x4 &v = w[0];
-            if (n & 1)
-                v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16), v[3] >> 16};
-            if (n & 2) v = u32x4{v[1], v[2], v[3], 0};
-            if (n & 4) v = u32x4{v[2], v[3], 0, 0};
-            if (n >= 8) v = u32x4{0, 0, 0, 0};
-        } else {
-            u32x4 &v = w[0], &x = w[E::BYTES / 4];
-            if (n & 1) {
-                v = u32x4{v[1], v[2], v[3], x[0]};
-                x = u32x4{x[1], x[2], x[3], 0};
-            }
-            if (n & 2) {
-                v = u32x4{v[2], v[3], x[0], x[1]};
-                x = u32x4{x[2], x[3], 0, 0};
-            }
-            if (n >= 4) {
-                v = n >= 8 ? u32x4{0, 0, 0, 0} : x;
-                x = u32x4{0, 0, 0, 0};
-            }
-        }
-    }
-    // `row`: the bytes of a row, or a place that all lanes share with `off` bytes to a lane's row
     __device__ __forceinline__ void fetch(const void *row, int k, int end, bool edge) { fetch(row, 0u, k, end, edge); }
     __device__ __forceinline__ void fetch(const void *place, uint32_t off, int k, int end, bool edge)
     {
-        const uint8_t *row = static_cast<const uint8_t *>(place);
         if constexpr (E::BYTES == 1) {
             if (edge) k = k < end ? k : (end - 1) & ~7;
-            const uint2 v = *reinterpret_cast<const uint2 *>(row + (off + (uint32_t)k));
+            const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(place) + (off + (uint32_t)k));
             w[0] = u32x4{v.x, v.y, 0, 0};
         } else {
-            if (end < 8) return fetch_short(row, off, k, end);
-            const int from = edge && k + 8 > end ? end - 8 : k;
-            const uint8_t *at = row + (off + (uint32_t)from * E::BYTES);
-            w[0] = reinterpret_cast<const Loose<E::BYTES> *>(at)->v;
-            if constexpr (E::BYTES == 4) w[1] = reinterpret_cast<const Loose<4> *>(at + 16)->v;
-            if (edge) without_first(k - from < 8 ? k - from : 8);
+            w[0] = fetch16<E, SHORT>(place, off, k, end, edge);
+            if constexpr (E::BYTES == 4) w[1] = fetch16<E, SHORT>(place, off, k + 4, end, edge);
         }
-    }
-    __device__ __forceinline__ void fetch_short(const uint8_t *row, uint32_t off, int k, int end)
-    {
-        clear();
-        if (k != 0) return;
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < end) {
-                const typename E::raw v = *reinterpret_cast<const typename E::raw *>(row + (off + i * E::BYTES));
-                if constexpr (E::BYTES == 4) w[i / 4][i % 4] = __float_as_uint(v);
-                else w[0][i / 2] |= (uint32_t)v << (16 * (i % 2));
-            }
     }
     __device__ __forceinline__ float get(int i) const
     {

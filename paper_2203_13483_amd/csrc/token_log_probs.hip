@@ -59,13 +59,6 @@ __device__ __forceinline__ int64_t given_token(const void *tokens, int bits, int
     return bits == 64 ? static_cast<const int64_t *>(tokens)[row] : (int64_t)static_cast<const int32_t *>(tokens)[row];
 }
 
-// What lanes of a wave wrote to LDS before is there for its other lanes behind: a wave's accesses are done in their order
-__device__ __forceinline__ void wave_order()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // ---- the order of scores --------------------------------------------------------------------------------------------------
 // A score and its place as one number: larger scores first, then lower places; -0 and 0 are equal, and a NaN is as low as -infinity.
 // 0 is none.

@@ -89,6 +89,7 @@ def test_adapter_refusals(lib):
     assert fwd(dt=mkq.MKQ_I8) == fwd(w=mkq.MKQ_I4) == fwd(odt=-1) == mkq.MKQ_ERR_DTYPE
     for bad in (dict(M=-1), dict(K=0), dict(N=0), dict(rank=0), dict(R=0), dict(ldx=63), dict(ldo=31), dict(base=P, ldb=31)):
         assert fwd(**bad) == mkq.MKQ_ERR_SHAPE, bad
+    assert fwd(K=7) == fwd(N=7) == fwd(ldo=2 ** 25 + 8) == fwd(base=P, ldb=2 ** 25 + 8) == mkq.MKQ_ERR_UNSUPPORTED
     assert fwd(rank=257) == fwd(R=2 ** 23) == fwd(M=2 ** 31) == fwd(K=2 ** 31, ldx=2 ** 31) == fwd(N=2 ** 31, ldo=2 ** 31) == mkq.MKQ_ERR_UNSUPPORTED
     assert fwd(x=None) == fwd(a=None) == fwd(down=None) == fwd(up=None) == fwd(out=None) == mkq.MKQ_ERR_NULL
     for bad in (dict(x=ODD), dict(a=VERY_ODD), dict(down=ODD), dict(up=ODD), dict(scales=VERY_ODD), dict(base=ODD), dict(out=ODD), dict(hidden=VERY_ODD), dict(ws=ODD)):
