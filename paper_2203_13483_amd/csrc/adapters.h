@@ -108,19 +108,18 @@ struct PlanParams {
 };
 __device__ __forceinline__ int task_of(int start, int a, int piece) { return start / piece + a; }
 
-// Blocks of 128 columns, four neighbours of a `row` of blocks a workgroup, and the rows in turn to the eight XCDs, whole.  (Workgroups go to the XCDs in
-// turn: with a row's eight workgroups side by side, each XCD had the same columns of every row, 1 KiB of 8, which only four of the 16
-// channels of its L2 hold: base and out of 8192 x 4096 bfloat16 76 instead of EXPAND_US us.)
+// Blocks of 128 columns, four neighbours of a `row` of blocks a workgroup.  (Whole rows to the XCDs in turn took as long: 8192 x 4096 bfloat16 with its
+// base 30.3 and 30.3 us.)
 struct ColumnTask {
     int64_t row;
     int block;
     __device__ __forceinline__ ColumnTask(unsigned workgroup, int column_blocks, int wave)
     {
-        const unsigned parts = (unsigned)(column_blocks + 3) / 4, eight = workgroup / (8 * parts), in = workgroup - eight * 8 * parts;
-        row = (int64_t)eight * 8 + in % 8;
-        block = (int)(in / 8) * 4 + wave;
+        const unsigned parts = (unsigned)(column_blocks + 3) / 4;
+        row = workgroup / parts;
+        block = (int)(workgroup % parts) * 4 + wave;
     }
-    static int64_t workgroups(int64_t rows, int64_t column_blocks) { return (rows + 7) / 8 * 8 * ((column_blocks + 3) / 4); }
+    static int64_t workgroups(int64_t rows, int64_t column_blocks) { return rows * ((column_blocks + 3) / 4); }
 };
 
 // ---- what the kernels take ------------------------------------------------------------------------------------------------

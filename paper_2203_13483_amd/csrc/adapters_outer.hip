@@ -108,13 +108,27 @@ __device__ __forceinline__ void outer(const OuterParams &p, const OuterSide &sid
                 *reinterpret_cast<v4f *>(tile + (4 * q + v) * 128 + 8 * c + i) = v4f{acc[r][i][v], acc[r][i + 1][v], acc[r][i + 2][v], acc[r][i + 3][v]};
         wave_order();
         const int at = (chunk * RT + r) * 16, rows = p.a.rank - at < 16 ? p.a.rank - at : 16;
-        for (int row = 0; row < rows; ++row)
-            for (int i = lane; i < columns; i += 64) {
-                const int64_t to = (int64_t)(at + row) * side.N + block * 128 + i;
-                const float value = tile[row * 128 + i];
-                if (pieces > 1) side.partials[(int64_t)part * p.a.rank * side.N + to] = value;
-                else write_grad(p, side, a, to, value);
+        const int64_t corner = (int64_t)at * side.N + block * 128;
+        if (pieces > 1) {
+            float *to = side.partials + (int64_t)part * p.a.rank * side.N + corner;
+            const int i = lane % 32 * 4;
+#pragma unroll
+            for (int two = 0; two < 8; ++two) {
+                const int row = 2 * two + lane / 32;
+                const v4f v = *reinterpret_cast<const v4f *>(tile + row * 128 + i);
+                if (row >= rows) continue;
+                if (i + 4 <= columns) {
+                    reinterpret_cast<Loose<4> *>(to + (int64_t)row * side.N + i)->v = __builtin_bit_cast(u32x4, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (i + e < columns) to[(int64_t)row * side.N + i + e] = v[e];
+                }
             }
+        } else {
+            for (int row = 0; row < rows; ++row)
+                for (int i = lane; i < columns; i += 64) write_grad(p, side, a, corner + (int64_t)row * side.N + i, tile[row * 128 + i]);
+        }
     }
 }
 
