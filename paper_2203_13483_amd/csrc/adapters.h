@@ -111,12 +111,11 @@ __device__ __forceinline__ int task_of(int start, int a, int piece) { return sta
 // Blocks of 128 columns, four neighbours of a `row` of blocks a workgroup.  (Whole rows to the XCDs in turn took as long: 8192 x 4096 bfloat16 with its
 // base 30.3 and 30.3 us.)
 struct ColumnTask {
-    int64_t row;
-    int block;
+    int row, block;
     __device__ __forceinline__ ColumnTask(unsigned workgroup, int column_blocks, int wave)
     {
         const unsigned parts = (unsigned)(column_blocks + 3) / 4;
-        row = workgroup / parts;
+        row = (int)(workgroup / parts);  // (a grid has fewer than 2^24 workgroups)
         block = (int)(workgroup % parts) * 4 + wave;
     }
     static int64_t workgroups(int64_t rows, int64_t column_blocks) { return rows * ((column_blocks + 3) / 4); }

@@ -99,9 +99,9 @@ template <class W, class O, bool ONE>
 __global__ __launch_bounds__(256, W::BYTES == 4 || O::BYTES == 4 || !ONE ? 2 : 4) void expand_kernel(const ExpandParams p)
 {
     const ColumnTask task(blockIdx.x, p.column_blocks, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-    const int slot = (int)(task.row / p.row_groups), block = task.block;
+    const int slot = task.row / p.row_groups, block = task.block;
     if (slot >= p.slots || block >= p.column_blocks) return;
-    const int64_t m0 = (task.row - (int64_t)slot * p.row_groups) * 16;
+    const int64_t m0 = (int64_t)(task.row - slot * p.row_groups) * 16;
     if (block * 128 + 128 > p.N) expand<W, O, ONE>(p, m0, block, slot, std::true_type());
     else expand<W, O, ONE>(p, m0, block, slot, std::false_type());
 }

@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256, (X::BYTES < 4 && D::BYTES < 4 ? 4 : 3) - RT) v
     float *tile = tiles[threadIdx.x >> 6];
     const int blocks = p.side[0].column_blocks + p.side[1].column_blocks;
     const ColumnTask at(blockIdx.x, blocks, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-    const int block = at.block, chunk = (int)(at.row % p.rank_chunks), task = (int)(at.row / p.rank_chunks);
+    const int block = at.block, chunk = at.row % p.rank_chunks, task = at.row / p.rank_chunks;
     if (task >= p.plan.tasks_most || block >= blocks) return;
     const int4 what = p.plan.tasks[task];
     const int a = __builtin_amdgcn_readfirstlane(what.x), first = __builtin_amdgcn_readfirstlane(what.y), last = __builtin_amdgcn_readfirstlane(what.z);

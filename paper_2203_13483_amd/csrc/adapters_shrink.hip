@@ -143,6 +143,21 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
         const int64_t row = m0 + XRows::row_of(i);
         x[i] = static_cast<const typename X::raw *>(p.x) + (row < p.a.M ? row : p.a.M - 1) * p.ldx;
     }
+    // Tiles of an XCD begin at steps of their own: rows a power of two apart would all ask the same memory channels at a time
+    const int n = to - from, turn = n > 0 ? (int)((m0 / 128 * 4) % n) : 0;
+    auto step = [&](int i) { return from + (i + turn < n ? i + turn : i + turn - n); };
+    XRows xs;
+    auto fetch_x = [&](int s) __attribute__((always_inline)) {
+        auto each = [&](auto edge) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < XRows::N; ++i) xs.v[i] = fetch16<X, false>(x[i], 0, s * STEP + XRows::piece_of() * (16 / X::BYTES), p.K, edge);
+        };
+        if ((s + 1) * STEP > p.K) each(std::true_type());
+        else each(std::false_type());
+    };
+    // the first of x do not wait for the rows' adapters
+    bool ahead = wave < n;
+    if (ahead) fetch_x(step(wave));
     Adapters adapters(mine, slot, p.slots, lane < 16 && m0 + lane < p.a.M && mine < 0);
     int a;
     uint64_t same;
@@ -160,33 +175,34 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[r] = v4f{0, 0, 0, 0};
         const typename W::raw *w = static_cast<const typename W::raw *>(p.w) + (int64_t)a * p.a.rank * p.K;
-        XRows xs;
         WRows ws[RT];
-        auto fetch_step = [&](int s, auto edge) __attribute__((always_inline)) {
+        auto fetch_w = [&](int s) __attribute__((always_inline)) {
+            auto each = [&](auto edge) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < XRows::N; ++i) xs.v[i] = fetch16<X, false>(x[i], 0, s * STEP + XRows::piece_of() * (16 / X::BYTES), p.K, edge);
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int i = 0; i < WRows::N; ++i) {
-                    const int at = (chunk * RT + r) * 16 + WRows::row_of(i);
-                    ws[r].v[i] = fetch16<W, false>(w, (uint32_t)(at < p.a.rank ? at : p.a.rank - 1) * ((uint32_t)p.K * W::BYTES),
-                                            s * STEP + WRows::piece_of() * (16 / W::BYTES), p.K, edge);
-                }
+                    for (int i = 0; i < WRows::N; ++i) {
+                        const int at = (chunk * RT + r) * 16 + WRows::row_of(i);
+                        ws[r].v[i] = fetch16<W, false>(w, (uint32_t)(at < p.a.rank ? at : p.a.rank - 1) * ((uint32_t)p.K * W::BYTES),
+                                                       s * STEP + WRows::piece_of() * (16 / W::BYTES), p.K, edge);
+                    }
+            };
+            if ((s + 1) * STEP > p.K) each(std::true_type());
+            else each(std::false_type());
         };
-        auto fetch = [&](int s) __attribute__((always_inline)) {
-            if ((s + 1) * STEP > p.K) fetch_step(s, std::true_type());
-            else fetch_step(s, std::false_type());
-        };
-        // Tiles of an XCD begin at steps of their own: rows a power of two apart would all ask the same memory channels at a time
-        const int n = to - from, turn = n > 0 ? (int)((m0 / 128 * 4) % n) : 0;
-        auto step = [&](int i) { return from + (i + turn < n ? i + turn : i + turn - n); };
-        if (wave < n) fetch(step(wave));
+        if (wave < n) {
+            fetch_w(step(wave));
+            if (!ahead) fetch_x(step(wave));
+            ahead = false;
+        }
         for (int i = wave; i < n; i += 4) {
             xs.put(lds_x);
 #pragma unroll
             for (int r = 0; r < RT; ++r) ws[r].put(lds_w + r * WRows::BYTES);
-            if (i + 4 < n) fetch(step(i + 4));
+            if (i + 4 < n) {
+                fetch_x(step(i + 4));
+                fetch_w(step(i + 4));
+            }
             wave_order();
 #pragma unroll
             for (int h = 0; h < STEP / 32; ++h) {

@@ -128,12 +128,14 @@ __device__ __forceinline__ Key merged(Key a, Key b)
 struct Choice {
     Key best = 0, least;
     int waiting = 0, top;
+    bool any = false;
     Key *room;
     __device__ __forceinline__ Choice(Key *room, int top, Key least) : least(least), top(top), room(room) {}
     __device__ __forceinline__ void take(Key batch)
     {
         batch = sorted_down(batch);
-        best = merged(best, batch);
+        best = any ? merged(best, batch) : batch;
+        any = true;
         const Key last = lane_key(best, top - 1);
         least = last > least ? last : least;
     }
@@ -323,8 +325,20 @@ struct RowResult {
     }
 };
 
-template <class E>
-__device__ __forceinline__ void write_row(const ScoreParams &p, int64_t row, const Mass &m, bool far, Key best)
+// The given token's score, asked for long before it is used
+struct Given {
+    bool inside;
+    float score;
+    template <class E>
+    __device__ __forceinline__ void fetch(const ScoreParams &p, int64_t row, E)
+    {
+        const int64_t t = given_token(p.tokens, p.token_bits, row);
+        inside = t >= 0 && t < p.V;
+        score = E::get(static_cast<const typename E::raw *>(p.logits)[row * p.ld + (inside ? t : 0)]);
+    }
+};
+
+__device__ __forceinline__ void write_row(const ScoreParams &p, int64_t row, const Given &given, const Mass &m, bool far, Key best)
 {
     const RowResult r(m, p, far);
     const int lane = threadIdx.x & 63;
@@ -334,10 +348,7 @@ __device__ __forceinline__ void write_row(const ScoreParams &p, int64_t row, con
     }
     if (lane != 0) return;
     const bool empty = m.most == -__builtin_inff() && m.sum == 0.0f;
-    const int64_t t = given_token(p.tokens, p.token_bits, row);
-    float log_prob = 0.0f;
-    if (t >= 0 && t < p.V) log_prob = r.log_prob(E::get(static_cast<const typename E::raw *>(p.logits)[row * p.ld + t]));
-    p.log_probs[row] = log_prob;
+    p.log_probs[row] = given.inside ? r.log_prob(given.score) : 0.0f;
     const float entropy = (r.log_sum - m.weighted / m.sum) * LN2;
     p.entropies[row] = empty || entropy < 0.0f ? 0.0f : entropy;
     const float above = far ? 0.0f : __builtin_fmaf(m.most, p.c, -m.ref);
@@ -356,6 +367,8 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
     const int64_t row = blockIdx.x / (unsigned)p.parts;
     const int part = (int)(blockIdx.x - (unsigned)row * (unsigned)p.parts);
     const ScoreRow<E> r(p, row);
+    Given given;
+    if (p.parts == 1 && threadIdx.x < 64) given.fetch(p, row, E());
     const int all_pieces = (r.end + PIECE - 1) / PIECE;
     const int piece0 = part * p.pieces_per_part < all_pieces ? part * p.pieces_per_part : all_pieces;
     const int pieces = all_pieces - piece0 < p.pieces_per_part ? all_pieces - piece0 : p.pieces_per_part;
@@ -437,20 +450,21 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
         wave_order();
         const Key least = pieces < p.top ? 0 : lane_key(piece, p.top - 1) & 0xFFFFFFFF00000000ull;
         Choice choice(room, p.top, least);
-        for (int i = 0; i < n; i += 4) {
-            Key k[4];
+        for (int i = 0; i < n; i += 8) {
+            Key k[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < 8; ++u) {
                 const int place = (piece0 + chosen[i + u < n ? i + u : i]) * PIECE + lane;
                 const bool real = i + u < n && place >= r.shift && place < r.end;
                 k[u] = real ? key_of(E::get(r.from[place]), (uint32_t)(place - r.shift)) : 0;
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) choice.add(k[u]);
+            for (int u = 0; u < 8; ++u)
+                if (i + u < n) choice.add(k[u]);
         }
         best = choice.finish();
     }
-    if (p.parts == 1) return write_row<E>(p, row, m, far, best);
+    if (p.parts == 1) return write_row(p, row, given, m, far, best);
     const int64_t at = row * p.parts + part;
     if (lane == 0) p.partials[at] = make_float4(m.most, m.ref, m.sum, m.weighted);
     if (TOP && lane < p.top) p.keys[at * p.top + lane] = best;
@@ -464,6 +478,8 @@ __global__ __launch_bounds__(64) void token_join_kernel(const ScoreParams p)
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x;
     const float4 *parts = p.partials + row * p.parts;
+    Given given;
+    given.fetch(p, row, E());
     float most = -__builtin_inff(), ref = -FAR;
     for (int i = lane; i < p.parts; i += 64) {
         most = fmaxf(most, parts[i].x);
@@ -489,7 +505,7 @@ __global__ __launch_bounds__(64) void token_join_kernel(const ScoreParams p)
         const Key *keys = p.keys + row * p.parts * p.top;
         best = choose(p.parts * p.top, p.top, room, [&](int i) { return keys[i]; });
     }
-    write_row<E>(p, row, m, far, best);
+    write_row(p, row, given, m, far, best);
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------------------
