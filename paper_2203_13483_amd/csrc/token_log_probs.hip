@@ -19,15 +19,16 @@ constexpr float NO_MASS = -16384.0f;  // an exponent (base 2) whose power is 0, 
 constexpr float FAR = 0x1p100f;       // scaled scores beyond are taken relative to the row's largest, in a pass of their own
 constexpr float RISE = 4.0f;          // (exponents above the reference cancel in the logarithms, with the rounding of their size)
 constexpr int TOP_MOST = 64;
-constexpr int PIECE = 64;             // neighbouring scores whose largest is kept for the choice of alternatives
-constexpr int PIECES_MOST = 4096;     // of a workgroup: 16 KiB of LDS
+constexpr int SCORE_UNROLL = 4;
+constexpr int STEP = 64 * SCORE_UNROLL;  // vectors of eight neighbouring scores that a wave takes at a time
+constexpr int STEPS_MOST = 64;           // of a workgroup that chooses alternatives: a lane's largest score of a step is kept, 16 KiB of LDS
 
 struct ScoreParams {
     const void *logits;
     const void *tokens;
     int64_t ld, M;
     int V, token_bits, top;
-    int parts, pieces_per_part;
+    int parts, steps_per_part;
     float c;  // scale * log2(e)
     float scale;
     float *normalizers, *log_probs, *entropies;
@@ -174,6 +175,7 @@ __device__ __forceinline__ Key choose(int n, int top, Key *room, F &&key)
 {
     const int lane = threadIdx.x & 63;
     Key mine = 0;
+#pragma unroll 4
     for (int i = lane; i < n; i += 64) {
         const Key k = key(i);
         mine = k > mine ? k : mine;
@@ -186,14 +188,6 @@ __device__ __forceinline__ Key choose(int n, int top, Key *room, F &&key)
 }
 
 // ---- one pass over the scores ---------------------------------------------------------------------------------------------
-// The largest of eight neighbouring lanes
-__device__ __forceinline__ float most_of_eight(float v)
-{
-    v = lane_pair<1>(v, MaxF32());
-    v = lane_pair<2>(v, MaxF32());
-    return fmaxf(v, __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x141, 0xF, 0xF, true)));
-}
-
 // Eight neighbouring scores as they are in memory
 template <class E>
 struct Eight {
@@ -211,22 +205,31 @@ struct Eight {
         if constexpr (E::BYTES == 4) return __uint_as_float(x);
         else return E::get((uint16_t)(x >> (16 * (i % 2))));
     }
-    // (binary16: two at a time, so that get() is only an operand of the fused product)
-    __device__ __forceinline__ float most() const
-    {
-        if constexpr (std::is_same<E, ElemF16>::value) {
-            auto larger = [](uint32_t a, uint32_t b) {
-                uint32_t r;
-                asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-                return r;
-            };
-            const uint32_t two = larger(larger(w[0].x, w[0].y), larger(w[0].z, w[0].w));
-            return fmaxf(ElemF16::get((uint16_t)two), ElemF16::get((uint16_t)(two >> 16)));
-        } else {
-            return fmaxf(fmaxf(fmaxf(get(0), get(1)), fmaxf(get(2), get(3))), fmaxf(fmaxf(get(4), get(5)), fmaxf(get(6), get(7))));
-        }
-    }
 };
+// The largest of a lane's vectors, a NaN as -infinity.  (Binary16: two at a time, so that get() is only an operand of the fused product)
+template <class E, int N>
+__device__ __forceinline__ float largest_of(const Eight<E> (&x)[N])
+{
+    float v = -__builtin_inff();
+    if constexpr (std::is_same<E, ElemF16>::value) {
+        uint32_t two = 0xFC00FC00u;
+        auto take = [&](uint32_t w) { asm("v_pk_max_f16 %0, %0, %1" : "+v"(two) : "v"(w)); };
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            take(x[u].w[0].x);
+            take(x[u].w[0].y);
+            take(x[u].w[0].z);
+            take(x[u].w[0].w);
+        }
+        v = fmaxf(fmaxf(v, ElemF16::get((uint16_t)two)), ElemF16::get((uint16_t)(two >> 16)));
+    } else {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v = fmaxf(v, x[u].get(e));
+    }
+    return v;
+}
 
 // A row, or a part of it, seen as vectors of eight from `shift` places before its first score
 template <class E>
@@ -264,23 +267,12 @@ struct ScoreRow {
     }
 };
 
-constexpr int SCORE_UNROLL = 4;
-
-// N vectors of each lane, 64 apart; the first lane's first is number `first` of the workgroup's
-template <class E, bool TOP, int N>
-__device__ __forceinline__ void add_vectors(const ScoreParams &p, const Eight<E> (&x)[N], Mass &m, float *largest, int first, int pieces)
+// N vectors of each lane, whose largest score is returned
+template <class E, int N>
+__device__ __forceinline__ float add_vectors(const ScoreParams &p, const Eight<E> (&x)[N], Mass &m)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-        float v = x[u].most();
-        m.most = fmaxf(m.most, v);
-        if constexpr (TOP) {
-            v = fmaxf(most_of_eight(v), -__builtin_inff());
-            const int at = (first + u * 64 + lane) / (PIECE / 8);
-            if ((lane & 7) == 0 && at < pieces) largest[at] = v;
-        }
-    }
+    const float largest = largest_of(x);
+    m.most = fmaxf(m.most, largest);
     const float up = m.most * p.c;
     if (up > m.ref + RISE) {
         const float ref = __builtin_ceilf(up);
@@ -295,6 +287,7 @@ __device__ __forceinline__ void add_vectors(const ScoreParams &p, const Eight<E>
             m.sum += power;
             m.weighted = __builtin_fmaf(power, fmaxf(d, NO_MASS), m.weighted);
         }
+    return largest;
 }
 
 // The masses of all lanes of a wave, or of several waves, one after the other, in every lane
@@ -369,33 +362,35 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
     const ScoreRow<E> r(p, row);
     Given given;
     if (p.parts == 1 && threadIdx.x < 64) given.fetch(p, row, E());
-    const int all_pieces = (r.end + PIECE - 1) / PIECE;
-    const int piece0 = part * p.pieces_per_part < all_pieces ? part * p.pieces_per_part : all_pieces;
-    const int pieces = all_pieces - piece0 < p.pieces_per_part ? all_pieces - piece0 : p.pieces_per_part;
-    const int v0 = piece0 * (PIECE / 8), v1 = v0 + pieces * (PIECE / 8);
+    const int all_steps = (r.end + STEP * 8 - 1) / (STEP * 8);
+    const int step0 = part * p.steps_per_part < all_steps ? part * p.steps_per_part : all_steps;
+    const int steps = all_steps - step0 < p.steps_per_part ? all_steps - step0 : p.steps_per_part;
+    const int v0 = step0 * STEP, v1 = v0 + steps * STEP;
 
-    // A wave has SCORE_UNROLL * 64 neighbouring vectors at a time.  Only where the row begins or ends among them they are looked at one by one.
+    // A wave has STEP neighbouring vectors at a time.  Only where the row begins or ends among them they are looked at one by one.
     // (Rows a power of two apart that all began at the same place would ask the same memory channels: each begins at another.)
     Mass m = {-__builtin_inff(), -FAR, 0.0f, 0.0f};
-    constexpr int STEP = 64 * SCORE_UNROLL;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int steps = (v1 - v0 + STEP - 1) / STEP, mine = (steps - wave + WAVES - 1) / WAVES;
-    int step = mine > 0 ? (int)(blockIdx.x % (unsigned)mine) : 0;
-    for (int i = 0; i < mine; ++i, step = step + 1 < mine ? step + 1 : 0) {
-        const int v = v0 + (step * WAVES + wave) * STEP;
-        if (v * 8 >= r.shift && (v + STEP) * 8 <= r.end && v + STEP <= v1) {
+    const int mine = (steps - wave + WAVES - 1) / WAVES;
+    int turn = mine > 0 ? (int)(blockIdx.x % (unsigned)mine) : 0;
+    for (int i = 0; i < mine; ++i, turn = turn + 1 < mine ? turn + 1 : 0) {
+        const int step = turn * WAVES + wave, v = v0 + step * STEP;
+        float most;
+        if (v * 8 >= r.shift && (v + STEP) * 8 <= r.end) {
             Eight<E> x[SCORE_UNROLL];
 #pragma unroll
             for (int u = 0; u < SCORE_UNROLL; ++u) x[u].fetch(r.from + (int64_t)(v + u * 64 + lane) * 8);
-            add_vectors<E, TOP>(p, x, m, largest, v - v0, pieces);
+            most = add_vectors(p, x, m);
         } else {
+            most = -__builtin_inff();
 #pragma unroll 1
-            for (int w = v; w < v + STEP && w < v1; w += 64) {
+            for (int w = v; w < v + STEP && w * 8 < r.end; w += 64) {
                 Eight<E> x[1];
-                r.get(w + lane, w + lane < v1, x[0]);
-                add_vectors<E, TOP>(p, x, m, largest, w - v0, pieces);
+                r.get(w + lane, true, x[0]);
+                most = fmaxf(most, add_vectors(p, x, m));
             }
         }
+        if constexpr (TOP) largest[step * 64 + lane] = most;
     }
     m = joined(m);
     if ((threadIdx.x & 63) == 0) masses[threadIdx.x >> 6] = m;
@@ -443,25 +438,44 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
     if (threadIdx.x >= 64) return;
     Key best = 0;
     if constexpr (TOP) {
-        // The `top` pieces with the largest scores hold the `top` largest scores (ties: the lower piece has the lower places)
-        const Key piece = choose(pieces, p.top, room, [&](int i) { return key_of(largest[i], (uint32_t)i); });
-        const int n = pieces < p.top ? pieces : p.top;
-        if (lane < n) chosen[lane] = (int)place_of(piece);
-        wave_order();
-        const Key least = pieces < p.top ? 0 : lane_key(piece, p.top - 1) & 0xFFFFFFFF00000000ull;
-        Choice choice(room, p.top, least);
-        for (int i = 0; i < n; i += 8) {
-            Key k[8];
+        // A lane's scores of a step are a piece.  The top-th largest of the pieces' largest scores is a bound that only `top` pieces reach, or
+        // more where scores are equal: the choice is among the scores of these that reach it.  Half a wave looks at a piece.
+        const int pieces = steps * 64;
+        const Key last = pieces < p.top ? 0 : lane_key(choose(pieces, p.top, room, [&](int i) { return key_of(largest[i], (uint32_t)i); }), p.top - 1);
+        const uint32_t bound = (uint32_t)(last >> 32);
+        Choice choice(room, p.top, (Key)bound << 32);
+        auto look = [&](int n) {
+            for (int i = 0; i < n; i += 16) {
+                Key k[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int place = (piece0 + chosen[i + u < n ? i + u : i]) * PIECE + lane;
-                const bool real = i + u < n && place >= r.shift && place < r.end;
-                k[u] = real ? key_of(E::get(r.from[place]), (uint32_t)(place - r.shift)) : 0;
+                for (int u = 0; u < 8; ++u) {
+                    const int which = i + 2 * u + lane / 32, piece = chosen[which < n ? which : 0];
+                    const int place = (v0 + (piece >> 6) * STEP + (lane >> 3 & 3) * 64 + (piece & 63)) * 8 + (lane & 7);
+                    const bool real = which < n && place >= r.shift && place < r.end;
+                    k[u] = real ? key_of(E::get(r.from[place]), (uint32_t)(place - r.shift)) : 0;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (i + 2 * u < n) choice.add(k[u]);
             }
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (i + u < n) choice.add(k[u]);
+        };
+        int found = 0;
+        for (int i = 0; i < pieces; i += 64) {
+            const bool reaches = ordered(largest[i + lane]) >= bound;
+            const uint64_t mask = __ballot(reaches);
+            if (!mask) continue;
+            const int n = __popcll(mask);
+            if (found + n > TOP_MOST) {
+                look(found);
+                found = 0;
+                wave_order();
+            }
+            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+            if (reaches) chosen[found + before] = i + lane;
+            found += n;
+            wave_order();
         }
+        look(found);
         best = choice.finish();
     }
     if (p.parts == 1) return write_row(p, row, given, m, far, best);
@@ -579,13 +593,13 @@ __global__ __launch_bounds__(256) void token_gradient_kernel(const ScoreGradPara
 // ---- host side ------------------------------------------------------------------------------------------------------------
 constexpr int64_t SCORES_MOST = 0x7FFFFF00;  // columns, rows
 
-// Parts of a row: so many that the pieces of each fit LDS, and more where there are few rows for 256 CUs
+// Parts of a row: so many that what is kept of each fits LDS, and more where there are few rows for 256 CUs
 static int row_parts(int64_t M, int64_t V, int top)
 {
-    const int64_t pieces = ceil_div(V + 7, PIECE);
-    int64_t parts = top > 0 ? ceil_div(pieces, PIECES_MOST) : 1;
-    const int64_t wanted = ceil_div(512, M);                 // workgroups for the chip
-    const int64_t useful = ceil_div(pieces, 1024);           // 64 scores a thread of a large workgroup
+    const int64_t steps = ceil_div(V + 7, STEP * 8);
+    int64_t parts = top > 0 ? ceil_div(steps, STEPS_MOST) : 1;
+    const int64_t wanted = ceil_div(512, M);        // workgroups for the chip
+    const int64_t useful = ceil_div(steps, 32);     // two steps for each wave of a large workgroup
     const int64_t more = wanted < useful ? wanted : useful;
     if (more > parts) parts = more;
     return (int)(parts < 1024 ? parts : 1024);
@@ -596,7 +610,7 @@ static bool score_scale_ok(float s) { return s >= 0x1p-100f && s <= 0x1p100f; }
 template <class E, bool TOP, int THREADS>
 static void launch_mass(const ScoreParams &p, hipStream_t st)
 {
-    const int lds = TOP ? p.pieces_per_part * (int)sizeof(float) : 0;
+    const int lds = TOP ? p.steps_per_part * 64 * (int)sizeof(float) : 0;
     token_mass_kernel<E, TOP, THREADS><<<(unsigned)(p.M * p.parts), THREADS, lds, st>>>(p);
 }
 
@@ -634,7 +648,7 @@ extern "C" int mkq_token_log_probs(const void *logits, int dtype, int64_t ld, in
     p.token_bits = token_bits;
     p.top = top;
     p.parts = row_parts(M, V, top);
-    p.pieces_per_part = (int)ceil_div(ceil_div(V + 7, PIECE), p.parts);
+    p.steps_per_part = (int)ceil_div(ceil_div(V + 7, STEP * 8), p.parts);
     p.scale = scale;
     p.c = scale * LOG2E;
     p.normalizers = normalizers;
