@@ -62,10 +62,15 @@ static ShrinkParams shrink_params(const AdapterShape &d, const AdapterParams &a,
     p.hidden = hidden;
     return p;
 }
+// Workgroups of the launches; a call whose grids do not fit is refused before the first of them
+static int64_t shrink_workgroups(const AdapterShape &d, int splits) { return ceil_div(d.M, 16) * slots_of(d) * splits * ceil_div(d.rank, 16 * rank_tiles(d.rank)); }
+static int64_t expand_workgroups(const AdapterShape &d, int64_t side) { return ColumnTask::workgroups(ceil_div(d.M, 16) * slots_of(d), ceil_div(side, 128)); }
+static int64_t outer_workgroups(const AdapterShape &d, int64_t tasks, int64_t blocks) { return ColumnTask::workgroups(tasks * ceil_div(d.rank, 16 * outer_tiles(d.rank)), blocks); }
+static int64_t join_workgroups(const AdapterShape &d, int64_t sides) { return d.R * ceil_div((int64_t)d.rank * sides, 256); }
+
 static int launch_shrink(const AdapterShape &d, const ShrinkParams &p, int x_dtype, int w_dtype, hipStream_t st)
 {
-    const int64_t workgroups = (p.x ? ceil_div(d.M, 16) * p.slots * p.a.splits * p.rank_chunks : 0) + p.plans;
-    if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
+    const int64_t workgroups = (p.x ? shrink_workgroups(d, p.a.splits) : 0) + p.plans;
     launch_shrink_kernel(p, x_dtype, w_dtype, (unsigned)workgroups, st);
     return launch_status();
 }
@@ -75,8 +80,7 @@ static int launch_expand(const AdapterShape &d, ExpandParams p, int w_dtype, int
     p.column_blocks = (int)ceil_div(p.N, 128);
     p.slots = slots_of(d);
     p.row_groups = (int)ceil_div(d.M, 16);
-    const int64_t workgroups = ColumnTask::workgroups((int64_t)p.row_groups * p.slots, p.column_blocks);
-    if (!grid_ok(workgroups, 256)) return MKQ_ERR_UNSUPPORTED;
+    const int64_t workgroups = expand_workgroups(d, p.N);
     launch_expand_kernel(p, w_dtype, out_dtype, (unsigned)workgroups, st);
     return launch_status();
 }
@@ -127,9 +131,8 @@ static AdapterWorkspace gradient_workspace(const AdapterShape &d)
 static int launch_outer(const AdapterShape &d, OuterParams p, int x_dtype, int dy_dtype, hipStream_t st)
 {
     p.rank_chunks = (int)ceil_div(d.rank, 16 * outer_tiles(d.rank));
-    const int64_t workgroups = ColumnTask::workgroups((int64_t)p.plan.tasks_most * p.rank_chunks, p.side[0].column_blocks + p.side[1].column_blocks);
-    const int64_t joins = d.R * ceil_div((int64_t)d.rank * ((p.side[0].column_blocks ? d.K : 0) + (p.side[1].column_blocks ? d.N : 0)), 256);
-    if (!grid_ok(workgroups, 256) || !grid_ok(joins, 256)) return MKQ_ERR_UNSUPPORTED;
+    const int64_t workgroups = outer_workgroups(d, p.plan.tasks_most, p.side[0].column_blocks + p.side[1].column_blocks);
+    const int64_t joins = join_workgroups(d, (p.side[0].column_blocks ? d.K : 0) + (p.side[1].column_blocks ? d.N : 0));
     launch_outer_kernel(p, x_dtype, dy_dtype, (unsigned)workgroups, st);
     if (d.M > p.plan.piece) launch_outer_join_kernel(p, (unsigned)joins, st);
     return launch_status();
@@ -161,6 +164,7 @@ extern "C" int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, co
     if (ld_out > STRIDE_MOST || (base && ld_base > STRIDE_MOST)) return MKQ_ERR_UNSUPPORTED;
     if (base && !in_place_or_apart(base, out_dtype, ld_base, out, out_dtype, ld_out, M, N)) return MKQ_ERR_UNSUPPORTED;
     const AdapterWorkspace w = forward_workspace(d);
+    if (!grid_ok(shrink_workgroups(d, w.splits), 256) || !grid_ok(expand_workgroups(d, N), 256)) return MKQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < w.total) return MKQ_ERR_WORKSPACE;
     if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
     const hipStream_t st = as_stream(stream);
@@ -219,7 +223,10 @@ extern "C" int mkq_low_rank_adapters_gradient(const void *dy, int dy_dtype, int6
         // the batch's rows are read again behind dx
         if (!apart(dy, dy_dtype, ld_dy, N, dx, dx_dtype, ld_dx, K, M) || (d_down && !apart(x, x_dtype, pitch, K, dx, dx_dtype, ld_dx, K, M))) return MKQ_ERR_UNSUPPORTED;
     }
-    AdapterWorkspace w = gradient_workspace(d);
+    const AdapterWorkspace w = gradient_workspace(d);
+    if (!grid_ok(shrink_workgroups(d, w.splits) + R, 256) || (dx && M > 0 && !grid_ok(expand_workgroups(d, K), 256)) ||
+        !grid_ok(outer_workgroups(d, w.tasks_most, ceil_div(K, 128) + ceil_div(N, 128)), 256) || !grid_ok(join_workgroups(d, K + N), 256))
+        return MKQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < w.total) return MKQ_ERR_WORKSPACE;
     if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
     uint8_t *ws = static_cast<uint8_t *>(workspace);

@@ -591,7 +591,7 @@ __global__ __launch_bounds__(256) void token_gradient_kernel(const ScoreGradPara
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
-constexpr int64_t SCORES_MOST = 0x7FFFFF00;  // columns, rows
+constexpr int64_t SCORES_MOST = (int64_t)1 << 30;  // columns, rows: places are counted in 32 bits, past a row's end too
 
 // Parts of a row: so many that what is kept of each fits LDS, and more where there are few rows for 256 CUs
 static int row_parts(int64_t M, int64_t V, int top)

@@ -308,3 +308,37 @@ def test_equal_calls_streams_and_graph_replays(M, K, N, rank, R):
         other = run(side, None, None, torch.empty_like(hidden))
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(other, want)), i
+
+
+@pytest.mark.parametrize("M", [5, 700])
+def test_some_of_the_gradients(M):
+    """Each of dx, d_down and d_up without the others, what only these need being absent: the bits of the call that makes all."""
+    c = Case(M, 72, 88, 7, 3, BF16, BF16, BF16, "requests")
+    hidden = torch.randn(M, 7, device="cuda") * c.real[:, None]
+    lib, stream = mkq.load(), torch.cuda.current_stream().cuda_stream
+    n = mkq.mkq_low_rank_adapters_gradient_workspace_bytes(M, 72, 88, 7, 3)
+    all_dx, all_down, all_up = mkq.mkq_low_rank_adapters_gradient(c.dy, c.x, c.ids, hidden, c.down, c.up, c.scales)
+    _, one_down, _ = mkq.mkq_low_rank_adapters_gradient(c.dy, c.x, c.ids, hidden, c.down, c.up, c.scales, want_dx=False)
+    for name, want in (("dx", all_dx), ("d_down", one_down), ("d_up", all_up)):
+        got, ws = torch.full_like(want, 7.0), torch.full((n,), 0x5A, dtype=torch.uint8, device="cuda")
+        at = lambda t, needed: t.data_ptr() if name in needed else None  # noqa: E731
+        status = lib.mkq_low_rank_adapters_gradient(
+            c.dy.data_ptr(), 2, 88, at(c.x, ("d_down",)), 2, 72, None, 0, c.ids.data_ptr(), at(hidden, ("d_up",)), M, 72, 88, 7, 3,
+            at(c.down, ("dx",)), at(c.up, ("dx", "d_down")), 2, c.scales.data_ptr(), None, 0, at(got, ("dx",)), 2, 72,
+            at(got, ("d_down",)), at(got, ("d_up",)), 0, 0, ws.data_ptr(), n, stream)
+        assert status == mkq.MKQ_OK, name
+        assert torch.equal(got, want), name
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, against the same calls one after the other."""
+    cases = [Case(900, 520, 264, 12, 3, F16, F16, F16, "requests", seed=s) for s in (1, 2)]
+    want = [mkq.mkq_low_rank_adapters(c.x, c.ids, c.down, c.up, c.scales, base=c.base) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[], []]
+    for _ in range(10):
+        for k, (c, s) in enumerate(zip(cases, streams)):
+            got[k].append(mkq.mkq_low_rank_adapters(c.x, c.ids, c.down, c.up, c.scales, base=c.base, stream=s))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for gs, w in zip(got, want) for g in gs)
