@@ -6,7 +6,8 @@
 //
 // Both matrices of an adapter have their long side in rows, so three kernels do all of it: `shrink` (t, u: products along rows),
 // `expand` (out, dx: sums of the adapter's rows) and `outer` (sums of the batch's rows).  Bound by the bytes of x, dy, base and out; products
-// are the matrix unit's.
+// are the matrix unit's.  Measured, 8192 bfloat16 rows of 1024 and 4096, rank 16, us: shrink of x 8.5, of dy 17 (4 TB/s), expand to out with its base 30 (4.5
+// TB/s), to dx 9, outer of both (x in 8 bits) 23, its join 5.
 //
 // Operands enter the products exactly: binary16 and bfloat16 as they are where both sides are the same, otherwise a number is the sum of
 // one to three bfloat16 parts (binary32 three, binary16 two), and products of parts whose places add up to 2^-24 or less are left out.
