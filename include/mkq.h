@@ -557,7 +557,8 @@ int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int gr
  *   hidden      [M, rank] binary32: an output of the first, or NULL; needed for d_up
  *   d_down, d_up  [R, rank, K], [R, rank, N] of grad_dtype (F32, F16, BF16); accumulate: added to what is there, with one rounding.  dx, d_down and
  *               d_up may be NULL, but not all of them; what only they need may be NULL then
- *   workspace   at least the *_workspace_bytes bytes, 16-byte aligned; no preparation.  Two calls that may run at the same time need two
+ *   workspace   at least the *_workspace_bytes bytes (0, for few rows: may be NULL), 16-byte aligned; no preparation.  Two calls that may run at
+ *               the same time need two
  * Products are exact, all sums and hidden are binary32 (sums of products with 16-bit results may leave out 2^-16 of a product); equal calls give
  * equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
  * rank 1 .. 256, R up to about 4e6, rank K and rank N below 2^29, K and N from 8 and, as

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from array import array
+from functools import lru_cache
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmkq.so")
@@ -966,6 +967,7 @@ class TokenLogProbs:
     __slots__ = ("log_probs", "entropies", "normalizers", "top_tokens", "top_log_probs")
 
 
+@lru_cache(maxsize=4096)  # (they go by sizes alone, and the smallest calls are bound by their own calls)
 def mkq_token_log_probs_workspace_bytes(M: int, V: int, top: int = 0) -> int:
     return int(load().mkq_token_log_probs_workspace_bytes(M, V, top))
 
@@ -1089,10 +1091,12 @@ def mkq_checkpoint_gelu_gradient(codes, steps, dy, group: int = 128, dx_dtype: i
     return dx
 
 
+@lru_cache(maxsize=4096)
 def mkq_low_rank_adapters_workspace_bytes(M: int, K: int, N: int, rank: int, R: int) -> int:
     return int(load().mkq_low_rank_adapters_workspace_bytes(M, K, N, rank, R))
 
 
+@lru_cache(maxsize=4096)
 def mkq_low_rank_adapters_gradient_workspace_bytes(M: int, K: int, N: int, rank: int, R: int) -> int:
     return int(load().mkq_low_rank_adapters_gradient_workspace_bytes(M, K, N, rank, R))
 
@@ -1132,10 +1136,11 @@ def mkq_low_rank_adapters(x, adapter, down, up, scales=None, out_dtype: int | No
         _vector(hidden, M * rank, "hidden")
     out, ld_out = _out_rows(out, M, N, dtype, x.device, stream, "out")
     if workspace is None:
-        workspace = _new(mkq_low_rank_adapters_workspace_bytes(M, K, N, rank, R), torch.uint8, x.device, stream)
+        need = mkq_low_rank_adapters_workspace_bytes(M, K, N, rank, R)
+        workspace = _new(need, torch.uint8, x.device, stream) if need else None
     _check(load().mkq_low_rank_adapters(_ptr(x), x_dtype, ldx, _ptr(adapter), M, K, N, rank, R, _ptr(down), _ptr(up), w_dtype, _ptr(scales),
                                         _ptr(base), ld_base, _ptr(out), int(out_dtype), ld_out, _ptr(hidden), _ptr(workspace),
-                                        workspace.nbytes, _stream_on(dev, stream)), "mkq_low_rank_adapters")
+                                        0 if workspace is None else workspace.nbytes, _stream_on(dev, stream)), "mkq_low_rank_adapters")
     return out
 
 

@@ -95,6 +95,9 @@ static int piece_rows(const AdapterShape &d)
 
 static int pitch_of(int rank) { return (rank + 7) / 8 * 8; }
 
+// Few rows of short sides go in one launch: at most 64 rows, one tile of the rank, and what every workgroup reads again is 64 KiB at most (of 2 bytes)
+static bool few_rows(const AdapterShape &d) { return d.M <= 64 && d.rank <= 16 && d.K <= 1024; }
+
 struct AdapterWorkspace {
     size_t t, u, order, starts, tasks, down, up, total;
     int splits, piece;
@@ -103,8 +106,8 @@ struct AdapterWorkspace {
 static AdapterWorkspace forward_workspace(const AdapterShape &d)
 {
     AdapterWorkspace w = {};
-    w.splits = splits_of(d, d.K);
-    w.total = (size_t)w.splits * d.M * pitch_of(d.rank) * sizeof(float);
+    w.splits = few_rows(d) ? 1 : splits_of(d, d.K);
+    if (!few_rows(d)) w.total = (size_t)w.splits * d.M * pitch_of(d.rank) * sizeof(float);
     return w;
 }
 static AdapterWorkspace gradient_workspace(const AdapterShape &d)
@@ -166,13 +169,11 @@ extern "C" int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, co
     if (base && !in_place_or_apart(base, out_dtype, ld_base, out, out_dtype, ld_out, M, N)) return MKQ_ERR_UNSUPPORTED;
     const AdapterWorkspace w = forward_workspace(d);
     if (!grid_ok(shrink_workgroups(d, w.splits), 256) || !grid_ok(expand_workgroups(d, N), 256)) return MKQ_ERR_UNSUPPORTED;
-    if (!workspace || workspace_bytes < w.total) return MKQ_ERR_WORKSPACE;
+    if (w.total > 0 && (!workspace || workspace_bytes < w.total)) return MKQ_ERR_WORKSPACE;
     if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
     const hipStream_t st = as_stream(stream);
     const AdapterParams a = {adapter, scales, M, (int)R, rank, pitch_of(rank), w.splits};
     float *t = static_cast<float *>(workspace);
-    status = launch_shrink(d, shrink_params(d, a, x, ldx, down, K, false, t, w.splits == 1 ? hidden : nullptr), x_dtype, w_dtype, st);
-    if (status != MKQ_OK) return status;
     ExpandParams e = {};
     e.a = a;
     e.t = t;
@@ -185,7 +186,15 @@ extern "C" int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, co
     e.scaled = true;
     e.keep = w.splits > 1 ? hidden : nullptr;
     e.keep_pitch = rank;
-    return launch_expand(d, e, w_dtype, out_dtype, st);
+    if (few_rows(d)) {  // (no workspace)
+        e.column_blocks = (int)ceil_div(N, 128);
+        e.slots = slots_of(d);
+        launch_few_kernel(shrink_params(d, a, x, ldx, down, K, false, nullptr, hidden), e, x_dtype, w_dtype, out_dtype,
+                          (unsigned)(ceil_div(M, 16) * e.slots * ceil_div(e.column_blocks, 4)), st);
+        return launch_status();
+    }
+    status = launch_shrink(d, shrink_params(d, a, x, ldx, down, K, false, t, w.splits == 1 ? hidden : nullptr), x_dtype, w_dtype, st);
+    return status == MKQ_OK ? launch_expand(d, e, w_dtype, out_dtype, st) : status;
 }
 
 extern "C" size_t mkq_low_rank_adapters_gradient_workspace_bytes(int64_t M, int64_t K, int64_t N, int rank, int64_t R)

@@ -64,54 +64,6 @@ __device__ void plan(const AdapterParams &p, const PlanParams &plan, int a)
 }
 
 // ---- shrink ---------------------------------------------------------------------------------------------------------------
-template <class E>
-__device__ __forceinline__ void operand(const Neighbours<E> &n, uint4 (&out)[Parts<E>::N])
-{
-    if constexpr (std::is_same<E, ElemBF16>::value) {
-        out[0] = __builtin_bit_cast(uint4, n.w[0]);
-    } else {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = n.get(i);
-        parts_of(v, out);
-    }
-}
-
-// Places of a row that a wave multiplies at a time: 256 bytes of the larger elements
-constexpr int shrink_step(int x_bytes, int w_bytes) { return x_bytes == 4 || w_bytes == 4 ? 64 : 128; }
-
-// Sixteen rows of a step on their way from memory to LDS: neighbouring lanes fetch neighbouring pieces of 16 bytes of a row.  (Fetched as
-// the matrix unit takes them, a row a lane, every lane asked for a line of its own: dy of 8192 x 4096 bfloat16 32 instead of 17 us.)  In LDS piece i of row r is
-// at i ^ r, so that sixteen rows' same pieces, and a row's sixteen pieces, are on different banks.
-template <class E, int STEP>
-struct ShrinkRows {
-    static constexpr int PIECES = STEP * E::BYTES / 16, N = PIECES / 4;  // of a row, of a lane
-    static constexpr int BYTES = 16 * STEP * E::BYTES;
-    u32x4 v[N];
-    __device__ static __forceinline__ int row_of(int i) { return (64 * i + (int)(threadIdx.x & 63)) / PIECES; }
-    __device__ static __forceinline__ int piece_of() { return (threadIdx.x & 63) % PIECES; }
-    __device__ __forceinline__ void put(uint8_t *lds) const
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int r = row_of(i);
-            *reinterpret_cast<u32x4 *>(lds + (r * PIECES + (piece_of() ^ (r % PIECES))) * 16) = v[i];
-        }
-    }
-    // lane (c, q): eight places from 32 h + 8 q on of row c
-    __device__ static __forceinline__ Neighbours<E> get(const uint8_t *lds, int h)
-    {
-        const int c = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
-        Neighbours<E> n;
-#pragma unroll
-        for (int i = 0; i < E::BYTES / 2; ++i) {
-            const int piece = (4 * h + q) * (E::BYTES / 2) + i;
-            n.w[i] = *reinterpret_cast<const u32x4 *>(lds + (c * PIECES + (piece ^ (c % PIECES))) * 16);
-        }
-        return n;
-    }
-};
-
 // Tiles of 16 rows and RT * 16 of the rank; the four waves of a workgroup take steps in turn and add up through LDS
 template <class X, class W, int RT>
 __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkParams p)

@@ -278,7 +278,7 @@ def test_no_rows():
 @pytest.mark.parametrize("M,K,N,rank,R", [(16, 768, 768, 8, 16), (1, 4096, 1024, 16, 4), (700, 520, 264, 12, 3)])
 def test_equal_calls_streams_and_graph_replays(M, K, N, rank, R):
     c = Case(M, K, N, rank, R, F16, F16, F16, "mixed")
-    ws = torch.empty(mkq.mkq_low_rank_adapters_workspace_bytes(M, K, N, rank, R), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(mkq.mkq_low_rank_adapters_workspace_bytes(M, K, N, rank, R) + 16, dtype=torch.uint8, device="cuda")
     wg = torch.empty(mkq.mkq_low_rank_adapters_gradient_workspace_bytes(M, K, N, rank, R), dtype=torch.uint8, device="cuda")
     hidden = torch.empty(M, rank, device="cuda")
 
