@@ -89,7 +89,7 @@ static int launch_expand(const AdapterShape &d, ExpandParams p, int w_dtype, int
 // Rows of a piece: about 3000 waves in all
 static int piece_rows(const AdapterShape &d)
 {
-    const int64_t columns = ceil_div(d.K, 128) + ceil_div(d.N, 128), n = ceil_div(ceil_div(d.M * columns, 3072), 64) * 64;
+    const int64_t columns = ceil_div(d.K, 128) + ceil_div(d.N, 128), n = ceil_div(ceil_div(d.M * columns, 3000), 64) * 64;
     return (int)(n < 64 ? 64 : n > 2048 ? 2048 : n);
 }
 
