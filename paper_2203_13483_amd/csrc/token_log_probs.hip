@@ -17,7 +17,9 @@ namespace mkq {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float NO_MASS = -16384.0f;  // an exponent (base 2) whose power is 0, to be multiplied by it
-constexpr float FAR = 0x1p100f;       // scaled scores beyond are taken relative to the row's largest, in a pass of their own
+// Rows whose largest scaled score (to the base 2) is beyond are summed relative to that score, in a pass of their own.  Up to here c * most rounded
+// to binary32 is off by 2^-4 at most, and so is the largest score's exponent relative to what is rounded up from it.
+constexpr float FAR = 0x1p20f;
 constexpr float RISE = 4.0f;          // (exponents above the reference cancel in the logarithms, with the rounding of their size)
 constexpr int TOP_MOST = 64;
 constexpr int SCORE_UNROLL = 4;
@@ -507,9 +509,10 @@ __global__ __launch_bounds__(64) void token_join_kernel(const ScoreParams p)
     for (int i = lane; i < p.parts; i += 64) {
         Mass o = {parts[i].x, parts[i].y, parts[i].z, parts[i].w};
         const bool far_part = is_far(o.most, p.c);
-        // a far part below a row that is not far, and a part that is not far in a far row, add nothing but a NaN
-        const float by = far != far_part ? NO_MASS : far ? (o.most == most ? 0.0f : fmaxf((o.most - most) * p.c, NO_MASS)) : fall(o.ref, ref);
-        rebase(o, by);
+        // a far part is relative to its largest score, another to its reference; and so is the row
+        float by = far ? __builtin_fmaf(-most, p.c, o.ref) : o.ref - ref;
+        if (far_part) by = !far ? __builtin_fmaf(o.most, p.c, -ref) : o.most == most ? 0.0f : (o.most - most) * p.c;
+        rebase(o, fmaxf(by, NO_MASS));
         m.sum += o.sum;
         m.weighted += o.weighted;
     }
