@@ -553,8 +553,9 @@ int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int gr
  *   down, up    [R, rank, K], [R, rank, N] of w_dtype: the long side in rows, of both;  scales [R] binary32, or NULL: 1.  A smaller adapter
  *               has zeros in its last rows
  *   base, out   [M, N] of out_dtype;  dx_base, dx [M, K] of dx_dtype; their row strides.  A base is its result if the strides are the same, otherwise
- *               apart from it; dx is apart from dy and x (else UNSUPPORTED).  What lies between the rows is left as it is
- *   hidden      [M, rank] binary32: an output of the first, or NULL; needed for d_up
+ *               apart from it; out is apart from x, but may be other columns of one matrix of wider rows; dx is apart from dy and x (else UNSUPPORTED).
+ *               What lies between the rows is left as it is
+ *   hidden      [M, rank] binary32: an output of the first, apart from x and out, or NULL; needed for d_up
  *   d_down, d_up  [R, rank, K], [R, rank, N] of grad_dtype (F32, F16, BF16); accumulate: added to what is there, with one rounding.  dx, d_down and
  *               d_up may be NULL, but not all of them; what only they need may be NULL then
  *   workspace   at least the *_workspace_bytes bytes (0, for few rows: may be NULL), 16-byte aligned; no preparation.  Two calls that may run at

@@ -1117,7 +1117,7 @@ def _adapters(adapter, down, up, scales, M: int):
 def mkq_low_rank_adapters(x, adapter, down, up, scales=None, out_dtype: int | None = None, *, base=None, out=None, hidden=None, workspace=None,
                           stream=None):
     """base + scales[a] * (x down_a^T) up_a for every row's adapter a (int32 [M]; outside: none) -> [M,N] of out_dtype (None: x's).  down [R,rank,K],
-    up [R,rank,N]; ``base`` [M,N] of out_dtype, ``out`` too if need be; ``hidden`` float32 [M,rank]: x down_a^T for the gradient."""
+    up [R,rank,N]; ``base`` [M,N] of out_dtype, ``out`` too if need be, but never x; ``hidden`` float32 [M,rank]: x down_a^T for the gradient."""
     torch = _torch()
     ldx, x_dtype = _rows(x, "x"), _float_code(x, "x")
     M = x.size(0)

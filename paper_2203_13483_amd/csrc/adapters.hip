@@ -167,6 +167,10 @@ extern "C" int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, co
     if (status != MKQ_OK) return status;
     if (ld_out > STRIDE_MOST || (base && ld_base > STRIDE_MOST)) return MKQ_ERR_UNSUPPORTED;
     if (base && !in_place_or_apart(base, out_dtype, ld_base, out, out_dtype, ld_out, M, N)) return MKQ_ERR_UNSUPPORTED;
+    // few rows' workgroups read whole rows of x beside others' writes
+    if (!apart_or_beside(x, x_dtype, ldx, K, out, out_dtype, ld_out, N, M)) return MKQ_ERR_UNSUPPORTED;
+    if (hidden && (!apart(x, x_dtype, ldx, K, hidden, MKQ_F32, rank, rank, M) || !apart(out, out_dtype, ld_out, N, hidden, MKQ_F32, rank, rank, M)))
+        return MKQ_ERR_UNSUPPORTED;
     const AdapterWorkspace w = forward_workspace(d);
     if (!grid_ok(shrink_workgroups(d, w.splits), 256) || !grid_ok(expand_workgroups(d, N), 256)) return MKQ_ERR_UNSUPPORTED;
     if (w.total > 0 && (!workspace || workspace_bytes < w.total)) return MKQ_ERR_WORKSPACE;

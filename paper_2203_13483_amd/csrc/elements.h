@@ -120,6 +120,16 @@ inline bool apart(const void *a, int a_dtype, int64_t ld_a, int64_t cols_a, cons
     const uintptr_t i = reinterpret_cast<uintptr_t>(a), o = reinterpret_cast<uintptr_t>(b);
     return i + extent(ld_a, cols_a, a_dtype) <= o || o + extent(ld_b, cols_b, b_dtype) <= i;
 }
+// ... or are different columns of one matrix of wider rows
+inline bool apart_or_beside(const void *a, int a_dtype, int64_t ld_a, int64_t cols_a, const void *b, int b_dtype, int64_t ld_b, int64_t cols_b, int64_t M)
+{
+    if (apart(a, a_dtype, ld_a, cols_a, b, b_dtype, ld_b, cols_b, M)) return true;
+    const uintptr_t i = reinterpret_cast<uintptr_t>(a), o = reinterpret_cast<uintptr_t>(b);
+    const uint64_t pitch = (uint64_t)ld_a * (uint64_t)dtype_bytes(a_dtype);
+    if (pitch != (uint64_t)ld_b * (uint64_t)dtype_bytes(b_dtype)) return false;
+    const uint64_t from = o >= i ? (o - i) % pitch : (pitch - (i - o) % pitch) % pitch;  // b's columns in a's rows
+    return from >= (uint64_t)cols_a * (uint64_t)dtype_bytes(a_dtype) && from + (uint64_t)cols_b * (uint64_t)dtype_bytes(b_dtype) <= pitch;
+}
 // Whether results [M, K] lie apart from what they are computed from, value by value, or exactly over it
 inline bool in_place_or_apart(const void *in, int in_dtype, int64_t ld_in, const void *out, int out_dtype, int64_t ld_out, int64_t M, int64_t K)
 {

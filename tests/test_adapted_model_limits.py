@@ -1,0 +1,53 @@
+"""Limits of the operators of adapted models that the host checks (no GPU): status codes of the C ABI before anything is enqueued."""
+import ctypes as C
+import os
+
+import pytest
+
+import paper_2203_13483_amd as mkq
+
+P, Q, X = C.c_void_p(0x1000), C.c_void_p(0x10000000), 0x20000000  # 16-byte aligned, never dereferenced: validation fails first
+F32, F16 = mkq.MKQ_F32, mkq.MKQ_F16
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(mkq.LIB_PATH):
+        from paper_2203_13483_amd import build
+        build.build()
+    return mkq.load()
+
+
+def _adapters(lib, x=X, ldx=768, out=0x30000000, ldo=768, base=None, hidden=None, M=16, K=768, N=768, rank=8, xt=F16, ot=F16, ws=None, n=0):
+    """Without room to work in: what is not refused before is a missing workspace, but for few rows, which would run."""
+    v = C.c_void_p
+    return lib.mkq_low_rank_adapters(v(x), xt, ldx, P, M, K, N, rank, 4, Q, Q, F16, None, v(base) if base else None, ldo, v(out), ot, ldo,
+                                     v(hidden) if hidden else None, ws, n, None)
+
+
+@pytest.mark.parametrize("M", [1, 16, 64, 65, 4096])
+def test_results_over_the_rows_they_are_computed_from(lib, M):
+    """Workgroups of other columns may still read x where results are written."""
+    last = 2 * 768 * M
+    for base in (None, X):
+        assert _adapters(lib, out=X, base=base, M=M) == mkq.MKQ_ERR_UNSUPPORTED
+    for out in (X + 16, X + last - 16, X - last + 16):
+        assert _adapters(lib, out=out, M=M) == mkq.MKQ_ERR_UNSUPPORTED, hex(out - X)
+    assert _adapters(lib, out=X, ot=F32, M=M) == _adapters(lib, out=X - 4 * 768 * M + 16, ot=F32, M=M) == mkq.MKQ_ERR_UNSUPPORTED
+    # hidden values are results, too
+    assert _adapters(lib, hidden=X, M=M) == _adapters(lib, hidden=X + last - 4, M=M) == mkq.MKQ_ERR_UNSUPPORTED
+    assert _adapters(lib, hidden=0x30000000, M=M) == _adapters(lib, hidden=0x30000000 - 32 * M + 4, M=M) == mkq.MKQ_ERR_UNSUPPORTED
+    # columns of one wide matrix that overlap by a vector, where rows follow each other
+    if M > 1:
+        assert _adapters(lib, ldx=1600, out=X + 2 * 760, ldo=1600, M=M) == _adapters(lib, ldx=1600, out=X + 2 * 840, ldo=1600, M=M) == mkq.MKQ_ERR_UNSUPPORTED
+
+
+def test_results_beside_the_rows_they_are_computed_from(lib):
+    M, last = 4096, 2 * 768 * 4096
+    for out in (X + last, X - last):
+        assert _adapters(lib, out=out, M=M) == mkq.MKQ_ERR_WORKSPACE
+    # columns of one wide matrix, side by side: none is written that is read
+    for at in (768, 800, 832):
+        assert _adapters(lib, ldx=1600, out=X + 2 * at, ldo=1600, M=M) == _adapters(lib, ldx=1600, out=X - 2 * at, ldo=1600, M=M) == mkq.MKQ_ERR_WORKSPACE
+    assert _adapters(lib, ldx=1600, out=X + 2 * 1600 + 2 * 800, ldo=1600, M=M) == mkq.MKQ_ERR_WORKSPACE
+    assert _adapters(lib, hidden=X + last, M=M) == _adapters(lib, hidden=X - 32 * M, M=M) == mkq.MKQ_ERR_WORKSPACE
