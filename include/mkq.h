@@ -531,6 +531,7 @@ int mkq_token_log_probs_gradient(const void *logits, int dtype, int64_t ld, int6
  * mkq_checkpoint_restore        out = act(code * step) of out_dtype (MKQ_ACT_NONE, or MKQ_ACT_GELU: what stood behind it), row stride ld_out
  * mkq_checkpoint_gelu_gradient  dx = dy (Phi(x) + x phi(x)), x = code * step; dx may be dy if type and stride are its own, otherwise it is apart
  *                               from it (else UNSUPPORTED)
+ * Codes and steps lie apart from each other, from x, and from out and dx (else UNSUPPORTED).
  * What lies between rows of out and dx is left as it is.  Any K; multiples of 8 in rows that are multiples of 16 bytes are faster.
  * mkq_low_rank_adapters_gradient reads such rows in the place of x.  M == 0 is a no-op.
  * Errors: NULL, SHAPE (group too), ALIGN, DTYPE (act too), UNSUPPORTED, HIP. */

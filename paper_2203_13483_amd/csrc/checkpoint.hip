@@ -263,6 +263,12 @@ static CheckpointParams checkpoint_params(const int8_t *codes, const float *step
     return p;
 }
 
+// Whether rows [M, K] lie apart from what is kept of them
+static bool apart_from_kept(const CheckpointParams &p, const void *rows, int dtype, int64_t ld)
+{
+    return apart(rows, dtype, ld, p.K, p.codes, MKQ_I8, p.pitch, p.pitch, p.M) && apart(rows, dtype, ld, p.K, p.steps, MKQ_F32, p.groups, p.groups, p.M);
+}
+
 }  // namespace mkq
 
 using namespace mkq;
@@ -282,6 +288,7 @@ extern "C" int mkq_checkpoint_int8(const void *x, int x_dtype, int64_t M, int64_
     if (!aligned16(x) || !aligned16(codes) || !aligned4(steps)) return MKQ_ERR_ALIGN;
     if (M > CHECKPOINT_MOST || K > COLUMNS_MOST) return MKQ_ERR_UNSUPPORTED;
     CheckpointParams p = checkpoint_params(codes, steps, group, M, K);
+    if (!apart_from_kept(p, x, x_dtype, ldx) || !apart(codes, MKQ_I8, p.pitch, p.pitch, steps, MKQ_F32, p.groups, p.groups, M)) return MKQ_ERR_UNSUPPORTED;
     p.x = x;
     p.ldx = ldx;
     p.chunks = p.groups * (group / 8);
@@ -308,6 +315,7 @@ extern "C" int mkq_checkpoint_restore(const int8_t *codes, const float *steps, i
     if (!aligned16(codes) || !aligned4(steps) || !aligned16(out)) return MKQ_ERR_ALIGN;
     if (M > CHECKPOINT_MOST || K > COLUMNS_MOST) return MKQ_ERR_UNSUPPORTED;
     CheckpointParams p = checkpoint_params(codes, steps, group, M, K);
+    if (!apart_from_kept(p, out, out_dtype, ld_out)) return MKQ_ERR_UNSUPPORTED;
     p.out = out;
     p.ld_out = ld_out;
     return act == MKQ_ACT_GELU ? launch_use<USE_GELU>(p, MKQ_F32, out_dtype, as_stream(stream))
@@ -325,6 +333,7 @@ extern "C" int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *st
     if (M > CHECKPOINT_MOST || K > COLUMNS_MOST) return MKQ_ERR_UNSUPPORTED;
     if (!in_place_or_apart(dy, dy_dtype, ld_dy, dx, dx_dtype, ld_dx, M, K)) return MKQ_ERR_UNSUPPORTED;
     CheckpointParams p = checkpoint_params(codes, steps, group, M, K);
+    if (!apart_from_kept(p, dx, dx_dtype, ld_dx)) return MKQ_ERR_UNSUPPORTED;
     p.x = dy;
     p.ldx = ld_dy;
     p.out = dx;

@@ -51,3 +51,28 @@ def test_results_beside_the_rows_they_are_computed_from(lib):
         assert _adapters(lib, ldx=1600, out=X + 2 * at, ldo=1600, M=M) == _adapters(lib, ldx=1600, out=X - 2 * at, ldo=1600, M=M) == mkq.MKQ_ERR_WORKSPACE
     assert _adapters(lib, ldx=1600, out=X + 2 * 1600 + 2 * 800, ldo=1600, M=M) == mkq.MKQ_ERR_WORKSPACE
     assert _adapters(lib, hidden=X + last, M=M) == _adapters(lib, hidden=X - 32 * M, M=M) == mkq.MKQ_ERR_WORKSPACE
+
+
+def test_activations_kept_over_what_they_are_made_of(lib):
+    """Rows are kept and read back by workgroups side by side: codes, steps and results lie apart."""
+    v, M, K, g = C.c_void_p, 100, 256, 64
+    x, codes, steps, out = X, X + 0x1000000, X + 0x2000000, X + 0x3000000
+    rows, kept, step = 2 * M * K, M * K, 4 * M * (K // g)
+
+    def keep(x=x, c=codes, s=steps, dt=F16):
+        return lib.mkq_checkpoint_int8(v(x), dt, M, K, K, g, v(c), v(s), None)
+
+    def back(c=codes, s=steps, o=out, dt=F16):
+        return lib.mkq_checkpoint_restore(v(c), v(s), g, M, K, mkq.MKQ_ACT_GELU, v(o), dt, K, None)
+
+    def slope(c=codes, s=steps, o=out, dy=x, dt=F16):
+        return lib.mkq_checkpoint_gelu_gradient(v(c), v(s), g, M, K, v(dy), dt, K, v(o), dt, K, None)
+    for at in (x, x + 16, x + rows - 16, x - kept + 16):
+        assert keep(c=at) == mkq.MKQ_ERR_UNSUPPORTED, hex(at)
+    for at in (x, x + rows - 4, x - step + 4, codes, codes + kept - 4, codes - step + 4):
+        assert keep(s=at) == mkq.MKQ_ERR_UNSUPPORTED, hex(at)
+    for f in (back, slope):
+        for at in (codes, codes + kept - 16, codes - rows + 16, steps, steps + step - 16, steps - rows + 16):
+            assert f(o=at) == mkq.MKQ_ERR_UNSUPPORTED, hex(at)
+        assert f(o=codes, dt=F32) == f(o=codes - 2 * rows + 16, dt=F32) == mkq.MKQ_ERR_UNSUPPORTED
+    assert slope(dy=codes, o=codes) == mkq.MKQ_ERR_UNSUPPORTED
