@@ -3,9 +3,10 @@
 
 namespace mkq {
 
-__device__ __forceinline__ void write_grad(const OuterParams &p, const OuterSide &side, int a, int64_t at, float v)
+// rows: how many of the batch the adapter has.  (0 times a scale that is infinite or NaN would not be the 0 of an adapter without any.)
+__device__ __forceinline__ void write_grad(const OuterParams &p, const OuterSide &side, int a, int rows, int64_t at, float v)
 {
-    v *= side.scaled ? scale_of(p.a, a) : 1.0f;
+    v *= side.scaled && rows > 0 ? scale_of(p.a, a) : 1.0f;
     at += (int64_t)a * p.a.rank * side.N;
     auto write = [&](auto o) __attribute__((always_inline)) {
         using O = decltype(o);
@@ -127,7 +128,7 @@ __device__ __forceinline__ void outer(const OuterParams &p, const OuterSide &sid
             }
         } else {
             for (int row = 0; row < rows; ++row)
-                for (int i = lane; i < columns; i += 64) write_grad(p, side, a, corner + (int64_t)row * side.N + i, tile[row * 128 + i]);
+                for (int i = lane; i < columns; i += 64) write_grad(p, side, a, n, corner + (int64_t)row * side.N + i, tile[row * 128 + i]);
         }
     }
 }
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(256) void outer_join_kernel(const OuterParams p)
         for (int k = 0; k < 8; ++k) sum += v[k];
     }
     for (; j < pieces; ++j) sum += from[j * step];
-    write_grad(p, side, a, i, sum);
+    write_grad(p, side, a, count, i, sum);
 }
 
 void launch_outer_kernel(const OuterParams &p, int x_dtype, int dy_dtype, unsigned workgroups, hipStream_t st)
