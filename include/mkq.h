@@ -561,8 +561,8 @@ int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int gr
  *               d_up may be NULL, but not all of them; what only they need may be NULL then
  *   workspace   at least the *_workspace_bytes bytes (0, for few rows: may be NULL), 16-byte aligned; no preparation.  Two calls that may run at
  *               the same time need two
- * Products are exact, all sums and hidden are binary32 (sums of products with 16-bit results may leave out 2^-16 of a product); equal calls give
- * equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
+ * All sums and hidden are binary32.  Products are exact, but that binary32 with binary32 may leave out 2^-24 of a product, and hidden values (u for dx)
+ * under 16-bit results 2^-17 of one, of either sign.  Equal calls give equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
  * rank 1 .. 256, R up to about 4e6, rank K and rank N below 2^29, K and N from 8 and, as
  * the strides of base, out, dx_base and dx, up to 2^25 (UNSUPPORTED).  M == 0: the first does nothing, the second writes its zeros.
  * Errors: NULL, SHAPE (x_group too), ALIGN, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */

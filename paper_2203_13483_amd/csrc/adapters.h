@@ -53,21 +53,32 @@ struct Adapters {
 // ---- numbers as parts -----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 __device__ __forceinline__ uint32_t lower_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-// x = sum of `parts` numbers that are the upper halves of what is left; nothing is left of an infinity, and a NaN stays one
-template <int PARTS>
+// x = sum of PARTS bfloat16 numbers, each the nearest to what is left: of three nothing is left, two leave 2^-17 of x.  (Cut off instead of rounded they
+// left up to 2^-15, always with the sign of x.)  The largest of them are the first part of what lies above; nothing is left of an infinity or a NaN.
+// HALVES: values of binary16, of which 2^8 is left at most (and of an infinity or a NaN something finite: beside the first part it makes no difference)
+template <bool HALVES = false, int PARTS>
 __device__ __forceinline__ void parts_of(const float (&x)[8], uint4 (&out)[PARTS])
 {
-    uint32_t left[8];
+    constexpr float MOST = 0x1.FEp127f;  // bfloat16's
+    float left[8];
+    bool finite[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) left[i] = x[i] != x[i] ? 0x7FC00000u : __float_as_uint(x[i]);
+    for (int i = 0; i < 8; ++i) {
+        finite[i] = HALVES || fabsf(x[i]) < __builtin_inff();
+        left[i] = !HALVES && finite[i] ? __builtin_amdgcn_fmed3f(x[i], -MOST, MOST) : x[i];
+    }
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-        out[p] = make_uint4(upper_halves(left[0], left[1]), upper_halves(left[2], left[3]), upper_halves(left[4], left[5]), upper_halves(left[6], left[7]));
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2_bf16(left[2 * i], left[2 * i + 1]);
+        out[p] = make_uint4(w[0], w[1], w[2], w[3]);
         if (p + 1 == PARTS) break;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float v = __uint_as_float(left[i]), r = v - __uint_as_float(left[i] & 0xFFFF0000u);
-            left[i] = fabsf(v) < __builtin_inff() ? __float_as_uint(r) : 0u;
+            const float part = __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+            if (HALVES) left[i] = __builtin_amdgcn_fmed3f(left[i] - part, -0x1p8f, 0x1p8f);
+            else left[i] = p == 0 ? (finite[i] ? x[i] - part : 0.0f) : left[i] - part;
         }
     }
 }
@@ -185,7 +196,7 @@ struct Block {
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = rows[j].get(i);
-            parts_of(v, out);
+            parts_of<std::is_same<E, ElemF16>::value>(v, out);
         }
     }
 };
@@ -200,7 +211,7 @@ __device__ __forceinline__ void operand(const Neighbours<E> &n, uint4 (&out)[Par
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = n.get(i);
-        parts_of(v, out);
+        parts_of<std::is_same<E, ElemF16>::value>(v, out);
     }
 }
 

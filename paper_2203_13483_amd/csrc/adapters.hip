@@ -10,8 +10,8 @@
 // TB/s), to dx 9, outer of both (x in 8 bits) 23, its join 5.
 //
 // Operands enter the products exactly: binary16 and bfloat16 as they are where both sides are the same, otherwise a number is the sum of
-// one to three bfloat16 parts (binary32 three, binary16 two), and products of parts whose places add up to 2^-24 or less are left out.
-// Sums are binary32.  A tile of rows may hold any adapters: it is gone through once for each of them, results are taken for the rows
+// one to three bfloat16 parts (binary32 three, binary16 two), each the nearest to what is left.  Of a product only that of a second part with a third, and
+// of thirds, are left out: 2^-24 of it at most, of either sign.  Sums are binary32.  A tile of rows may hold any adapters: it is gone through once for each of them, results are taken for the rows
 // that have it, so a request's infinities and NaN stay in its rows.
 #include "adapters.h"
 

@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256, W::BYTES == 4 ? 1 : 2) void few_kernel(const S
             for (int i = 0; i < 8; ++i) {
                 uint4 wp[Parts<W>::N];
                 rows.column(i, wp);
-                acc[i] = multiply<PT>(tp, wp, acc[i]);
+                acc[i] = multiply<3>(tp, wp, acc[i]);
             }
         }
         if (!mine_to_write || n0 >= p.N || (a < 0 && p.base == p.out)) continue;
