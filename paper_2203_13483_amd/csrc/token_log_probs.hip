@@ -69,7 +69,7 @@ __device__ __forceinline__ int64_t given_token(const void *tokens, int bits, int
 typedef unsigned long long Key;
 __device__ __forceinline__ uint32_t ordered(float v)
 {
-    const uint32_t b = __float_as_uint(fmaxf(v, -__builtin_inff()) + 0.0f);
+    const uint32_t b = __float_as_uint((v == v ? v : -__builtin_inff()) + 0.0f);
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
@@ -209,7 +209,7 @@ struct Eight {
         else return E::get((uint16_t)(x >> (16 * (i % 2))));
     }
 };
-// The largest of a lane's vectors, a NaN as -infinity.  (Binary16: two at a time, so that get() is only an operand of the fused product)
+// The largest of a lane's vectors, a quiet NaN as -infinity.  (Binary16: two at a time, so that get() is only an operand of the fused product)
 template <class E, int N>
 __device__ __forceinline__ float largest_of(const Eight<E> (&x)[N])
 {
@@ -394,6 +394,24 @@ __global__ __launch_bounds__(THREADS) void token_mass_kernel(const ScoreParams p
             }
         }
         if constexpr (TOP) largest[step * 64 + lane] = most;
+    }
+    // Beside a signalling NaN the unit's maximum is not the other value, but NaN, and the next maximum starts anew: a wave that has met any NaN looks
+    // for its largest scores again by comparing them.  (In the loop above, this took half of the waves' registers: 8192 rows of 30522 in 150 instead of 122 us.)
+    if (__builtin_expect(__ballot(m.sum != m.sum) != 0, 0)) {
+#pragma unroll 1
+        for (int step = wave; step < steps; step += WAVES) {
+            const int v = v0 + step * STEP;
+            float most = -__builtin_inff();
+#pragma unroll 1
+            for (int w = v; w < v + STEP && w * 8 < r.end; w += 64) {
+                Eight<E> x;
+                r.get(w + lane, true, x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = x.get(e) > most ? x.get(e) : most;
+            }
+            if constexpr (TOP) largest[step * 64 + lane] = most;
+            m.most = fmaxf(m.most, most);
+        }
     }
     m = joined(m);
     if ((threadIdx.x & 63) == 0) masses[threadIdx.x >> 6] = m;
