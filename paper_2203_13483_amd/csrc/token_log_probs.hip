@@ -25,6 +25,7 @@ constexpr int TOP_MOST = 64;
 constexpr int SCORE_UNROLL = 4;
 constexpr int STEP = 64 * SCORE_UNROLL;  // vectors of eight neighbouring scores that a wave takes at a time
 constexpr int STEPS_MOST = 64;           // of a workgroup that chooses alternatives: a lane's largest score of a step is kept, 16 KiB of LDS
+constexpr int PARTS_MOST = 1024;         // of a row: from 2^27 columns on they have more steps each, up to 128 KiB at 2^30
 
 struct ScoreParams {
     const void *logits;
@@ -624,7 +625,7 @@ static int row_parts(int64_t M, int64_t V, int top)
     const int64_t useful = ceil_div(steps, 32);     // two steps for each wave of a large workgroup
     const int64_t more = wanted < useful ? wanted : useful;
     if (more > parts) parts = more;
-    return (int)(parts < 1024 ? parts : 1024);
+    return (int)(parts < PARTS_MOST ? parts : PARTS_MOST);
 }
 
 static bool score_scale_ok(float s) { return s >= 0x1p-100f && s <= 0x1p100f; }

@@ -83,3 +83,19 @@ def test_rows_around_powers_of_two(V, exponent):
     some[:, : V // 2] = -math.inf
     tokens = torch.randint(V // 2, V, (len(rows),), generator=g, device="cuda")
     _both(some, tokens, LN2, 20)
+
+
+@pytest.mark.parametrize("V", [2 ** 28 + 3, 2 ** 30])
+def test_the_longest_rows(V):
+    z = torch.zeros(1, V, dtype=torch.bfloat16, device="cuda")
+    places = [V - 1, 0, V // 2, V - 2 ** 20, 131071, 131072 * 64, 7]
+    z[0, places] = torch.tensor([12.0 - i for i in range(7)], device="cuda").bfloat16()
+    tokens = torch.tensor([V - 1], device="cuda")
+    r = mkq.mkq_token_log_probs(z, tokens, 1.0, 10)
+    left = [p for p in range(20) if p not in places][:3]  # equal ones: the lowest tokens
+    assert r.top_tokens[0].tolist() == places + left
+    total = math.log(V - 7 + sum(math.exp(12.0 - i) for i in range(7)))
+    want = torch.tensor([12.0 - i for i in range(7)] + [0.0] * 3, dtype=torch.float64) - total
+    # (2^30 / 2^20 = 1024 terms a thread of equal powers, their joining and a logarithm: below 2^-24 (1024 + 200) of the sum)
+    assert float((r.top_log_probs[0].double().cpu() - want).abs().max()) <= 2.0 ** -24 * 1300
+    assert abs(float(r.log_probs[0]) - float(want[0])) <= 2.0 ** -24 * 1300
