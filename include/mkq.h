@@ -563,8 +563,9 @@ int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int gr
  *               the same time need two
  * All sums and hidden are binary32.  Products are exact, but that binary32 with binary32 may leave out 2^-24 of a product, and hidden values (u for dx)
  * under 16-bit results 2^-17 of one, of either sign.  Equal calls give equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
- * rank 1 .. 256, R up to about 4e6, rank K and rank N below 2^29, K and N from 8 and, as
- * the strides of base, out, dx_base and dx, up to 2^25 (UNSUPPORTED).  M == 0: the first does nothing, the second writes its zeros.
+ * rank 1 .. 256, R up to 2^22 - 1, rank K and rank N below 2^29, K and N from 8 and, as the strides of base, out, dx_base and dx, up to 2^25
+ * (UNSUPPORTED).  The gradient: R rank (K + N) below about 2^32 and, for d_down and d_up, R M up to 2^40 (UNSUPPORTED): the rows of each of the R adapters
+ * are found by reading all M numbers, which shows from about 2^26 on (R = 10^5, M = 8192: 0.7 ms).  M == 0: the first does nothing, the second writes its zeros.
  * Errors: NULL, SHAPE (x_group too), ALIGN, DTYPE, WORKSPACE, UNSUPPORTED, HIP. */
 size_t mkq_low_rank_adapters_workspace_bytes(int64_t M, int64_t K, int64_t N, int rank, int64_t R);
 int mkq_low_rank_adapters(const void *x, int x_dtype, int64_t ldx, const int32_t *adapter, int64_t M, int64_t K, int64_t N, int rank, int64_t R,

@@ -20,6 +20,7 @@ namespace mkq {
 constexpr int64_t ADAPTERS_MOST = 0x3FFFFF, SIDES_MOST = 0x7FFFFF00;
 constexpr int RANK_MOST = 256;
 constexpr int64_t STRIDE_MOST = (int64_t)1 << 25;  // elements between rows: 16 of them are addressed in 32 bits
+constexpr int64_t PLANNED_MOST = (int64_t)1 << 40;  // adapters times rows, which the plan reads: about 1e12 of them a second
 constexpr int FEW_ROWS = 512;  // up to here a tile's adapters are shared out among workgroups
 
 struct AdapterShape {
@@ -237,6 +238,7 @@ extern "C" int mkq_low_rank_adapters_gradient(const void *dy, int dy_dtype, int6
         // the batch's rows are read again behind dx
         if (!apart(dy, dy_dtype, ld_dy, N, dx, dx_dtype, ld_dx, K, M) || (d_down && !apart(x, x_dtype, pitch, K, dx, dx_dtype, ld_dx, K, M))) return MKQ_ERR_UNSUPPORTED;
     }
+    if ((d_down || d_up) && M * R > PLANNED_MOST) return MKQ_ERR_UNSUPPORTED;  // (below 2^31 and 2^22)
     const AdapterWorkspace w = gradient_workspace(d);
     if (!grid_ok(shrink_workgroups(d, w.splits) + R, 256) || (dx && M > 0 && !grid_ok(expand_workgroups(d, K), 256)) ||
         !grid_ok(outer_workgroups(d, w.tasks_most, ceil_div(K, 128) + ceil_div(N, 128)), 256) || !grid_ok(join_workgroups(d, K + N), 256))

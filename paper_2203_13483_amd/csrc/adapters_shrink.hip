@@ -3,7 +3,9 @@
 
 namespace mkq {
 
-// A workgroup of 256 has an adapter: each thread looks through neighbouring rows for those of the adapter and those of smaller ones
+// A workgroup of 256 has an adapter: each thread looks through neighbouring rows for those of the adapter and those of smaller ones.  That reads R M
+// numbers, most of them from the caches, in the launch that is there anyway: 8192 rows take as long with 1000 adapters as with 32, with 10000 80 us
+// more, with 100000 700.
 __device__ void plan(const AdapterParams &p, const PlanParams &plan, int a)
 {
     __shared__ int equal_before[4], less_before[4];

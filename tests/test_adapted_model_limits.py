@@ -76,3 +76,16 @@ def test_activations_kept_over_what_they_are_made_of(lib):
             assert f(o=at) == mkq.MKQ_ERR_UNSUPPORTED, hex(at)
         assert f(o=codes, dt=F32) == f(o=codes - 2 * rows + 16, dt=F32) == mkq.MKQ_ERR_UNSUPPORTED
     assert slope(dy=codes, o=codes) == mkq.MKQ_ERR_UNSUPPORTED
+
+
+def test_adapters_times_rows(lib):
+    """Every adapter's rows are found by reading all rows' adapters: so many that a call would hold the GPU for seconds are refused."""
+    def call(M, R, dd=0x40000000000, du=0x50000000000, dx=None):
+        v = lambda a: C.c_void_p(a) if a else None  # noqa: E731
+        return lib.mkq_low_rank_adapters_gradient(v(X), F16, 8, v(0x10000000000), F16, 8, None, 0, P, P, M, 8, 8, 1, R, P, P, F16, None, None, 0, v(dx), F16, 8,
+                                                  v(dd), v(du), F32, 0, None, 0, None)
+    for M, R in ((2 ** 20, 2 ** 20 + 1), (2 ** 26, 2 ** 15), (2 ** 19 + 1, 2 ** 21)):
+        assert call(M, R) == call(M, R, dd=None) == call(M, R, du=None) == mkq.MKQ_ERR_UNSUPPORTED, (M, R)
+    for M, R in ((2 ** 20, 2 ** 20), (2 ** 26, 2 ** 14), (2 ** 14, 2 ** 22 - 1)):
+        assert call(M, R) == mkq.MKQ_ERR_WORKSPACE, (M, R)
+    assert call(2 ** 26, 2 ** 15, dd=None, du=None, dx=0x60000000000) == mkq.MKQ_ERR_WORKSPACE
