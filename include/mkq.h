@@ -501,7 +501,7 @@ int mkq_clip_gradients(int64_t n, const void *const *grads_host, void *const *ou
  *     entropies[m]   = -sum_j p_j log p_j
  *     top_tokens[m]  = the `top` tokens with the largest scores, equal scores (0 and -0 too) by the lower token, with their log p
  *     grad[m,j]      = scale ( d_log_probs[m] (delta_jt - p_j)  -  d_entropies[m] p_j (log p_j + entropies[m]) )
- * -infinity forbids a token: p = 0, its gradient is 0.  A row of nothing else has no distribution: log probabilities and L are -infinity,
+ * -infinity forbids a token: p = 0, and its gradient is 0 but for the given token's own part, scale d_log_probs.  A row of nothing else has no distribution: log probabilities and L are -infinity,
  * the entropy is 0, its gradient zeros.  A NaN or +infinity makes its row's results NaN (a NaN is ordered as -infinity).  A row whose d_log_probs
  * (or whose token is outside) and d_entropies are 0 has zeros for a gradient, whatever its scores are.  top_log_probs have no gradient here.
  *   logits  [M, V] of dtype (F32, F16, BF16), row stride ld: any, rows are read in aligned pieces of 16 bytes
@@ -562,7 +562,7 @@ int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int gr
  *   workspace   at least the *_workspace_bytes bytes (0, for few rows: may be NULL), 16-byte aligned; no preparation.  Two calls that may run at
  *               the same time need two
  * All sums and hidden are binary32.  Products are exact, but that binary32 with binary32 may leave out 2^-24 of a product, and hidden values (u for dx)
- * under 16-bit results 2^-17 of one, of either sign.  Equal calls give equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
+ * under 16-bit results 2^-17 of one, of either sign; binary32 numbers enter as multiples of 2^-133.  Equal calls give equal bits.  Infinities and NaN of a row or an adapter reach the rows and gradients that depend on it, as infinities or NaN, and no others.
  * rank 1 .. 256, R up to 2^22 - 1, rank K and rank N below 2^29, K and N from 8 and, as the strides of base, out, dx_base and dx, up to 2^25
  * (UNSUPPORTED).  The gradient: R rank (K + N) below about 2^32 and, for d_down and d_up, R M up to 2^40 (UNSUPPORTED): the rows of each of the R adapters
  * are found by reading all M numbers, which shows from about 2^26 on (R = 10^5, M = 8192: 0.7 ms).  M == 0: the first does nothing, the second writes its zeros.

@@ -149,7 +149,7 @@ struct ShrinkParams {
 
 struct ExpandParams {
     AdapterParams a;
-    const float *t;   // [splits, M, rank]
+    const float *t;   // [splits, M, pitch]
     const void *w;    // [R, rank, N]
     const void *base; // [M, N], or NULL
     void *out;

@@ -28,7 +28,8 @@ __device__ __forceinline__ void hidden_values(const ExpandParams &p, const float
 template <class W, class O, bool ONE, class EDGE>
 __device__ __forceinline__ void expand(const ExpandParams &p, int64_t m0, int block, int slot, EDGE edge)
 {
-    constexpr int PT = O::BYTES == 4 ? 3 : 2;  // (two leave out 2^-17 of a product, of either sign, under results of 16 bits, which end at 2^-9 or 2^-12)
+    constexpr int PT = O::BYTES == 4 ? 3 : 2;  // (two leave out 2^-17 of a product, of either sign, under results of 16 bits, which end at 2^-9 or 2^-12.  With three, 8192 rows of 1024 and 4096, rank 16:
+    // bfloat16 39.3 instead of 38.9 us, binary16 53.5 instead of 49.1)
     const int last_row = p.a.M - m0 < 16 ? (int)(p.a.M - m0) - 1 : 15;
     const int first_lane = threadIdx.x & 63, mine = adapter_of(p.a, first_lane < 16 ? m0 + first_lane : p.a.M);
     Neighbours<O> base[4];

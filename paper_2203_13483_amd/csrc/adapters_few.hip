@@ -1,6 +1,6 @@
 // Few rows of short sides: hidden values and results in one launch.  A workgroup has a tile of 16 rows, an adapter of it and 512 columns, and makes
 // the hidden values for itself, as every other 512 columns' workgroup does: a launch and a round trip less for 64 KiB through the caches more.
-// Measured, us a call among others: a token each of 16 requests, 768 -> 768, rank 8, binary16 11.1 instead of 15.6; 64 rows of 64 adapters of rank 16,
+// Measured, us a call among others: a token each of 16 requests, 768 -> 768, rank 8, binary16 11.1 instead of 15.6 (the kernel 7.9); 64 rows of 64 adapters of rank 16,
 // bfloat16, 1024 -> 1024 10.9 (1025 -> 1024, in two launches, 14.6).
 #include "adapters.h"
 

@@ -4,7 +4,8 @@
 //     x' = code * step,   gelu(x') again,   dx = dy (Phi(x') + x' phi(x'))
 //
 // All are bound by bytes: each value is read once and written once.  A thread has eight neighbours, 4 to 16 lanes a group.  Measured, 16384 x 4096
-// bfloat16, us: kept 38 (5.3 TB/s), GELU again 45 (4.5 TB/s: vector issue), GELU's gradient 66 (5.1 TB/s).
+// bfloat16, us among other calls (a trace's fastest; its medians, of calls one by one, are 43, 56 and 72): kept 38 (5.3 TB/s; vector issue 29), GELU again 45
+// (4.5 TB/s; vector issue 44), GELU's gradient 66 (5.1 TB/s; vector issue 52).
 #include "gemm_common.h"
 #include "neighbours.h"
 

@@ -5,8 +5,9 @@
 //     dx_j = scale (g (delta_jt - p_j) - h p_j (log p_j + H))
 //
 // Bound by bytes: the scores are read once (and read once more and written for the gradient).  What a score costs beside its load is
-// vector issue: a fused product, an exponential, two sums and a maximum.  Measured, us: 8192 binary16 rows of 30522 with 20 alternatives
-// 115 (4.3 TB/s; vector issue alone 81), 2048 bfloat16 rows of 131072 122 (4.4 TB/s) and their gradient 169 (6.3 TB/s); one binary32 row of 30522 11.
+// vector issue: a fused product, an exponential, two sums and a maximum.  Measured, us a call among others (where calls come
+// one by one, as in a trace, large ones take up to a fifth more): 8192 binary16 rows of 30522 with 20 alternatives 115 (4.3 TB/s; vector issue alone 81),
+// 2048 bfloat16 rows of 131072 122 (4.4 TB/s) and their gradient 169 (6.3 TB/s); the kernel of one binary32 row of 30522 11.7.
 //
 // Rows of any alignment: with `shift` = the place of a row's first score modulo eight, the row is cut at multiples of eight
 // counted from shift places before it, so that all whole vectors of eight are aligned to 16 bytes whatever the row stride is.
