@@ -513,7 +513,8 @@ int mkq_clip_gradients(int64_t n, const void *const *grads_host, void *const *ou
  *   grad    [M, V] of grad_dtype (F32, F16, BF16), row stride ld_grad (what lies between the rows is left as it is); the logits themselves if type
  *           and stride are theirs, otherwise apart from them (else UNSUPPORTED).  Strides that differ by no multiple of 8 are slower.
  *   d_log_probs [M];  d_entropies [M], or NULL (then entropies may be NULL)
- * Exponents and sums are binary32, log probabilities are off by about 1e-7 plus as much of their own size.  Equal calls give equal bits.
+ * Exponents and sums are binary32 (a probability below 2^-126 counts as 0), log probabilities are off by about 1e-7 plus as much of their own size.
+ * Equal calls give equal bits.
  * M == 0 is a no-op.  Errors: NULL, SHAPE (top > V too), ALIGN, SCALE, DTYPE (token_bits too), WORKSPACE, UNSUPPORTED (top > 64), HIP. */
 size_t mkq_token_log_probs_workspace_bytes(int64_t M, int64_t V, int top);
 int mkq_token_log_probs(const void *logits, int dtype, int64_t ld, int64_t M, int64_t V, float scale, const void *tokens, int token_bits,
