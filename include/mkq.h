@@ -559,7 +559,8 @@ int mkq_checkpoint_gelu_gradient(const int8_t *codes, const float *steps, int gr
  *               What lies between the rows is left as it is
  *   hidden      [M, rank] binary32: an output of the first, apart from x and out, or NULL; needed for d_up
  *   d_down, d_up  [R, rank, K], [R, rank, N] of grad_dtype (F32, F16, BF16); accumulate: added to what is there, with one rounding.  dx, d_down and
- *               d_up may be NULL, but not all of them; what only they need may be NULL then
+ *               d_up may be NULL, but not all of them; what only they need may be NULL then.  They lie apart from each other, dx, dy, x and hidden, and dx
+ *               from hidden (else UNSUPPORTED)
  *   workspace   at least the *_workspace_bytes bytes (0, for few rows: may be NULL), 16-byte aligned; no preparation.  Two calls that may run at
  *               the same time need two
  * All sums and hidden are binary32.  Products are exact, but that binary32 with binary32 may leave out 2^-24 of a product, and hidden values (u for dx)

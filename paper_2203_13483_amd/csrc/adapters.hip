@@ -134,6 +134,15 @@ static AdapterWorkspace gradient_workspace(const AdapterShape &d)
     return w;
 }
 
+// Memory from an address on
+struct Extent {
+    uintptr_t from, to;
+    Extent(const void *p, int64_t rows, int64_t ld, int64_t cols, int dtype)
+        : from(reinterpret_cast<uintptr_t>(p)),
+          to(p && rows > 0 ? from + (uintptr_t)(((unsigned __int128)(rows - 1) * (uint64_t)ld + (uint64_t)cols) * (uint64_t)(is_float_dtype(dtype) ? dtype_bytes(dtype) : 1)) : from) {}
+    bool apart(const Extent &o) const { return from == to || o.from == o.to || to <= o.from || o.to <= from; }
+};
+
 static int launch_outer(const AdapterShape &d, OuterParams p, int x_dtype, int dy_dtype, hipStream_t st)
 {
     p.rank_chunks = (int)ceil_div(d.rank, 16 * outer_tiles(d.rank));
@@ -246,6 +255,15 @@ extern "C" int mkq_low_rank_adapters_gradient(const void *dy, int dy_dtype, int6
         return MKQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < w.total) return MKQ_ERR_WORKSPACE;
     if (!aligned16(workspace)) return MKQ_ERR_ALIGN;
+    {  // the rows, hidden values and other results are read or written beside the gradients, and hidden values behind dx
+        const int64_t groups = d_down && kept ? ceil_div(K, x_group) : 0;
+        const Extent to_down(d_down, R * rank, K, K, grad_dtype), to_up(d_up, R * rank, N, N, grad_dtype), to_dx(dx, M, ld_dx, K, dx_dtype);
+        const Extent read[] = {{dy, M, ld_dy, N, dy_dtype}, {d_down ? x : nullptr, M, pitch, K, x_dtype}, {d_down && kept ? x_steps : nullptr, M, groups, groups, MKQ_F32},
+                               {d_up ? hidden : nullptr, M, rank, rank, MKQ_F32}};
+        bool fine = to_down.apart(to_up) && to_down.apart(to_dx) && to_up.apart(to_dx) && to_dx.apart(read[3]);
+        for (const Extent &r : read) fine = fine && to_down.apart(r) && to_up.apart(r);
+        if (!fine) return MKQ_ERR_UNSUPPORTED;
+    }
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     const hipStream_t st = as_stream(stream);
     const AdapterParams a = {adapter, scales, M, (int)R, rank, pitch_of(rank), dx && M > 0 ? w.splits : 1};

@@ -89,3 +89,28 @@ def test_adapters_times_rows(lib):
     for M, R in ((2 ** 20, 2 ** 20), (2 ** 26, 2 ** 14), (2 ** 14, 2 ** 22 - 1)):
         assert call(M, R) == mkq.MKQ_ERR_WORKSPACE, (M, R)
     assert call(2 ** 26, 2 ** 15, dd=None, du=None, dx=0x60000000000) == mkq.MKQ_ERR_WORKSPACE
+
+
+def test_gradients_over_what_they_are_computed_from(lib):
+    """The batch's rows, the hidden values and the other results are read or written beside the adapters' gradients."""
+    M, K, N, rank, R = 100, 64, 96, 8, 3
+    at = dict(dy=X, x=X + 0x1000000, hidden=X + 0x2000000, dx=X + 0x3000000, dd=X + 0x4000000, du=X + 0x5000000, steps=X + 0x6000000)
+    size = dict(dy=2 * M * N, x=2 * M * K, hidden=4 * M * rank, dx=2 * M * K, dd=4 * R * rank * K, du=4 * R * rank * N, steps=4 * M)
+    need = lib.mkq_low_rank_adapters_gradient_workspace_bytes(M, K, N, rank, R)
+
+    def call(**kw):
+        a = dict(at, **kw)
+        v = lambda name: C.c_void_p(a[name]) if a[name] else None  # noqa: E731
+        kept = a.get("kept", False)
+        return lib.mkq_low_rank_adapters_gradient(v("dy"), F16, N, v("x"), mkq.MKQ_I8 if kept else F16, K, v("steps"), 64, P, v("hidden"), M, K, N, rank, R, P, P, F16, None,
+                                                  None, 0, v("dx"), F16, K, v("dd"), v("du"), F32, 0, P, need, None)
+    for result in ("dd", "du"):
+        for other in ("dy", "x", "hidden", "dx", "du" if result == "dd" else "dd"):
+            for to in (at[other], at[other] + size[other] - 16, at[other] - size[result] + 16):
+                assert call(**{result: to}) == mkq.MKQ_ERR_UNSUPPORTED, (result, other, hex(to))
+        assert call(kept=True, **{result: at["steps"] + size["steps"] - 16}) == mkq.MKQ_ERR_UNSUPPORTED
+    for to in (at["hidden"], at["hidden"] + size["hidden"] - 16, at["hidden"] - size["dx"] + 16):
+        assert call(dx=to) == mkq.MKQ_ERR_UNSUPPORTED
+    # what is not read or written does not count
+    assert call(dx=None, dd=None, hidden=None, du=at["dy"] + 16) == mkq.MKQ_ERR_NULL
+    assert call(dd=None, du=at["dy"]) == call(du=None, dd=at["x"]) == mkq.MKQ_ERR_UNSUPPORTED
